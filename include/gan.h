@@ -309,6 +309,82 @@ gan_status gan_op_dropout(gan_ctx* ctx, void* x, const int32_t* offs, int32_t n_
 gan_status gan_op_w3_to_w4(gan_ctx* ctx, const float* w3, void* w4, void* w4t, int32_t n_groups, int32_t cb, int32_t cs);
 gan_status gan_op_dw4_to_dw3(gan_ctx* ctx, const float* dw4, float* dw3, int32_t n_groups, int32_t cb, int32_t cs);
 
+/* ---- operators for label experts that are not DC-CGANs ------------------------------------------------------------
+   Rows of many labels stand in one matrix, one label's behind the other's, and every label has weights of its own
+   (an expert): the root-mean-square norm, the products grouped by label, and the optimiser step over all tensors.
+   None needs a context.  All matrices are row-major and DEVICE; a stride is the number of elements from one row to the
+   next, at least the row's length.  Any length, stride and alignment of the element's own size is taken (multiples of
+   16 bytes run faster), up to 2^30 rows and 2^28 elements a row; offsets into tensors are 64-bit.  `precision` is the storage
+   type: GAN_FP32, or GAN_BF16_FP32MASTER for bf16 matrices; sums and statistics are fp32.
+   Every call enqueues its kernels on hip_stream (a hipStream_t of the current device, 0 = the null stream) and returns
+   without waiting; nothing is allocated or kept, so calls may be captured into a graph.  Every sum runs in an order
+   fixed by sizes and offsets: results are the same bit for bit from run to run.  Zero rows or zero groups are valid.
+   Refusals (GAN_E_ARG, GAN_E_SHAPE) come before anything is launched; gan_operator_last_error has the reason (text of the calling
+   thread's last failed call, never NULL).
+
+   8-bit matrices: e4m3 values in rows padded to a multiple of 128 with zeros, uint8 [rows][padded], and one byte E + 127 for each 128
+   neighbours of a row, uint8 [rows][padded/128]: an element is code * 2^E.  E is the least in [-126, 127] with |value| <= 448 * 2^E for the
+   block's finite values, codes are rounded to nearest even; infinities and NaN become the NaN code 0x7f.  Both 16-byte aligned (the bytes of the
+   scales: any alignment). */
+const char* gan_operator_last_error(void);
+
+/* sum = x + residual, in the storage type; y = sum * inv_rms * gain with inv_rms = 1 / sqrt(mean(sum^2) + eps), computed
+   from the sum as it is stored.  residual NULL: sum = x.  Outputs, any of which may be NULL: sum [rows][cols], y [rows][cols], y8
+   and y8_scale (both or neither: y in 8 bits), inv_rms fp32 [rows].  gain: fp32 [cols].  sum may be the memory of x or of residual, y that of x,
+   if the strides are the same. */
+gan_status gan_rms_norm(int32_t precision, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const float* gain, float eps,
+                        int64_t rows, int32_t cols, void* sum, int64_t sum_stride, void* y, int64_t y_stride, uint8_t* y8, uint8_t* y8_scale,
+                        float* inv_rms, void* hip_stream);
+/* Its gradient: dx [rows][cols], that of x and of residual alike, from dy (of y), sum and inv_rms as the forward call left them, and dsum, the
+   gradient that reaches sum by other ways (or NULL): with h = gain * dy, dx = inv_rms * (h - sum * inv_rms^2 * mean(h * sum)) + dsum.
+   dgain fp32 [cols] = sum over the rows of dy * sum * inv_rms, or NULL.  dx may be the memory of dy or dsum, if the strides are the same.  work: DEVICE,
+   gan_rms_norm_backward_bytes(rows, cols), 16-byte aligned. */
+int64_t gan_rms_norm_backward_bytes(int64_t rows, int32_t cols);
+gan_status gan_rms_norm_backward(int32_t precision, const void* dy, int64_t dy_stride, const void* sum, int64_t sum_stride, const float* gain,
+                                 const float* inv_rms, const void* dsum, int64_t dsum_stride, int64_t rows, int32_t cols, void* dx, int64_t dx_stride,
+                                 float* dgain, void* work, int64_t work_bytes, void* hip_stream);
+/* A matrix into 8 bits: weights once, or activations that no norm precedes. */
+gan_status gan_quantize8(int32_t precision, const void* x, int64_t x_stride, int64_t rows, int32_t cols, uint8_t* q, uint8_t* scale, void* hip_stream);
+
+/* Products grouped by label: rows offs[g] .. offs[g+1] - 1 are expert g's.  offs: DEVICE int32 [groups + 1], not decreasing, offs[0] = 0 (as
+   gan_get_routing reports them; an entry below the one before it or outside [0, rows] counts as that one or as the nearest inside);
+   rows from offs[groups] on belong to no expert: their results are zero.  w [groups][n_out][n_in] in the storage type.
+     gan_group_linear       y[i] = w[g] x[i]                       [rows][n_out]
+     gan_group_linear_dgrad dx[i] = dy[i] w[g]                     [rows][n_in]
+     gan_group_linear_wgrad dw[g] = sum of dy[i]^T x[i] over g's i  fp32 [groups][n_out][n_in], zero for an expert without rows
+     gan_group_linear8      y[i] = w[g] x[i] of 8-bit matrices: x8 [rows][padded n_in], w8 [groups][n_out][padded n_in]; y in y_precision
+   fp32 products are sums of products of three bf16 parts of every value, as in the training step (or of fp32 values, where experts have few rows).
+   work: DEVICE, gan_group_linear_wgrad_bytes(...) (0: none is needed, and work may be NULL), 16-byte aligned.  At most 65535 groups. */
+gan_status gan_group_linear(int32_t precision, const void* x, int64_t x_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows,
+                            int32_t n_in, int32_t n_out, void* y, int64_t y_stride, void* hip_stream);
+gan_status gan_group_linear_dgrad(int32_t precision, const void* dy, int64_t dy_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows,
+                                  int32_t n_in, int32_t n_out, void* dx, int64_t dx_stride, void* hip_stream);
+int64_t gan_group_linear_wgrad_bytes(int32_t groups, int64_t rows, int32_t n_in, int32_t n_out);
+gan_status gan_group_linear_wgrad(int32_t precision, const void* x, int64_t x_stride, const void* dy, int64_t dy_stride, const int32_t* offs, int32_t groups,
+                                  int64_t rows, int32_t n_in, int32_t n_out, float* dw, void* work, int64_t work_bytes, void* hip_stream);
+gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scale, const uint8_t* w8, const uint8_t* w_scale, const int32_t* offs, int32_t groups,
+                             int64_t rows, int32_t n_in, int32_t n_out, int32_t y_precision, void* y, int64_t y_stride, void* hip_stream);
+
+/* AdamW over many tensors in one launch.  The handle holds where they are (HOST arrays of DEVICE pointers, read by gan_adamw_create) and nothing that
+   a step changes: params[t] fp32 [sizes[t]], grads[t] in grad_precision, copies[t] (copies or an entry may be NULL) a bf16 copy that every step writes,
+   decay[t] the tensor's weight decay (decay NULL: none).  The moments are the caller's, of all tensors in one array each, tensor t's from element
+   128 * (blocks of 128 of the tensors before it) on, gan_adamw_blocks in all; all bytes zero at the start.
+     state_bits 32: m and v fp32, 128 * blocks elements each; m_scale and v_scale NULL
+     state_bits 8 : m and v uint8, 128 * blocks each, m_scale and v_scale uint8 [blocks]: m and the square root of the second moment in the
+                    8-bit format above, rounded up or down with the probability of the part cut off (a step changes a moment by less than
+                    half a code, which rounding to nearest would undo for ever): by floor(|x| / ulp + u / 65536), u = bits 0 .. 15 (m) and 16 .. 31
+                    (v) of a 32-bit mix of the element's index in these arrays, the step number and the seed.  What is not zero never becomes zero in v.
+   A step, with t = step >= 1, every operation rounded to fp32 on its own:
+     m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+     p = p (1 - lr decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps) */
+typedef struct gan_adamw gan_adamw;
+int64_t gan_adamw_blocks(int32_t tensors, const int64_t* sizes);
+gan_status gan_adamw_create(int32_t tensors, const int64_t* sizes, float* const* params, const void* const* grads, int32_t grad_precision, void* const* copies,
+                            const float* decay, int32_t state_bits, void* m, void* v, uint8_t* m_scale, uint8_t* v_scale, gan_adamw** out);
+gan_status gan_adamw_step(gan_adamw* h, double lr, double beta1, double beta2, double eps, int64_t step, uint32_t seed, void* hip_stream);
+/* Waits for the device's work before it frees the handle's table. */
+gan_status gan_adamw_destroy(gan_adamw* h);
+
 #ifdef __cplusplus
 }
 #endif

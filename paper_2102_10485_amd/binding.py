@@ -98,8 +98,101 @@ def load_library():
     L.gan_static_last_error.restype = C.c_char_p
     L.gan_probe_mfma.argtypes = [C.c_int32, _VP, C.POINTER(C.c_double)]
     L.gan_probe_copy.argtypes = [C.c_int64, _VP, C.POINTER(C.c_double)]
+    i32, i64, dbl = C.c_int32, C.c_int64, C.c_double
+    L.gan_operator_last_error.restype = C.c_char_p
+    L.gan_rms_norm.argtypes = [i32, _VP, i64, _VP, i64, _VP, C.c_float, i64, i32, _VP, i64, _VP, i64, _VP, _VP, _VP, _VP]
+    L.gan_rms_norm_backward_bytes.argtypes, L.gan_rms_norm_backward_bytes.restype = [i64, i32], i64
+    L.gan_rms_norm_backward.argtypes = [i32, _VP, i64, _VP, i64, _VP, _VP, _VP, i64, i64, i32, _VP, i64, _VP, _VP, i64, _VP]
+    L.gan_quantize8.argtypes = [i32, _VP, i64, i64, i32, _VP, _VP, _VP]
+    L.gan_group_linear.argtypes = L.gan_group_linear_dgrad.argtypes = [i32, _VP, i64, _VP, _VP, i32, i64, i32, i32, _VP, i64, _VP]
+    L.gan_group_linear_wgrad_bytes.argtypes, L.gan_group_linear_wgrad_bytes.restype = [i32, i64, i32, i32], i64
+    L.gan_group_linear_wgrad.argtypes = [i32, _VP, i64, _VP, i64, _VP, i32, i64, i32, i32, _VP, _VP, i64, _VP]
+    L.gan_group_linear8.argtypes = [_VP, _VP, _VP, _VP, _VP, i32, i64, i32, i32, i32, _VP, i64, _VP]
+    L.gan_adamw_blocks.argtypes, L.gan_adamw_blocks.restype = [i32, _I64P], i64
+    L.gan_adamw_create.argtypes = [i32, _I64P, C.POINTER(_VP), C.POINTER(_VP), i32, C.POINTER(_VP), _FP, i32, _VP, _VP, _VP, _VP, C.POINTER(_VP)]
+    L.gan_adamw_step.argtypes = [_VP, dbl, dbl, dbl, dbl, i64, C.c_uint32, _VP]
+    L.gan_adamw_destroy.argtypes = [_VP]
     _lib = L
     return L
+
+
+# operators for label experts (device pointers as integers, 0 for none)
+def _operator(status):
+    if status != GAN_OK:
+        raise GanError(status, (_lib.gan_operator_last_error() or b"").decode())
+
+
+def rms_norm(precision, x, x_stride, residual, residual_stride, gain, eps, rows, cols, total, total_stride, y, y_stride, y8, y8_scale, inv_rms, stream=0):
+    _operator(load_library().gan_rms_norm(precision, x, x_stride, residual, residual_stride, gain, eps, rows, cols, total, total_stride, y, y_stride,
+                                          y8, y8_scale, inv_rms, stream))
+
+
+def rms_norm_backward_bytes(rows, cols):
+    return load_library().gan_rms_norm_backward_bytes(rows, cols)
+
+
+def rms_norm_backward(precision, dy, dy_stride, total, total_stride, gain, inv_rms, dtotal, dtotal_stride, rows, cols, dx, dx_stride, dgain, work, work_bytes,
+                      stream=0):
+    _operator(load_library().gan_rms_norm_backward(precision, dy, dy_stride, total, total_stride, gain, inv_rms, dtotal, dtotal_stride, rows, cols, dx, dx_stride,
+                                                   dgain, work, work_bytes, stream))
+
+
+def quantize8(precision, x, x_stride, rows, cols, q, scale, stream=0):
+    _operator(load_library().gan_quantize8(precision, x, x_stride, rows, cols, q, scale, stream))
+
+
+def group_linear(precision, x, x_stride, w, offs, groups, rows, n_in, n_out, y, y_stride, stream=0):
+    _operator(load_library().gan_group_linear(precision, x, x_stride, w, offs, groups, rows, n_in, n_out, y, y_stride, stream))
+
+
+def group_linear_dgrad(precision, dy, dy_stride, w, offs, groups, rows, n_in, n_out, dx, dx_stride, stream=0):
+    _operator(load_library().gan_group_linear_dgrad(precision, dy, dy_stride, w, offs, groups, rows, n_in, n_out, dx, dx_stride, stream))
+
+
+def group_linear_wgrad_bytes(groups, rows, n_in, n_out):
+    return load_library().gan_group_linear_wgrad_bytes(groups, rows, n_in, n_out)
+
+
+def group_linear_wgrad(precision, x, x_stride, dy, dy_stride, offs, groups, rows, n_in, n_out, dw, work, work_bytes, stream=0):
+    _operator(load_library().gan_group_linear_wgrad(precision, x, x_stride, dy, dy_stride, offs, groups, rows, n_in, n_out, dw, work, work_bytes, stream))
+
+
+def group_linear8(x8, x_scale, w8, w_scale, offs, groups, rows, n_in, n_out, y_precision, y, y_stride, stream=0):
+    _operator(load_library().gan_group_linear8(x8, x_scale, w8, w_scale, offs, groups, rows, n_in, n_out, y_precision, y, y_stride, stream))
+
+
+def adamw_blocks(sizes):
+    """Blocks of 128 values that the moments of tensors of these sizes take."""
+    return load_library().gan_adamw_blocks(len(sizes), (C.c_int64 * len(sizes))(*sizes))
+
+
+class AdamW:
+    """The step over many tensors: sizes, and device pointers of each; copies and decay may be None."""
+
+    def __init__(self, sizes, params, grads, grad_precision, copies, decay, state_bits, m, v, m_scale=0, v_scale=0):
+        self.lib = load_library()
+        self.h = _VP()
+        n = len(sizes)
+        if len(params) != n or len(grads) != n or (copies is not None and len(copies) != n) or (decay is not None and len(decay) != n):
+            raise GanError(GAN_E_ARG, "one entry for each tensor is wanted")
+        pointers = _VP * n
+        _operator(self.lib.gan_adamw_create(n, (C.c_int64 * n)(*sizes), pointers(*params), pointers(*grads), grad_precision,
+                                            None if copies is None else pointers(*copies), None if decay is None else (C.c_float * n)(*decay),
+                                            state_bits, m, v, m_scale, v_scale, C.byref(self.h)))
+
+    def step(self, lr, beta1, beta2, eps, step, seed=0, stream=0):
+        _operator(self.lib.gan_adamw_step(self.h, lr, beta1, beta2, eps, step, seed, stream))
+
+    def close(self):
+        if self.h:
+            self.lib.gan_adamw_destroy(self.h)
+            self.h = _VP()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def anova_f_static(label_ids_ptr, images_ptr, n, n_labels, img_c, img_hw, stream=0):

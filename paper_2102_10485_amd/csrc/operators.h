@@ -1,0 +1,116 @@
+// What the operators for label experts share: refusals, the 8-bit format, vectors of eight elements.
+#pragma once
+
+#include "../../include/gan.h"
+#include "common.h"
+
+namespace gan {
+
+gan_status operator_fail(gan_status s, const char* why);          // records the calling thread's text and returns s
+gan_status operator_launched();                                   // GAN_OK, or GAN_E_HIP with the runtime's text
+
+constexpr int BLOCK8 = 128;                                       // neighbours that share a scale
+__host__ __device__ inline long long padded8(long long cols) { return (cols + BLOCK8 - 1) / BLOCK8 * BLOCK8; }
+
+// Eight neighbouring elements as fp32, from 16-byte aligned memory (VEC), or one by one where fewer than eight are left or the
+// memory is not aligned; what is missing is zero.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
+  if constexpr (VEC) {
+    if (left <= 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    } else if constexpr (sizeof(T) == 4) {
+      const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+      const uint4 a = *reinterpret_cast<const uint4*>(p);
+      const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.f;
+  }
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T* p, int left, const float (&v)[8]) {
+  if constexpr (VEC) {
+    if (left <= 0) return;
+    if constexpr (sizeof(T) == 4) {
+      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      *reinterpret_cast<uint4*>(p) = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i] = from_float<T>(v[i]);
+  }
+}
+
+// ---- the 8-bit format: e4m3 times one power of two for 128 neighbours, which 16 lanes hold, eight each ----
+
+__device__ __forceinline__ bool finite_bits(unsigned magnitude) { return magnitude < 0x7f800000u; }
+
+// The block's scale byte E + 127: the least E in [-126, 127] with every finite |value| <= 448 * 2^E = 1.75 * 2^(E+8).  The bits of the largest
+// magnitude carry into the exponent where its mantissa is above 1.75.
+__device__ __forceinline__ int scale_byte(const float (&v)[8]) {
+  unsigned top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const unsigned a = __float_as_uint(v[i]) & 0x7fffffffu;
+    top = max(top, finite_bits(a) ? a : 0u);
+  }
+#pragma unroll
+  for (int d = 1; d < 16; d *= 2) top = max(top, (unsigned)__shfl_xor((int)top, d));
+  return max((int)((top + 0x1fffffu) >> 23) - 8, 1);
+}
+__device__ __forceinline__ float power_of_two(int biased) { return __uint_as_float((unsigned)biased << 23); }    // biased in [1, 254]; 0 gives 0
+
+// Rounded to nearest even.  Scaled values are within +-448, where the conversion needs no saturation.
+__device__ __forceinline__ unsigned to_e4m3_x4(float a, float b, float c, float d) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
+__device__ __forceinline__ uint2 to_e4m3_x8(const float (&v)[8], int byte) {
+  const float f = power_of_two(254 - byte);
+  float s[8];
+  unsigned bad = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    s[i] = v[i] * f;
+    bad |= (finite_bits(__float_as_uint(v[i]) & 0x7fffffffu) ? 0u : 1u) << i;
+  }
+  uint2 q = make_uint2(to_e4m3_x4(s[0], s[1], s[2], s[3]), to_e4m3_x4(s[4], s[5], s[6], s[7]));
+  if (bad) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (bad >> i & 1) {
+        unsigned& w = i < 4 ? q.x : q.y;
+        w = (w & ~(0xffu << 8 * (i & 3))) | 0x7fu << 8 * (i & 3);
+      }
+  }
+  return q;
+}
+__device__ __forceinline__ void from_e4m3_x8(uint2 q, int byte, float (&v)[8]) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const float f = power_of_two(byte);
+  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.x, true);
+  const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.y, false), d = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.y, true);
+  v[0] = a.x * f; v[1] = a.y * f; v[2] = b.x * f; v[3] = b.y * f;
+  v[4] = c.x * f; v[5] = c.y * f; v[6] = d.x * f; v[7] = d.y * f;
+}
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// whether rows of this matrix start at multiples of 16 bytes (no matrix: yes)
+inline bool rows_aligned16(const void* p, long long stride, int esize) { return aligned16(p) && stride * esize % 16 == 0; }
+
+}  // namespace gan

@@ -1,0 +1,418 @@
+// The root-mean-square norm of rows with the residual's addition, its gradient, and matrices into 8 bits.
+//
+//   sum = round(x + residual), inv = 1 / sqrt(mean(sum^2) + eps), y = sum * inv * gain
+//
+// Bound by memory: one pass over x and residual, six operations an element.  A row is held in registers between the sum of its squares and
+// its output, by one wave (rows up to 2048 elements, where no barrier is needed), a block of four waves, or one of sixteen; rows beyond
+// 32768 elements (16384 in the gradient) are read a second time.
+#include "operators.h"
+
+namespace gan {
+namespace {
+
+constexpr int E = 8;                                              // elements of a lane's chunk
+
+template <int WAVES>
+__device__ __forceinline__ float row_total(float v, float* scratch) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+  if constexpr (WAVES > 1) {
+    __syncthreads();                                              // (what the last row left in scratch has been read)
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = scratch[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v += scratch[w];
+  }
+  return v;
+}
+
+struct NormArgs {
+  const void *x, *residual;
+  const float* gain;
+  void *sum, *y;
+  uint8_t *y8, *y8_scale;
+  float* inv_rms;
+  long long x_stride, residual_stride, sum_stride, y_stride, rows;
+  int cols;
+  float eps;
+};
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void add_rounded(float (&v)[E], const T* residual, int left) {
+  float r[E];
+  load8<T, VEC>(residual, left, r);
+#pragma unroll
+  for (int i = 0; i < E; ++i) v[i] = to_float(from_float<T>(v[i] + r[i]));
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void write_chunk(const NormArgs& a, long long row, int col, const float (&s)[E], float inv) {
+  float g[E], y[E];
+  load8<float, VEC>(a.gain + col, a.cols - col, g);
+#pragma unroll
+  for (int i = 0; i < E; ++i) y[i] = s[i] * inv * g[i];
+  if (a.y) store8<T, VEC>((T*)a.y + row * a.y_stride + col, a.cols - col, y);
+  if (a.y8) {                                                     // the sixteen lanes of a block of 128 are here together, or none is
+    const long long padded = padded8(a.cols);
+    const int byte = scale_byte(y);
+    *reinterpret_cast<uint2*>(a.y8 + row * padded + col) = to_e4m3_x8(y, byte);
+    if ((threadIdx.x & 15) == 0) a.y8_scale[(row * padded + col) / BLOCK8] = (uint8_t)byte;
+  }
+}
+
+// WAVES waves a row, lane l of them holding the chunks l, l + 64 WAVES, ...; blocks of four rows where a row is a wave's
+template <typename T, int WAVES, int CHUNKS, bool VEC>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_kernel(NormArgs a) {
+  __shared__ float scratch[WAVES];
+  const long long row = WAVES == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  if (row >= a.rows) return;                                      // (whole waves; blocks of several waves have one row)
+  const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+  float s[CHUNKS][E];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int col = (c * 64 * WAVES + lane) * E;
+    load8<T, VEC>((const T*)a.x + row * a.x_stride + col, a.cols - col, s[c]);
+  }
+  if (a.residual)
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const int col = (c * 64 * WAVES + lane) * E;
+      add_rounded<T, VEC>(s[c], (const T*)a.residual + row * a.residual_stride + col, a.cols - col);
+    }
+  float q = 0.f;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int col = (c * 64 * WAVES + lane) * E;
+    if (a.sum) store8<T, VEC>((T*)a.sum + row * a.sum_stride + col, a.cols - col, s[c]);
+#pragma unroll
+    for (int i = 0; i < E; ++i) q += s[c][i] * s[c][i];
+  }
+  const float inv = 1.f / sqrtf(row_total<WAVES>(q, scratch) / (float)a.cols + a.eps);
+  if (a.inv_rms && lane == 0) a.inv_rms[row] = inv;
+  if (!a.y && !a.y8) return;
+  const int wide = (int)padded8(a.cols);
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int col = (c * 64 * WAVES + lane) * E;
+    if (col < wide) write_chunk<T, VEC>(a, row, col, s[c], inv);
+  }
+}
+
+// Rows of any length: the sum is formed again for the output (from `sum`, where it was stored over an operand).
+template <typename T, bool VEC>
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
+  __shared__ float scratch[16];
+  const long long row = blockIdx.x;
+  const T* x = (const T*)a.x + row * a.x_stride;
+  const T* residual = a.residual ? (const T*)a.residual + row * a.residual_stride : nullptr;
+  T* sum = a.sum ? (T*)a.sum + row * a.sum_stride : nullptr;
+  float q = 0.f, s[E];
+  for (int col = threadIdx.x * E; col < a.cols; col += 1024 * E) {
+    load8<T, VEC>(x + col, a.cols - col, s);
+    if (residual) add_rounded<T, VEC>(s, residual + col, a.cols - col);
+    if (sum) store8<T, VEC>(sum + col, a.cols - col, s);
+#pragma unroll
+    for (int i = 0; i < E; ++i) q += s[i] * s[i];
+  }
+  const float inv = 1.f / sqrtf(row_total<16>(q, scratch) / (float)a.cols + a.eps);
+  if (a.inv_rms && threadIdx.x == 0) a.inv_rms[row] = inv;
+  if (!a.y && !a.y8) return;
+  const int wide = (int)padded8(a.cols);
+  for (int col = threadIdx.x * E; col < wide; col += 1024 * E) {
+    if (sum) {
+      load8<T, VEC>(sum + col, a.cols - col, s);                  // (this thread's own stores)
+    } else {
+      load8<T, VEC>(x + col, a.cols - col, s);
+      if (residual) add_rounded<T, VEC>(s, residual + col, a.cols - col);
+    }
+    write_chunk<T, VEC>(a, row, col, s, inv);
+  }
+}
+
+template <typename T, bool VEC>
+void launch_norm(const NormArgs& a, hipStream_t st) {
+  const long long cols = a.cols;
+  const unsigned rows = (unsigned)a.rows, by4 = (unsigned)((a.rows + 3) / 4);
+#define GAN_NORM(W, C) hipLaunchKernelGGL((norm_kernel<T, W, C, VEC>), dim3(W == 1 ? by4 : rows), dim3(W == 1 ? 256 : 64 * W), 0, st, a)
+  if (cols <= 512) GAN_NORM(1, 1);
+  else if (cols <= 1024) GAN_NORM(1, 2);
+  else if (cols <= 2048) GAN_NORM(1, 4);
+  else if (cols <= 4096) GAN_NORM(4, 2);
+  else if (cols <= 8192) GAN_NORM(4, 4);
+  else if (cols <= 16384) GAN_NORM(16, 2);
+  else if (cols <= 32768) GAN_NORM(16, 4);
+  else hipLaunchKernelGGL((norm_long_kernel<T, VEC>), dim3(rows), dim3(1024), 0, st, a);
+#undef GAN_NORM
+}
+
+// ---- gradient ----
+
+struct NormBackArgs {
+  const void *dy, *sum, *dsum;
+  const float *gain, *inv_rms;
+  void* dx;
+  float* partial;                                                 // [blocks][cols]: the gain's gradient of each block's rows, or NULL
+  long long dy_stride, sum_stride, dsum_stride, dx_stride, rows;
+  int cols;
+};
+
+// A row's share of the gain's gradient stays in its lanes' registers over all rows of the wave; four waves of one row each are joined
+// at the end.
+template <typename T, int WAVES, int CHUNKS, bool VEC>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_back_kernel(NormBackArgs a) {
+  __shared__ float scratch[WAVES == 1 ? 4 * 64 * E : WAVES];
+  const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int wave = WAVES == 1 ? threadIdx.x >> 6 : 0;
+  const long long step = (long long)gridDim.x * (WAVES == 1 ? 4 : 1);
+  float dg[CHUNKS][E];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int i = 0; i < E; ++i) dg[c][i] = 0.f;
+  for (long long row = WAVES == 1 ? (long long)blockIdx.x * 4 + wave : blockIdx.x; row < a.rows; row += step) {
+    const float inv = a.inv_rms[row];
+    float s[CHUNKS][E], h[CHUNKS][E], dot = 0.f;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const int col = (c * 64 * WAVES + lane) * E;
+      load8<T, VEC>((const T*)a.dy + row * a.dy_stride + col, a.cols - col, h[c]);
+      load8<T, VEC>((const T*)a.sum + row * a.sum_stride + col, a.cols - col, s[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const int col = (c * 64 * WAVES + lane) * E;
+      float g[E];
+      load8<float, VEC>(a.gain + col, a.cols - col, g);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        dg[c][i] += h[c][i] * (s[c][i] * inv);
+        h[c][i] *= g[i];
+        dot += h[c][i] * s[c][i];
+      }
+    }
+    const float k = inv * inv * (row_total<WAVES>(dot, scratch) / (float)a.cols);
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const int col = (c * 64 * WAVES + lane) * E;
+      float d[E];
+      if (a.dsum) {
+        load8<T, VEC>((const T*)a.dsum + row * a.dsum_stride + col, a.cols - col, d);
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) d[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < E; ++i) d[i] += inv * (h[c][i] - s[c][i] * k);
+      store8<T, VEC>((T*)a.dx + row * a.dx_stride + col, a.cols - col, d);
+    }
+  }
+  if (!a.partial) return;
+  float* out = a.partial + (long long)blockIdx.x * a.cols;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int col = (c * 64 * WAVES + lane) * E;
+    if constexpr (WAVES == 1) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < E; ++i) scratch[(wave * E + i) * 64 + lane] = dg[c][i];
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) dg[c][i] = scratch[i * 64 + lane] + scratch[(E + i) * 64 + lane] + scratch[(2 * E + i) * 64 + lane] + scratch[(3 * E + i) * 64 + lane];
+        store8<float, false>(out + col, a.cols - col, dg[c]);
+      }
+    } else {
+      store8<float, false>(out + col, a.cols - col, dg[c]);
+    }
+  }
+}
+
+// Rows of any length: the products are formed twice, and the gain's gradient by threads that own columns.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(1024) void norm_back_long_kernel(NormBackArgs a) {
+  __shared__ float scratch[16];
+  const long long row = blockIdx.x;
+  const T *dy = (const T*)a.dy + row * a.dy_stride, *sum = (const T*)a.sum + row * a.sum_stride;
+  const float inv = a.inv_rms[row];
+  float h[E], s[E], g[E], dot = 0.f;
+  for (int col = threadIdx.x * E; col < a.cols; col += 1024 * E) {
+    load8<T, VEC>(dy + col, a.cols - col, h);
+    load8<T, VEC>(sum + col, a.cols - col, s);
+    load8<float, VEC>(a.gain + col, a.cols - col, g);
+#pragma unroll
+    for (int i = 0; i < E; ++i) dot += h[i] * g[i] * s[i];
+  }
+  const float k = inv * inv * (row_total<16>(dot, scratch) / (float)a.cols);
+  for (int col = threadIdx.x * E; col < a.cols; col += 1024 * E) {
+    load8<T, VEC>(dy + col, a.cols - col, h);
+    load8<T, VEC>(sum + col, a.cols - col, s);
+    load8<float, VEC>(a.gain + col, a.cols - col, g);
+    float d[E];
+    if (a.dsum) {
+      load8<T, VEC>((const T*)a.dsum + row * a.dsum_stride + col, a.cols - col, d);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) d[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) d[i] += inv * (h[i] * g[i] - s[i] * k);
+    store8<T, VEC>((T*)a.dx + row * a.dx_stride + col, a.cols - col, d);
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void gain_long_kernel(NormBackArgs a) {
+  const int col = blockIdx.x * 256 + threadIdx.x;
+  if (col >= a.cols) return;
+  float d = 0.f;
+  for (long long row = blockIdx.y; row < a.rows; row += gridDim.y)
+    d += to_float(((const T*)a.dy)[row * a.dy_stride + col]) * (to_float(((const T*)a.sum)[row * a.sum_stride + col]) * a.inv_rms[row]);
+  a.partial[(long long)blockIdx.y * a.cols + col] = d;
+}
+
+// dgain[c] = the blocks' partial sums, added in 32 chains that are joined in order
+__global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, float* dgain, int blocks, int cols) {
+  __shared__ float part[32][33];
+  const int c = threadIdx.x & 31, k = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+  float d = 0.f;
+  if (col < cols)
+    for (int b = k; b < blocks; b += 32) d += partial[(long long)b * cols + col];
+  part[k][c] = d;
+  __syncthreads();
+  if (k == 0 && col < cols) {
+#pragma unroll
+    for (int j = 1; j < 32; ++j) d += part[j][c];
+    dgain[col] = d;
+  }
+}
+
+constexpr int REGISTER_COLS = 16384;                              // rows that norm_back_kernel holds
+
+// Blocks of the gradient: each leaves a row of partial sums.
+int back_blocks(long long rows, int cols) {
+  if (cols > REGISTER_COLS) return (int)(rows < 64 ? rows : 64);
+  const long long per = cols <= 2048 ? 4 : 1, blocks = (rows + per - 1) / per, most = cols <= 8192 ? 1024 : 256;
+  return (int)(blocks < most ? blocks : most);
+}
+
+template <typename T, bool VEC>
+void launch_back(const NormBackArgs& a, hipStream_t st) {
+  const unsigned blocks = (unsigned)back_blocks(a.rows, a.cols);
+#define GAN_BACK(W, C) hipLaunchKernelGGL((norm_back_kernel<T, W, C, VEC>), dim3(blocks), dim3(W == 1 ? 256 : 64 * W), 0, st, a)
+  if (a.cols <= 512) GAN_BACK(1, 1);
+  else if (a.cols <= 1024) GAN_BACK(1, 2);
+  else if (a.cols <= 2048) GAN_BACK(1, 4);
+  else if (a.cols <= 4096) GAN_BACK(4, 2);
+  else if (a.cols <= 8192) GAN_BACK(4, 4);
+  else if (a.cols <= REGISTER_COLS) GAN_BACK(16, 2);
+  else {
+    // (the gain's gradient first: dx may be the memory of dy)
+    if (a.partial) hipLaunchKernelGGL(gain_long_kernel<T>, dim3((a.cols + 255) / 256, blocks), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((norm_back_long_kernel<T, VEC>), dim3((unsigned)a.rows), dim3(1024), 0, st, a);
+  }
+#undef GAN_BACK
+}
+
+// ---- 8 bits ----
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void quantize8_kernel(const T* x, long long stride, long long rows, int cols, uint8_t* q, uint8_t* scale) {
+  const long long wide = padded8(cols), chunks = rows * (wide / E);
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (long long)gridDim.x * 256) {   // (sixteen lanes of a block stay together)
+    const long long row = i * E / wide;
+    const int col = (int)(i * E - row * wide);
+    float v[E];
+    load8<T, VEC>(x + row * stride + col, cols - col, v);
+    const int byte = scale_byte(v);
+    *reinterpret_cast<uint2*>(q + i * E) = to_e4m3_x8(v, byte);
+    if ((threadIdx.x & 15) == 0) scale[i * E / BLOCK8] = (uint8_t)byte;
+  }
+}
+
+constexpr long long MOST_ROWS = 1 << 30;
+constexpr int MOST_COLS = 1 << 28;
+
+bool precision_known(int32_t p) { return p == GAN_FP32 || p == GAN_BF16_FP32MASTER; }
+gan_status check_matrix(const void* p, long long stride, int cols, const char* why) {
+  return p && stride < cols ? operator_fail(GAN_E_ARG, why) : GAN_OK;
+}
+gan_status check_sizes(int32_t precision, long long rows, int cols) {
+  if (!precision_known(precision)) return operator_fail(GAN_E_ARG, "unknown precision");
+  if (rows < 0 || cols < 1) return operator_fail(GAN_E_ARG, "negative rows or no columns");
+  if (rows > MOST_ROWS || cols > MOST_COLS) return operator_fail(GAN_E_SHAPE, "more than 2^30 rows or 2^28 columns");
+  return GAN_OK;
+}
+
+}  // namespace
+}  // namespace gan
+
+using namespace gan;
+
+extern "C" gan_status gan_rms_norm(int32_t precision, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const float* gain,
+                                   float eps, int64_t rows, int32_t cols, void* sum, int64_t sum_stride, void* y, int64_t y_stride, uint8_t* y8,
+                                   uint8_t* y8_scale, float* inv_rms, void* hip_stream) {
+  if (const gan_status s = check_sizes(precision, rows, cols)) return s;
+  if (!x || !gain) return operator_fail(GAN_E_ARG, "x or gain is NULL");
+  if (!y8 != !y8_scale) return operator_fail(GAN_E_ARG, "y8 and y8_scale go together");
+  if (!aligned16(y8)) return operator_fail(GAN_E_ARG, "y8 is not 16-byte aligned");
+  if (!(eps >= 0.f)) return operator_fail(GAN_E_ARG, "eps is negative");
+  for (const gan_status s : {check_matrix(x, x_stride, cols, "x_stride is below cols"), check_matrix(residual, residual_stride, cols, "residual_stride is below cols"),
+                             check_matrix(sum, sum_stride, cols, "sum_stride is below cols"), check_matrix(y, y_stride, cols, "y_stride is below cols")})
+    if (s) return s;
+  if (rows == 0) return GAN_OK;
+  const int e = precision == GAN_FP32 ? 4 : 2;
+  const bool vec = cols % E == 0 && rows_aligned16(x, x_stride, e) && (!residual || rows_aligned16(residual, residual_stride, e)) && aligned16(gain) &&
+                   (!sum || rows_aligned16(sum, sum_stride, e)) && (!y || rows_aligned16(y, y_stride, e));
+  const NormArgs a = {x, residual, gain, sum, y, y8, y8_scale, inv_rms, x_stride, residual_stride, sum_stride, y_stride, rows, cols, eps};
+  const hipStream_t st = (hipStream_t)hip_stream;
+  if (precision == GAN_FP32) vec ? launch_norm<float, true>(a, st) : launch_norm<float, false>(a, st);
+  else vec ? launch_norm<bf16_t, true>(a, st) : launch_norm<bf16_t, false>(a, st);
+  return operator_launched();
+}
+
+extern "C" int64_t gan_rms_norm_backward_bytes(int64_t rows, int32_t cols) {
+  if (rows <= 0 || cols < 1 || rows > MOST_ROWS || cols > MOST_COLS) return 0;
+  return (int64_t)back_blocks(rows, cols) * cols * (int64_t)sizeof(float);
+}
+
+extern "C" gan_status gan_rms_norm_backward(int32_t precision, const void* dy, int64_t dy_stride, const void* sum, int64_t sum_stride, const float* gain,
+                                            const float* inv_rms, const void* dsum, int64_t dsum_stride, int64_t rows, int32_t cols, void* dx,
+                                            int64_t dx_stride, float* dgain, void* work, int64_t work_bytes, void* hip_stream) {
+  if (const gan_status s = check_sizes(precision, rows, cols)) return s;
+  if (!dy || !sum || !gain || !inv_rms || !dx) return operator_fail(GAN_E_ARG, "dy, sum, gain, inv_rms or dx is NULL");
+  for (const gan_status s : {check_matrix(dy, dy_stride, cols, "dy_stride is below cols"), check_matrix(sum, sum_stride, cols, "sum_stride is below cols"),
+                             check_matrix(dsum, dsum_stride, cols, "dsum_stride is below cols"), check_matrix(dx, dx_stride, cols, "dx_stride is below cols")})
+    if (s) return s;
+  if (dgain && (work_bytes < gan_rms_norm_backward_bytes(rows, cols) || (!work && rows > 0) || !aligned16(work)))
+    return operator_fail(GAN_E_ARG, "work is smaller than gan_rms_norm_backward_bytes, or not 16-byte aligned");
+  const hipStream_t st = (hipStream_t)hip_stream;
+  const int e = precision == GAN_FP32 ? 4 : 2;
+  if (rows > 0) {
+    const bool vec = cols % E == 0 && rows_aligned16(dy, dy_stride, e) && rows_aligned16(sum, sum_stride, e) && (!dsum || rows_aligned16(dsum, dsum_stride, e)) &&
+                     rows_aligned16(dx, dx_stride, e) && aligned16(gain);
+    const NormBackArgs a = {dy, sum, dsum, gain, inv_rms, dx, dgain ? (float*)work : nullptr, dy_stride, sum_stride, dsum_stride, dx_stride, rows, cols};
+    if (precision == GAN_FP32) vec ? launch_back<float, true>(a, st) : launch_back<float, false>(a, st);
+    else vec ? launch_back<bf16_t, true>(a, st) : launch_back<bf16_t, false>(a, st);
+  }
+  if (dgain)
+    hipLaunchKernelGGL(gain_sum_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, (const float*)work, dgain, rows > 0 ? back_blocks(rows, cols) : 0, cols);
+  return operator_launched();
+}
+
+extern "C" gan_status gan_quantize8(int32_t precision, const void* x, int64_t x_stride, int64_t rows, int32_t cols, uint8_t* q, uint8_t* scale, void* hip_stream) {
+  if (const gan_status s = check_sizes(precision, rows, cols)) return s;
+  if (!x || !q || !scale) return operator_fail(GAN_E_ARG, "x, q or scale is NULL");
+  if (!aligned16(q)) return operator_fail(GAN_E_ARG, "q is not 16-byte aligned");
+  if (const gan_status s = check_matrix(x, x_stride, cols, "x_stride is below cols")) return s;
+  if (rows == 0) return GAN_OK;
+  const int e = precision == GAN_FP32 ? 4 : 2;
+  const bool vec = cols % E == 0 && rows_aligned16(x, x_stride, e);
+  const long long want = (rows * (padded8(cols) / E) + 255) / 256;
+  const dim3 grid((unsigned)(want < 8192 ? want : 8192));
+  const hipStream_t st = (hipStream_t)hip_stream;
+#define GAN_Q8(T, V) hipLaunchKernelGGL((quantize8_kernel<T, V>), grid, dim3(256), 0, st, (const T*)x, x_stride, rows, cols, q, scale)
+  if (precision == GAN_FP32) { if (vec) GAN_Q8(float, true); else GAN_Q8(float, false); }
+  else { if (vec) GAN_Q8(bf16_t, true); else GAN_Q8(bf16_t, false); }
+#undef GAN_Q8
+  return operator_launched();
+}

@@ -1,0 +1,201 @@
+"""The root-mean-square norm, its gradient and the 8-bit format (GPU) against 64-bit sums: lengths that end in every form of the kernels, odd
+ones, strides, memory that is not 16-byte aligned, values that are not finite.
+
+Bounds.  A lane adds at most 40 squares in a chain, and log2(64 * 16) more sums follow; with the divide, the root and the products an element of
+y is off by at most half of 64 roundings (the root halves the sum's error) and a few more: 40 roundings of 2^-24, and one of the storage type."""
+import numpy as np
+import pytest
+
+from paper_2102_10485_amd import binding as B
+from tests import gpu_util as U
+from tests import operators_ref as R
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+SHAPES = [(1, 1), (3, 5), (2, 127), (5, 128), (7, 129), (4, 512), (3, 520), (9, 1000), (5, 2048), (3, 2056), (2, 4104), (2, 8192), (3, 8200),
+          (1, 16384), (2, 16392), (2, 32776), (1, 40001)]
+
+
+def matrix(a, bf16, stride, offset=0):
+    """A device buffer whose row i starts at offset + i * stride; what lies between the rows is NaN."""
+    torch = U.torch_mod()
+    rows, cols = a.shape
+    t = torch.full((offset + rows * stride + 8,), float("nan"), dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda")
+    view = t[offset:offset + rows * stride].view(rows, stride)[:, :cols]
+    view.copy_(torch.from_numpy(np.ascontiguousarray(a, np.float32)))
+    return t, view, view.data_ptr()
+
+
+def host(view):
+    return view.float().cpu().numpy()
+
+
+def forward(x, residual, gain, bf16, pad=0, offset=0, eight=False):
+    torch = U.torch_mod()
+    rows, cols = x.shape
+    st = cols + pad
+    kind = torch.bfloat16 if bf16 else torch.float32
+    _, _, px = mx = matrix(x, bf16, st, offset)
+    mr = matrix(residual, bf16, st, offset) if residual is not None else None
+    ms, my = (matrix(np.zeros_like(x), bf16, st, offset) for _ in range(2))
+    inv = torch.zeros(rows, device="cuda")
+    g = torch.from_numpy(gain).cuda()
+    wide = R.padded(cols)
+    q, sc = (torch.full(s, 77, dtype=torch.uint8, device="cuda") for s in ((rows, wide), (rows, wide // 128)))
+    B.rms_norm(B.BF16 if bf16 else B.FP32, px, st, mr[2] if mr else 0, st, g.data_ptr(), EPS, rows, cols, ms[2], st, my[2], st,
+               q.data_ptr() if eight else 0, sc.data_ptr() if eight else 0, inv.data_ptr())
+    torch.cuda.synchronize()
+    for whole, view, _ in (ms, my):                              # nothing is written between the rows or behind them
+        rest = whole.clone()
+        rest[offset:offset + rows * st].view(rows, st)[:, :cols] = float("nan")
+        assert bool(rest.isnan().all())
+    assert kind == my[1].dtype
+    return host(ms[1]), host(my[1]), inv.cpu().numpy(), q.cpu().numpy(), sc.cpu().numpy()
+
+
+def inputs(rows, cols, bf16, seed):
+    rng = np.random.default_rng([rows, cols, seed])
+    x, r = (U.round_to(rng.normal(size=(rows, cols)) * np.exp(rng.normal(size=cols)), bf16) for _ in range(2))
+    return x, r, rng.normal(1, 0.2, cols).astype(np.float32)
+
+
+def bound(bf16):
+    return 40 * R.U32 + (R.UBF if bf16 else 0)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_forward(rows, cols, bf16):
+    for pad, offset, with_residual in ((0, 0, True), (8, 8, False), (3, 1, True)):
+        x, r, gain = inputs(rows, cols, bf16, pad)
+        r = r if with_residual else None
+        s, y, inv, q, sc = forward(x, r, gain, bf16, pad, offset, eight=True)
+        es, einv, ey = R.norm(x, r, gain, EPS, lambda v: U.round_to(v, bf16))
+        assert np.array_equal(s, es.astype(np.float32))
+        assert np.all(np.abs(inv - einv) <= 40 * R.U32 * einv)
+        assert np.all(np.abs(y - ey) <= bound(bf16) * np.abs(ey))
+        # 8 bits: the least scale that holds the block (up to y's own error), codes to the nearest, zeros behind the last column
+        wide = np.zeros((rows, R.padded(cols)))
+        wide[:, :cols] = ey
+        top, full = np.abs(wide).reshape(rows, -1, 128).max(-1), 448 * 2.0 ** (sc.astype(np.float64) - 127)
+        assert np.all(top <= full * (1 + 1e-5)) and np.all((top * (1 + 1e-5) > full / 2) | (sc == 1))
+        ulp = np.maximum(np.exp2(np.floor(np.log2(np.maximum(np.abs(wide), 1e-300)))), np.repeat(full / 448, 128, -1) * 2.0 ** -6) / 8
+        assert np.all(np.abs(R.decode(q, sc) - wide) <= 0.5 * ulp + 40 * R.U32 * np.abs(wide))
+        assert not q[:, cols:].any()
+
+
+def test_zero_rows_and_rows_of_zeros():
+    torch = U.torch_mod()
+    x = np.zeros((3, 300), np.float32)
+    s, y, inv, q, sc = forward(x, None, np.ones(300, np.float32), True, eight=True)
+    assert not y.any() and not q.any() and np.all(sc == 1) and np.allclose(inv, EPS ** -0.5, rtol=1e-6)
+    t = torch.zeros(1, device="cuda")
+    B.rms_norm(B.FP32, t.data_ptr(), 64, 0, 0, t.data_ptr(), EPS, 0, 64, 0, 0, t.data_ptr(), 64, 0, 0, 0)
+    dg = torch.ones(64, device="cuda")
+    B.rms_norm_backward(B.FP32, t.data_ptr(), 64, t.data_ptr(), 64, t.data_ptr(), t.data_ptr(), 0, 0, 0, 64, t.data_ptr(), 64, dg.data_ptr(), 0, 0)
+    assert not dg.cpu().numpy().any()
+
+
+@pytest.mark.parametrize("cols", [96, 1024, 4096, 40000])
+def test_values_that_are_not_finite_stay_in_their_rows(cols):
+    x, r, gain = inputs(4, cols, True, 9)
+    clean = forward(x, r, gain, True, eight=True)
+    x[1, cols // 2], x[2, 0] = np.inf, np.nan
+    s, y, inv, q, sc = forward(x, r, gain, True, eight=True)
+    for a, b in zip((s, y, inv, q, sc), clean):
+        assert np.array_equal(a[[0, 3]], b[[0, 3]])
+    # an infinity: the norm is infinite, finite values become zero, the infinity NaN; a NaN: the whole row
+    assert inv[1] == 0 and np.isnan(y[1, cols // 2]) and not np.delete(y[1], cols // 2).any()
+    assert q[1, cols // 2] & 0x7F == 0x7F and not (np.delete(q[1], cols // 2) & 0x7F).any()
+    assert np.isnan(y[2]).all() and np.all(q[2, :cols] & 0x7F == 0x7F)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_quantize8_is_the_format(bf16):
+    torch = U.torch_mod()
+    rng = np.random.default_rng(3)
+    for rows, cols, pad in ((1, 1, 0), (5, 128, 0), (4, 1000, 0), (3, 129, 2), (70, 640, 0)):
+        x = rng.normal(size=(rows, cols)) * np.exp(3 * rng.normal(size=(rows, cols)))
+        x[rng.random(x.shape) < 0.1] = 0
+        x = U.round_to(x, bf16)
+        x[0, 0] = 448 if cols == 128 else x[0, 0]
+        if rows > 3:
+            x[1, cols // 2], x[2, 1], x[3, 0] = np.inf, -np.inf, np.nan
+        whole, view, p = matrix(x, bf16, cols + pad)
+        wide = R.padded(cols)
+        q, sc = (torch.full(s, 77, dtype=torch.uint8, device="cuda") for s in ((rows, wide), (rows, wide // 128)))
+        B.quantize8(B.BF16 if bf16 else B.FP32, p, cols + pad, rows, cols, q.data_ptr(), sc.data_ptr())
+        full = np.zeros((rows, wide), np.float32)
+        full[:, :cols] = x
+        es = R.scale_bytes(full)
+        assert np.array_equal(sc.cpu().numpy(), es)
+        got, want = q.cpu().numpy(), R.nearest_codes(full, es)
+        assert np.array_equal(got & 0x7F, want & 0x7F)
+        assert np.array_equal(got[np.isfinite(full)], want[np.isfinite(full)])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("rows,cols", SHAPES + [(70, 40), (1030, 264), (300, 2500), (70, 17000)])
+def test_backward(rows, cols, bf16):
+    torch = U.torch_mod()
+    for pad, offset, with_dsum in ((0, 0, True), (8, 8, False), (5, 1, True)):
+        rng = np.random.default_rng([rows, cols, pad, 1])
+        s, _, gain = inputs(rows, cols, bf16, 5)
+        dy, ds = (U.round_to(rng.normal(size=(rows, cols)), bf16) for _ in range(2))
+        st = cols + pad
+        ms, mdy, mds, mdx = (matrix(a, bf16, st, offset) for a in (s, dy, ds, np.zeros_like(s)))
+        inv = torch.from_numpy((1 / np.sqrt((s.astype(np.float64) ** 2).mean(1) + EPS)).astype(np.float32)).cuda()
+        g, dg, n = torch.from_numpy(gain).cuda(), torch.zeros(cols, device="cuda"), B.rms_norm_backward_bytes(rows, cols)
+        work = torch.full((n // 4,), float("nan"), device="cuda")
+        B.rms_norm_backward(B.BF16 if bf16 else B.FP32, mdy[2], st, ms[2], st, g.data_ptr(), inv.data_ptr(), mds[2] if with_dsum else 0, st, rows, cols,
+                            mdx[2], st, dg.data_ptr(), work.data_ptr(), n)
+        edx, edg, size, gsize = R.norm_backward(dy, s, gain, EPS, ds if with_dsum else None)
+        dx = host(mdx[1])
+        # (inv as given carries one rounding, its square and the mean's chain the rest)
+        assert np.all(np.abs(dx - edx) <= 64 * R.U32 * size + (R.UBF * np.abs(edx) if bf16 else 0))
+        # a lane adds at most rows / blocks terms, then 32 chains of at most 32 partial sums are joined
+        assert np.all(np.abs(dg.cpu().numpy() - edg) <= (min(rows, 8) + 4 + 64 + 4) * R.U32 * gsize)
+
+
+def test_gradient_against_differences():
+    """Central differences of the forward kernel's own fp32 output along random directions: h = 2^-7 leaves h^2/6 of the third derivative
+    (below 1e-4 of the gradient's size) and 2^-24 / h = 8e-6 of rounding."""
+    torch = U.torch_mod()
+    rng = np.random.default_rng(0)
+    rows, cols, h = 6, 200, 2.0 ** -7
+    x, d, w = (rng.normal(size=(rows, cols)).astype(np.float32) for _ in range(3))
+    gain, dgain_dir = rng.normal(1, 0.2, cols).astype(np.float32), rng.normal(size=cols).astype(np.float32)
+
+    def value(x, gain):
+        return float((forward(x.astype(np.float32), None, gain.astype(np.float32), False)[1].astype(np.float64) * w).sum())
+
+    tx, tg, tw = (torch.from_numpy(a).cuda() for a in (x, gain, w))
+    inv = torch.from_numpy(forward(x, None, gain, False)[2]).cuda()
+    dx, dg, n = torch.zeros_like(tx), torch.zeros_like(tg), B.rms_norm_backward_bytes(rows, cols)
+    work = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    B.rms_norm_backward(B.FP32, tw.data_ptr(), cols, tx.data_ptr(), cols, tg.data_ptr(), inv.data_ptr(), 0, 0, rows, cols, dx.data_ptr(), cols, dg.data_ptr(),
+                        work.data_ptr(), n)
+    dx, dg = dx.cpu().numpy().astype(np.float64), dg.cpu().numpy().astype(np.float64)
+    along_x = (value(x + h * d, gain) - value(x - h * d, gain)) / (2 * h)
+    along_g = (value(x, gain + h * dgain_dir) - value(x, gain - h * dgain_dir)) / (2 * h)
+    assert abs(along_x - (dx * d).sum()) <= 1e-3 * np.linalg.norm(dx) * np.linalg.norm(d)
+    assert abs(along_g - (dg * dgain_dir).sum()) <= 1e-3 * np.linalg.norm(dg) * np.linalg.norm(dgain_dir)
+
+
+@pytest.mark.parametrize("cols", [512, 4096, 40000])
+def test_in_place(cols):
+    """sum over x, y over the residual's... and dx over dy: the same bits as with memory of their own."""
+    torch = U.torch_mod()
+    x, r, gain = inputs(5, cols, True, 2)
+    s, y, inv, _, _ = forward(x, r, gain, True)
+    tx, tr = (torch.from_numpy(a).cuda().bfloat16() for a in (x, r))
+    tg, ty, tinv = torch.from_numpy(gain).cuda(), torch.empty_like(tx), torch.empty(5, device="cuda")
+    B.rms_norm(B.BF16, tx.data_ptr(), cols, tr.data_ptr(), cols, tg.data_ptr(), EPS, 5, cols, tx.data_ptr(), cols, ty.data_ptr(), cols, 0, 0, tinv.data_ptr())
+    assert np.array_equal(host(tx), s) and np.array_equal(host(ty), y)
+    n = B.rms_norm_backward_bytes(5, cols)
+    work, dx, dg, dg2 = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty_like(tx), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    B.rms_norm_backward(B.BF16, ty.data_ptr(), cols, tx.data_ptr(), cols, tg.data_ptr(), tinv.data_ptr(), tr.data_ptr(), cols, 5, cols, dx.data_ptr(), cols,
+                        dg.data_ptr(), work.data_ptr(), n)
+    B.rms_norm_backward(B.BF16, ty.data_ptr(), cols, tx.data_ptr(), cols, tg.data_ptr(), tinv.data_ptr(), tr.data_ptr(), cols, 5, cols, ty.data_ptr(), cols,
+                        dg2.data_ptr(), work.data_ptr(), n)
+    assert torch.equal(dx, ty) and torch.equal(dg, dg2)
