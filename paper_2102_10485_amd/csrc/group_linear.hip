@@ -224,50 +224,26 @@ __global__ __launch_bounds__(256, 2) void linear_any_kernel(LinearArgs q) {
 
 // ---- rows of multiples of 16 bytes: bf16, and 8 bits ----
 //
-// Tiles of BM x BN, 128 bytes of the sum's index a step (64 bf16 values or 128 of 8 bits), copied straight into LDS while the last step's are multiplied.
-// k-major operands: LDS rows of 128 bytes; the others: 64 rows (sum indices) of BM or BN values, read with transposing reads.
-struct BF16 { typedef bf16_t T; static constexpr bool EIGHT = false; static constexpr int STEP = 64; };
-struct F8 { typedef uint8_t T; static constexpr bool EIGHT = true; static constexpr int STEP = 128; };
+// Tiles of BM x BN, 64 of the sum's index a step, in LDS as bf16: k-major operands in rows of 128 bytes, the others as 64 rows (sum indices) of BM or BN
+// values that are read with transposing reads.  bf16 operands are copied straight from memory while the step before the last is multiplied; 8-bit ones go through
+// registers, where a code times its block's power of two becomes the bf16 number that it is: every product is exact and every sum fp32.
+// (The 8-bit MFMAs would take half the matrix-pipe time, but they add eight neighbouring products with what lies 2^-13 below the largest of them
+// cut off (2^16 + 2^2 is 2^16): 1.5e-5 of the result's norm on normal values, 5e-5 on codes of all sizes.)
+constexpr int STEP = 64;
 
 // One operand's tile: R rows (or columns) of it, NW waves copying.
-template <typename M, bool KMAJOR, int R, int NW>
-struct Copied {
-  typedef typename M::T T;
+template <bool KMAJOR, int R, int NW>
+struct Tile {
   static constexpr int BYTES = R * 128;
   static constexpr int PIECES = BYTES / 1024 / NW;                // of 1 KiB, for each wave
   static constexpr int PER_ROW = R / 8;                           // granules of a row that is no k-major one
   static_assert(BYTES % (1024 * NW) == 0, "whole pieces");
-  unsigned off[PIECES];                                           // byte offset of the lane's granule in the step's memory
-  int k_at[PIECES];                                               // the sum index of it (its first)
 
   // Banks: sixteen lanes read sixteen k-major rows of 128 bytes at a time, or 32 lanes eight sum indices with 32 bytes each.
   __device__ static __forceinline__ int swap_of(int r) {
     if constexpr (KMAJOR) return (r >> 1) & 7;
     else if constexpr (PER_ROW >= 16) return ((r & 3) | ((r >> 3) & 1) << 2) << 1;
     else return (((r >> 1) & 1) | ((r >> 3) & 1) << 1) << 1;
-  }
-  // rows (k-major) or columns row0 .. of them `rows` exist; stride in elements
-  __device__ __forceinline__ void prepare(int wave, long long stride, int rows) {
-    const int l = threadIdx.x & 63;
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-      const int piece = wave * PIECES + p;
-      if constexpr (KMAJOR) {
-        const int r = piece * 8 + (l >> 3), g = (l & 7) ^ swap_of(r);
-        off[p] = r < rows ? (unsigned)(r * stride * (int)sizeof(T)) + g * 16 : NO_ROW;
-        k_at[p] = g * (16 / (int)sizeof(T));
-      } else {
-        const int r = piece * (64 / PER_ROW) + l / PER_ROW, g = (l % PER_ROW) ^ swap_of(r);
-        off[p] = g * 8 < rows ? (unsigned)(r * stride * (int)sizeof(T)) + g * 16 : NO_ROW;
-        k_at[p] = r;
-      }
-    }
-  }
-  // a step whose memory starts at `base` (of which `bytes` exist), `left` sum indices before the end
-  __device__ __forceinline__ void copy(int wave, const unsigned char* base, long long bytes, int left, unsigned lds) const {
-    const int4v rsrc = make_rsrc(base, (unsigned long long)bytes);
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) load16_to_lds(rsrc, k_at[p] < left ? off[p] : NO_ROW, 0, lds + (wave * PIECES + p) * 1024);
   }
   // MFMA operand of rows row .. row + 15 (a multiple of 16): half h of the step
   __device__ static __forceinline__ u32x4 read(const unsigned char* lds, int row, int h) {
@@ -287,98 +263,112 @@ struct Copied {
 
 __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(unsigned long long)(__attribute__((address_space(3))) const void*)p; }
 
-// 8-bit products on the bf16 MFMA: a code times its block's power of two is a bf16 number, and so every product is exact and every sum fp32.
-// The 8-bit MFMAs would take half the matrix-pipe time, but they add eight neighbouring products with what lies 2^-13 below the largest of them
-// cut off (2^16 + 2^2 is 2^16): 1.5e-5 of the result's norm on normal values, 5e-5 on codes of all sizes.
-struct Pair8 { u32x4 lo, hi; };
-__device__ __forceinline__ Pair8 to_bf16(const u32x4& q, int byte) {
-  const float f = power_of_two(byte);
-  Pair8 r;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    r.lo[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[i], f, false));
-    r.lo[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[i], f, true));
-    r.hi[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 + i], f, false));
-    r.hi[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 + i], f, true));
-  }
-  return r;
-}
+// A bf16 operand: copies.
+template <bool KMAJOR, int R, int NW>
+struct Copied : Tile<KMAJOR, R, NW> {
+  typedef Tile<KMAJOR, R, NW> S;
+  typedef bf16_t T;
+  static constexpr bool COPIES = true;
+  unsigned off[S::PIECES];                                        // byte offset of the lane's granule in the step's memory
+  int4v memory;
+  const unsigned char* at;                                        // the next step's memory, what there is of it, and the way to the one behind
+  long long bytes, move;
 
-// the scale bytes of one step for a wave's operand rows: lane l has row l % 16 of each sixteen
-template <int N>
-struct Scales {
-  int v[N];
-  __device__ __forceinline__ void load(const uint8_t* scale, long long blocks, int row0, int rows, int step) {
-    const int l = threadIdx.x & 15;
+  // rows (k-major; else columns) row0 .. of expert `base`, of which `rows` exist, sum indices k0 .. k_end - 1; stride in elements
+  __device__ __forceinline__ void prepare(const T* base, const uint8_t*, long long stride, int row0, int rows, int k0, int k_end, int wave) {
+    const int l = threadIdx.x & 63;
+    at = (const unsigned char*)(base + (KMAJOR ? row0 * stride + k0 : k0 * stride + row0));
+    bytes = (KMAJOR ? (rows - 1) * stride + k_end - k0 : (k_end - k0 - 1) * stride + rows) * 2;
+    move = KMAJOR ? STEP * 2 : STEP * 2 * stride;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int r = row0 + i * 16 + l;
-      v[i] = r < rows ? scale[r * blocks + step] : 0;
+    for (int p = 0; p < S::PIECES; ++p) {
+      const int piece = wave * S::PIECES + p;
+      const int r = KMAJOR ? piece * 8 + (l >> 3) : piece * (64 / S::PER_ROW) + l / S::PER_ROW;
+      const int g = (KMAJOR ? l & 7 : l % S::PER_ROW) ^ S::swap_of(r);
+      off[p] = (KMAJOR ? r : g * 8) < rows ? (unsigned)(r * stride * 2) + g * 16 : NO_ROW;
     }
+  }
+  __device__ __forceinline__ void next_step() {
+    memory = make_rsrc(at, (unsigned long long)max(bytes, 0ll));
+    at += move;
+    bytes -= move;
+  }
+  // piece p of the step, whose first sum index is `left` before the end
+  __device__ __forceinline__ void piece(int p, int wave, int left, unsigned char*, unsigned lds) {
+    const int l = threadIdx.x & 63, piece = wave * S::PIECES + p;
+    const int k = KMAJOR ? ((l & 7) ^ S::swap_of(piece * 8 + (l >> 3))) * 8 : piece * (64 / S::PER_ROW) + l / S::PER_ROW;
+    load16_to_lds(memory, k < left ? off[p] : NO_ROW, 0, lds + piece * 1024);
   }
 };
 
-template <typename M, int KIND, int BM, int BN, int WM, int WN, typename C>
-__global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearArgs q) {
-  typedef typename M::T T;
-  constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-  typedef Copied<M, KIND != WGRAD, BM, NW> CA;
-  typedef Copied<M, KIND == FORWARD, BN, NW> CB;
-  extern __shared__ __align__(1024) unsigned char lds[];          // two steps of both operands
-  constexpr int STAGE = CA::BYTES + CB::BYTES;
+// An 8-bit operand, k-major: chunks of sixteen codes of a row, thread t's being chunk t % 4 of rows t / 4, t / 4 + THREADS / 4, ...  A chunk is written to LDS two
+// steps after it was asked for.
+template <int R, int NW>
+struct Converted : Tile<true, R, NW> {
+  typedef Tile<true, R, NW> S;
+  typedef uint8_t T;
+  static constexpr bool COPIES = false;
+  static constexpr int CHUNKS = R * 4 / (64 * NW);
+  static constexpr int PIECES = CHUNKS;
+  static_assert(R * 4 % (64 * NW) == 0, "whole chunks");
+  uint4 q[CHUNKS];
+  int byte[CHUNKS];
+  __amdgpu_buffer_rsrc_t codes, scales;
+  unsigned off[CHUNKS], scale_off[CHUNKS];
+  int k;                                                          // of the step that is asked for next
 
-  const int n_tiles = (q.n + BN - 1) / BN, n0 = (int)(blockIdx.x % n_tiles) * BN;
-  int group, m0, m_end, k_begin = 0, k_end = q.k;
-  if (KIND == WGRAD) {
-    const int m_tiles = (q.m + BM - 1) / BM, t = blockIdx.x / n_tiles;
-    group = t / m_tiles;
-    m0 = t % m_tiles * BM;
-    m_end = q.m;
-    group_rows(q.offs, q.groups, q.rows, group, k_begin, k_end);
-  } else {
-    if (!find_tile(q.offs, q.groups, q.rows, BM, blockIdx.x / n_tiles, group, m0, m_end)) return;
-    if (group == q.groups) k_end = 0;                             // rows of no expert: zeros
+  __device__ __forceinline__ void prepare(const T* base, const uint8_t* scale, long long stride, int row0, int rows, int k0, int k_end, int) {
+    const long long blocks = stride / BLOCK8;
+    codes = buffer_of(base + row0 * stride, (unsigned long long)(rows * stride));
+    scales = buffer_of(scale + row0 * blocks, (unsigned long long)(rows * blocks));
+#pragma unroll
+    for (int p = 0; p < CHUNKS; ++p) {
+      const int r = threadIdx.x / 4 + p * (16 * NW);
+      off[p] = r < rows ? (unsigned)(r * stride) + threadIdx.x % 4 * 16 : NO_ROW;
+      scale_off[p] = r < rows ? (unsigned)(r * blocks) : NO_ROW;
+    }
+    k = 0;
+#pragma unroll
+    for (int p = 0; p < CHUNKS; ++p) ask(p);
+    k = STEP;
   }
+  __device__ __forceinline__ void ask(int p) {
+    // (behind the last step: the start of the rows again, which is not used)
+    q[p] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)off[p], k, 0));
+    byte[p] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_off[p], k / BLOCK8, 0);
+  }
+  __device__ __forceinline__ void next_step() {}
+  __device__ __forceinline__ void piece(int p, int, int left, unsigned char* lds, unsigned) {
+    const int r = threadIdx.x / 4 + p * (16 * NW), c = threadIdx.x % 4 * 2;
+    const float f = power_of_two(byte[p]);
+    const unsigned w[4] = {q[p].x, q[p].y, q[p].z, q[p].w};
+    u32x4 lo, hi;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      lo[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], f, false));
+      lo[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], f, true));
+      hi[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 + i], f, false));
+      hi[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 + i], f, true));
+    }
+    *reinterpret_cast<u32x4*>(lds + r * 128 + ((c ^ S::swap_of(r)) * 16)) = lo;
+    *reinterpret_cast<u32x4*>(lds + r * 128 + (((c + 1) ^ S::swap_of(r)) * 16)) = hi;
+    ask(p);
+    if (p == CHUNKS - 1) k = left > 2 * STEP ? k + STEP : 0;
+  }
+};
+
+// One tile of expert `group` (q.groups: of none): rows m0 .. m_end - 1, columns n0 .., sum indices k_begin .. k_end - 1.
+template <bool EIGHT, int KIND, int BM, int BN, int WM, int WN, typename C>
+__device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char* lds, int group, int m0, int m_end, int n0, int k_begin, int k_end) {
+  constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+  typedef typename std::conditional<EIGHT, Converted<BM, NW>, Copied<KIND != WGRAD, BM, NW>>::type CA;
+  typedef typename std::conditional<EIGHT, Converted<BN, NW>, Copied<KIND == FORWARD, BN, NW>>::type CB;
+  typedef typename CA::T T;
+  constexpr int STAGE = CA::BYTES + CB::BYTES;                    // two of them
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-
-  // memory of the first step, and how it moves on
-  const int expert = KIND == WGRAD || group == q.groups ? 0 : group;
-  const T* a0 = (const T*)q.a + (KIND == WGRAD ? (long long)k_begin * q.a_stride + m0 : (long long)m0 * q.a_stride);
-  const T* b0 = (const T*)q.b + (KIND == WGRAD ? (long long)k_begin * q.b_stride + n0
-                                               : (long long)expert * q.b_group + (KIND == FORWARD ? (long long)n0 * q.b_stride : n0));
-  const int a_rows = min(BM, m_end - m0), b_rows = min(BN, q.n - n0);
-  // what exists behind them: the rest of the rows (a k-major one's last ends with the sum; a row that is none ends with its columns)
-  long long a_bytes = KIND == WGRAD ? ((long long)(k_end - k_begin - 1) * q.a_stride + a_rows) * (int)sizeof(T)
-                                    : ((long long)(a_rows - 1) * q.a_stride + q.k) * (int)sizeof(T);
-  long long b_bytes = KIND == FORWARD ? ((long long)(b_rows - 1) * q.b_stride + q.k) * (int)sizeof(T)
-                                      : ((long long)(k_end - k_begin - 1) * q.b_stride + b_rows) * (int)sizeof(T);
-  const long long a_move = (KIND == WGRAD ? M::STEP * q.a_stride : M::STEP) * (int)sizeof(T);
-  const long long b_move = (KIND == FORWARD ? M::STEP : M::STEP * q.b_stride) * (int)sizeof(T);
-  const unsigned char *pa = (const unsigned char*)a0, *pb = (const unsigned char*)b0;
-
-  CA ca;
-  CB cb;
-  ca.prepare(wave, q.a_stride, a_rows);
-  cb.prepare(wave, q.b_stride, b_rows);
-  const unsigned lds0 = lds_address(lds);
+  const int steps = (k_end - k_begin + STEP - 1) / STEP;
   int left = k_end - k_begin;
-  auto copy_step = [&](int stage) {
-    ca.copy(wave, pa, a_bytes, left, lds0 + stage * STAGE);
-    cb.copy(wave, pb, b_bytes, left, lds0 + stage * STAGE + CA::BYTES);
-    pa += a_move; a_bytes -= a_move;
-    pb += b_move; b_bytes -= b_move;
-    left -= M::STEP;
-  };
-  Scales<TM> sa, sa_next;
-  Scales<TN> sb, sb_next;
-  const long long blocks8 = q.k / 128;
-  auto load_scales = [&](int step) {
-    if constexpr (M::EIGHT) {
-      sa_next.load(q.a_scale, blocks8, m0 + wm, m_end, step);
-      sb_next.load(q.b_scale + (long long)expert * q.n * blocks8, blocks8, n0 + wn, q.n, step);
-    }
-  };
 
   floatx4 acc[TM][TN];
 #pragma unroll
@@ -386,65 +376,155 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearArgs q) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  const int steps = (k_end - k_begin + M::STEP - 1) / M::STEP;
   if (steps > 0) {
-    load_scales(0);
-    copy_step(0);
-  }
-  for (int s = 0; s < steps; ++s) {
-    wait_vm<0>();
-    __syncthreads();                                              // the step is in LDS, and the other stage has been read
-    sa = sa_next;
-    sb = sb_next;
-    if (s + 1 < steps) {
-      load_scales(s + 1);
-      copy_step((s + 1) & 1);
+    const int expert = KIND == WGRAD ? 0 : group;
+    CA ca;
+    CB cb;
+    const long long blocks8 = (long long)q.n * (q.b_stride / BLOCK8);
+    ca.prepare((const T*)q.a, q.a_scale, q.a_stride, m0, min(BM, m_end - m0), k_begin, k_end, wave);
+    cb.prepare((const T*)q.b + expert * q.b_group, EIGHT ? q.b_scale + expert * blocks8 : nullptr, q.b_stride, n0, min(BN, q.n - n0), k_begin, k_end, wave);
+    const unsigned lds0 = lds_address(lds);
+    constexpr int PIECES = CA::PIECES + CB::PIECES;
+    auto copy_piece = [&](int p, int stage) {
+      if (p < CA::PIECES) ca.piece(p, wave, left, lds + stage * STAGE, lds0 + stage * STAGE);
+      else cb.piece(p - CA::PIECES, wave, left, lds + stage * STAGE + CA::BYTES, lds0 + stage * STAGE + CA::BYTES);
+    };
+
+    // Half a step is multiplied while the operands of the next half are read from LDS, so that the matrix pipe sees no wait: the second half's during the
+    // first, and during the second those of the next step, whose copies have then had a whole step to arrive.  The barrier between the halves
+    // says that they have, and that no wave reads this step's stage any more, which the copies of the step after the next overwrite.
+    struct Operands { u32x4 a[TM], b[TN]; };
+    Operands f0, f1;
+    auto read_piece = [&](Operands& f, int p, int stage, int h) {
+      const unsigned char* at = lds + stage * STAGE;
+      if (p < TN) f.b[p] = CB::read(at + CA::BYTES, wn + p * 16, h);
+      else f.a[p - TN] = CA::read(at, wm + (p - TN) * 16, h);
+    };
+    constexpr int SLOTS = TM > 2 ? TM - 1 : TM;                   // rows of products that reads and copies are issued between
+    // products of `f`; meanwhile the operands `next` of half h of `stage`, and (COPY) the copies of another step into the other stage
+    auto half_step = [&](const Operands& f, Operands& next, int stage, int h, auto copy) {
+      static_for<0, TM>([&](auto iv) {
+        constexpr int i = iv.value;
+        static_for<i * (TM + TN) / SLOTS, (i + 1) * (TM + TN) / SLOTS>([&](auto p) { if constexpr (p.value < TM + TN) read_piece(next, p.value, stage, h); });
+        if constexpr (copy.value)
+          static_for<i * PIECES / SLOTS, (i + 1) * PIECES / SLOTS>([&](auto p) { if constexpr (p.value < PIECES) copy_piece(p.value, stage ^ 1); });
+#pragma unroll
+        for (int j = 0; j < TN; ++j) mma(acc[i][j], f.b[j], f.a[i]);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+
+    // (Copies behind the last step ask for nothing and fill the stage with zeros; its operands are read and not multiplied.)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      ca.next_step();
+      cb.next_step();
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) copy_piece(p, s);
+      left -= STEP;
     }
-    const unsigned char *la = lds + (s & 1) * STAGE, *lb = la + CA::BYTES;
-    if constexpr (M::EIGHT) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        Pair8 fb[TN];
-#pragma unroll
-        for (int j = 0; j < TN; ++j) fb[j] = to_bf16(CB::read(lb, wn + j * 16, h), sb.v[j]);
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          const Pair8 fa = to_bf16(CA::read(la, wm + i * 16, h), sa.v[i]);
-#pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            mma(acc[i][j], fb[j].lo, fa.lo);
-            mma(acc[i][j], fb[j].hi, fa.hi);
-          }
-        }
-      }
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u32x4 fb[TN];
-#pragma unroll
-        for (int j = 0; j < TN; ++j) fb[j] = CB::read(lb, wn + j * 16, h);
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          const u32x4 fa = CA::read(la, wm + i * 16, h);
-#pragma unroll
-          for (int j = 0; j < TN; ++j) mma(acc[i][j], fb[j], fa);
-        }
-      }
+    if constexpr (CA::COPIES) wait_vm<0>();
+    __syncthreads();
+    static_for<0, TM + TN>([&](auto p) { read_piece(f0, p.value, 0, 0); });
+    for (int s = 0; s < steps; ++s) {
+      const int stage = s & 1;
+      half_step(f0, f1, stage, 1, std::false_type());
+      if constexpr (CA::COPIES) wait_vm<0>();
+      __syncthreads();
+      ca.next_step();
+      cb.next_step();
+      half_step(f1, f0, stage ^ 1, 0, std::true_type());
+      left -= STEP;
     }
+    if constexpr (CA::COPIES) wait_vm<0>();
+    __syncthreads();                                              // nothing is written to LDS any more, or read
   }
 
+  // Sixteen rows of a wave's columns at a time go through LDS, so that its lanes store whole rows, 16 bytes each: 64 lanes with four columns each of
+  // sixteen rows would write 32 or 64 bytes of a row at a time, at 2.5 TB/s.
   C* c = (C*)q.c + (KIND == WGRAD ? (long long)group * q.c_group : 0);
+  constexpr int WIDE = TN * 16 * (int)sizeof(C), LANES = WIDE / 16, EACH = 16 / (int)sizeof(C);
+  unsigned char* out = lds + wave * 16 * (WIDE + 16);
+  static_assert(NW * 16 * (WIDE + 16) <= 2 * STAGE && 64 % LANES == 0, "the outputs' LDS");
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int m = m0 + wm + i * 16 + (l & 15);
+    if (m0 + wm + i * 16 >= m_end) break;
+    if (q.vec & 4) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int n = n0 + wn + j * 16 + (l >> 4) * 4;
-      if (m >= m_end || n >= q.n) continue;
-      const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-      store_four<C>(c + (long long)m * q.c_stride + n, q.n - n, v, q.vec & 4);
+      for (int j = 0; j < TN; ++j) {
+        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        store_four<C>((C*)(out + (l & 15) * (WIDE + 16)) + j * 16 + (l >> 4) * 4, 4, v, true);
+      }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int r = l / LANES; r < 16; r += 64 / LANES) {
+        const int m = m0 + wm + i * 16 + r, n = n0 + wn + l % LANES * EACH;
+        const uint4 v = *reinterpret_cast<const uint4*>(out + r * (WIDE + 16) + l % LANES * 16);
+        if (m >= m_end || n >= q.n) continue;
+        C* at = c + (long long)m * q.c_stride + n;
+        if (n + EACH <= q.n) {
+          *reinterpret_cast<uint4*>(at) = v;
+        } else {
+          const C* e = reinterpret_cast<const C*>(out + r * (WIDE + 16) + l % LANES * 16);
+          for (int k = 0; k < q.n - n; ++k) at[k] = e[k];
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    } else {
+      const int m = m0 + wm + i * 16 + (l & 15);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int n = n0 + wn + j * 16 + (l >> 4) * 4;
+        if (m >= m_end || n >= q.n) continue;
+        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        store_four<C>(c + (long long)m * q.c_stride + n, q.n - n, v, false);
+      }
     }
   }
+}
+
+// Rows of tiles in bands of 8, columns by 4 within a band: 32 tiles in a row, which the CUs of one XCD work on together, then read 8 + 4
+// panels through its L2 in place of 64.
+__device__ __forceinline__ void banded(unsigned id, unsigned row_tiles, unsigned col_tiles, unsigned& r, unsigned& c) {
+  const unsigned band = id / (8 * col_tiles), first = band * 8, high = min(8u, row_tiles - first), in_band = id - first * col_tiles;
+  const unsigned four = in_band / (high * 4), in_four = in_band - four * (high * 4);
+  r = first + in_four % high;
+  c = four * 4 + in_four / high;
+}
+
+// Forward and dgrad.  Block b runs on XCD b % 8: each XCD takes one stretch of the whole tiles, then its share of the experts' shorter last ones, in
+// half the height where that is enough.
+template <bool EIGHT, int KIND, int BM, int BN, int WM, int WN, typename C>
+__global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearArgs q) {
+  extern __shared__ __align__(1024) unsigned char lds[];
+  unsigned whole, ends;
+  count_tiles(q.offs, q.groups, q.rows, BM, whole, ends);
+  const unsigned cols = (unsigned)(q.n + BN - 1) / BN, xcd = blockIdx.x & 7, i = blockIdx.x >> 3, share = (whole * cols + 7) / 8;
+  int group, m0, m_end;
+  if (i < share) {
+    const unsigned id = xcd * share + i;
+    if (id >= whole * cols) return;
+    unsigned r, c;
+    banded(id, whole, cols, r, c);
+    find_tile_of<false>(q.offs, q.groups, q.rows, BM, r, group, m0, m_end);
+    tile_product<EIGHT, KIND, BM, BN, WM, WN, C>(q, lds, group, m0, m_end, (int)c * BN, 0, group < q.groups ? q.k : 0);
+  } else {
+    const unsigned id = (i - share) * 8 + xcd;
+    if (id >= ends * cols) return;
+    find_tile_of<true>(q.offs, q.groups, q.rows, BM, id / cols, group, m0, m_end);
+    const int n0 = (int)(id % cols) * BN, k = group < q.groups ? q.k : 0;
+    if (m_end - m0 > BM / 2) tile_product<EIGHT, KIND, BM, BN, WM, WN, C>(q, lds, group, m0, m_end, n0, 0, k);
+    else tile_product<EIGHT, KIND, BM / 2, BN, WM, WN, C>(q, lds, group, m0, m_end, n0, 0, k);
+  }
+}
+
+template <int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void linear_wgrad_kernel(LinearArgs q) {
+  extern __shared__ __align__(1024) unsigned char lds[];
+  const int n_tiles = (q.n + BN - 1) / BN, m_tiles = (q.m + BM - 1) / BM, t = blockIdx.x / n_tiles;
+  int begin, end;
+  group_rows(q.offs, q.groups, q.rows, t / m_tiles, begin, end);
+  tile_product<false, WGRAD, BM, BN, WM, WN, float>(q, lds, t / m_tiles, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
 }
 
 // ---- launches ----
@@ -463,24 +543,30 @@ gan_status launch_any(int kind, const LinearArgs& q, hipStream_t st) {
   return operator_launched();
 }
 
-template <typename M, int KIND, int BM, int BN, int WM, int WN, typename C>
-gan_status launch_tiles(const LinearArgs& q, hipStream_t st) {
-  const long long n_tiles = (q.n + BN - 1) / BN;
-  const long long blocks = n_tiles * (KIND == WGRAD ? (long long)q.groups * ((q.m + BM - 1) / BM) : most_tiles(q.rows, q.groups, BM));
+template <typename F>
+gan_status launch(F* kernel, long long blocks, int threads, int lds, const LinearArgs& q, hipStream_t st) {
   if (blocks > MOST_BLOCKS) return operator_fail(GAN_E_SHAPE, "more than 2^31 - 1 tiles");
-  constexpr int LDS = 2 * (BM + BN) * 128;
-  const void* f = (const void*)linear_kernel<M, KIND, BM, BN, WM, WN, C>;
-  if (LDS > 65536 && hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) {
+  if (lds > 65536 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) {
     (void)hipGetLastError();
     return operator_fail(GAN_E_HIP, "the kernel's LDS could not be set");
   }
-  hipLaunchKernelGGL((linear_kernel<M, KIND, BM, BN, WM, WN, C>), dim3((unsigned)blocks), dim3(64 * WM * WN), LDS, st, q);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, st, q);
   return operator_launched();
 }
 
-template <typename M, int KIND, typename C>
+template <bool EIGHT, int KIND, int BM, int BN, int WM, int WN, typename C>
+gan_status launch_tiles(const LinearArgs& q, hipStream_t st) {
+  const long long cols = (q.n + BN - 1) / BN;
+  constexpr int LDS = 2 * (BM + BN) * 128;
+  if constexpr (KIND == WGRAD)
+    return launch(linear_wgrad_kernel<BM, BN, WM, WN>, q.groups * cols * ((q.m + BM - 1) / BM), 64 * WM * WN, LDS, q, st);
+  else    // (whole tiles and ends are each shared among the eight XCDs)
+    return launch(linear_kernel<EIGHT, KIND, BM, BN, WM, WN, C>, 8 * ((most_tiles(q.rows, q.groups, BM) * cols + 7) / 8 + 1), 64 * WM * WN, LDS, q, st);
+}
+
+template <bool EIGHT, int KIND, typename C>
 gan_status launch_aligned(const LinearArgs& q, hipStream_t st) {
-  return launch_tiles<M, KIND, 128, 128, 2, 2, C>(q, st);
+  return launch_tiles<EIGHT, KIND, 256, 256, 2, 4, C>(q, st);
 }
 
 gan_status check(int32_t precision, const void* x, const void* w, const int32_t* offs, int32_t groups, int64_t rows, int32_t n_in, int32_t n_out, const void* out) {
@@ -510,7 +596,7 @@ extern "C" gan_status gan_group_linear(int32_t precision, const void* x, int64_t
                         (va ? 1 : 0) | (vb ? 2 : 0) | (rows_aligned16(y, y_stride, e) ? 4 : 0)};
   const hipStream_t st = (hipStream_t)hip_stream;
   if (precision == GAN_FP32) return launch_any<float>(FORWARD, q, st);
-  return va && vb && short_rows(x_stride, e) && short_rows(n_in, e) ? launch_aligned<BF16, FORWARD, bf16_t>(q, st) : launch_any<bf16_t>(FORWARD, q, st);
+  return va && vb && short_rows(x_stride, e) && short_rows(n_in, e) ? launch_aligned<false, FORWARD, bf16_t>(q, st) : launch_any<bf16_t>(FORWARD, q, st);
 }
 
 extern "C" gan_status gan_group_linear_dgrad(int32_t precision, const void* dy, int64_t dy_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows,
@@ -524,7 +610,7 @@ extern "C" gan_status gan_group_linear_dgrad(int32_t precision, const void* dy, 
                         (va ? 1 : 0) | (vb ? 2 : 0) | (rows_aligned16(dx, dx_stride, e) ? 4 : 0)};
   const hipStream_t st = (hipStream_t)hip_stream;
   if (precision == GAN_FP32) return launch_any<float>(DGRAD, q, st);
-  return va && vb && short_rows(dy_stride, e) && short_rows(n_in, e) ? launch_aligned<BF16, DGRAD, bf16_t>(q, st) : launch_any<bf16_t>(DGRAD, q, st);
+  return va && vb && short_rows(dy_stride, e) && short_rows(n_in, e) ? launch_aligned<false, DGRAD, bf16_t>(q, st) : launch_any<bf16_t>(DGRAD, q, st);
 }
 
 extern "C" int64_t gan_group_linear_wgrad_bytes(int32_t groups, int64_t rows, int32_t n_in, int32_t n_out) {
@@ -544,7 +630,7 @@ extern "C" gan_status gan_group_linear_wgrad(int32_t precision, const void* x, i
                         (va ? 1 : 0) | (vb ? 2 : 0) | (rows_aligned16(dw, n_in, 4) ? 4 : 0)};
   const hipStream_t st = (hipStream_t)hip_stream;
   if (precision == GAN_FP32) return launch_any<float>(WGRAD, q, st);
-  return va && vb && short_rows(x_stride, e) && short_rows(dy_stride, e) ? launch_aligned<BF16, WGRAD, float>(q, st) : launch_any<bf16_t>(WGRAD, q, st);
+  return va && vb && short_rows(x_stride, e) && short_rows(dy_stride, e) ? launch_aligned<false, WGRAD, float>(q, st) : launch_any<bf16_t>(WGRAD, q, st);
 }
 
 extern "C" gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scale, const uint8_t* w8, const uint8_t* w_scale, const int32_t* offs, int32_t groups,
@@ -560,5 +646,5 @@ extern "C" gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scal
   const LinearArgs q = {x8, w8, x_scale, w_scale, y, offs, k, k, y_stride, k * n_out, 0, groups, (int)rows, 0, n_out, (int)k,
                         rows_aligned16(y, y_stride, e) ? 7 : 3};
   const hipStream_t st = (hipStream_t)hip_stream;
-  return y_precision == GAN_FP32 ? launch_aligned<F8, FORWARD, float>(q, st) : launch_aligned<F8, FORWARD, bf16_t>(q, st);
+  return y_precision == GAN_FP32 ? launch_aligned<true, FORWARD, float>(q, st) : launch_aligned<true, FORWARD, bf16_t>(q, st);
 }
