@@ -12,6 +12,8 @@
 #include "operators.h"
 #include "split_mfma.h"
 
+#include <algorithm>
+
 namespace gan {
 namespace {
 
@@ -28,31 +30,29 @@ struct LinearArgs {
   long long b_group, c_group;                  // between experts (c_group: wgrad)
   int groups, rows;
   int m, n, k;                                 // wgrad: m = outputs, n = inputs; else n, k (m: the expert's rows; wgrad: k)
-  int vec;                                     // any-alignment kernel: 16-byte loads of a (bit 0), of b (bit 1), 16-byte stores (bit 2)
+  int parts;                                   // wgrad: an expert's rows are shared by this many blocks, whose results follow one another at `part` elements
+  long long part;
 };
 
-// ---- any alignment, fp32 and bf16 ----
+// ---- fp32 ----
 //
-// 128 x 128 tiles, 32 of the sum's index at a time: loaded into registers while the last ones are multiplied, then written to LDS as bf16, in fp32
-// as three planes of parts (split_mfma.h).  What has the sum's index as its row is kept that way and read with transposing LDS reads.
+// 128 x 128 tiles, 32 of the sum's index at a time: loaded into registers while the last ones are multiplied, then written to LDS as three planes of bf16
+// parts (split_mfma.h).  What has the sum's index as its row is kept that way and read with transposing LDS reads.
 constexpr int RT = 128, RK = 32;
 
-template <typename T, bool KMAJOR>
+template <bool KMAJOR>
 struct Staged {
-  static constexpr int PLANES = sizeof(T) == 4 ? 3 : 1;
   static constexpr int PLANE = RT * RK * 2;
   float v[2][8];
 
   // thread t's two chunks of eight: k-major row t / 4 (+ 64), elements 8 (t % 4) ..; else sum index t / 16 (+ 16), columns 8 (t % 16) ..
-  __device__ __forceinline__ void load(const T* p, long long stride, int row0, int rows, int k0, int k_end, bool vec) {
+  __device__ __forceinline__ void load(const float* p, long long stride, int row0, int rows, int k0, int k_end) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int r = KMAJOR ? row0 + threadIdx.x / 4 + 64 * h : k0 + threadIdx.x / 16 + 16 * h;
       const int c = KMAJOR ? k0 + threadIdx.x % 4 * 8 : row0 + threadIdx.x % 16 * 8;
       const int left = r < (KMAJOR ? rows : k_end) ? (KMAJOR ? k_end : rows) - c : 0;
-      const T* at = p + (long long)r * stride + c;
-      if (vec) load8<T, true>(at, left, v[h]);
-      else load8<T, false>(at, left, v[h]);
+      load8<float, false>(p + (long long)r * stride + c, left, v[h]);
     }
   }
   __device__ __forceinline__ void store(unsigned char* lds) const {
@@ -61,20 +61,16 @@ struct Staged {
       const int r = KMAJOR ? threadIdx.x / 4 + 64 * h : threadIdx.x / 16 + 16 * h;
       const int g = KMAJOR ? threadIdx.x % 4 : threadIdx.x % 16;
       unsigned char* at = lds + offset(r, g);
-      if constexpr (PLANES == 3) {
-        u32x4 lo, hi;
+      u32x4 lo, hi;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          lo[i] = __float_as_uint(v[h][i]);
-          hi[i] = __float_as_uint(v[h][4 + i]);
-        }
-        const Split8 s = split8(lo, hi);
-        *reinterpret_cast<u32x4*>(at) = s.h;
-        *reinterpret_cast<u32x4*>(at + PLANE) = s.m;
-        *reinterpret_cast<u32x4*>(at + 2 * PLANE) = s.l;
-      } else {
-        *reinterpret_cast<uint4*>(at) = make_uint4(pack2_bf16(v[h][0], v[h][1]), pack2_bf16(v[h][2], v[h][3]), pack2_bf16(v[h][4], v[h][5]), pack2_bf16(v[h][6], v[h][7]));
+      for (int i = 0; i < 4; ++i) {
+        lo[i] = __float_as_uint(v[h][i]);
+        hi[i] = __float_as_uint(v[h][4 + i]);
       }
+      const Split8 s = split8(lo, hi);
+      *reinterpret_cast<u32x4*>(at) = s.h;
+      *reinterpret_cast<u32x4*>(at + PLANE) = s.m;
+      *reinterpret_cast<u32x4*>(at + 2 * PLANE) = s.l;
     }
   }
   // Granules of eight elements are exchanged within a row so that the lanes of a read fall into different banks: rows of 64 bytes (k-major), read
@@ -100,12 +96,16 @@ __device__ __forceinline__ void mma(floatx4& acc, const u32x4& a, const u32x4& b
   acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
 }
 
-// four neighbouring outputs of one row
+// four neighbouring outputs of one row, of any alignment
 template <typename C>
-__device__ __forceinline__ void store_four(C* p, int left, const float (&v)[4], bool vec) {
-  if (vec && left >= 4) {
-    if constexpr (sizeof(C) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else *reinterpret_cast<uint2*>(p) = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
+__device__ __forceinline__ void store_four(C* p, int left, const float (&v)[4]) {
+  if (left >= 4) {
+    if constexpr (sizeof(C) == 4) {
+      *reinterpret_cast<Words<4>::T*>(p) = Words<4>::T{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    } else {
+      typedef unsigned two __attribute__((ext_vector_type(2), aligned(2)));
+      *reinterpret_cast<two*>(p) = two{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -113,30 +113,37 @@ __device__ __forceinline__ void store_four(C* p, int left, const float (&v)[4], 
   }
 }
 
-template <typename T, int KIND>
-__global__ __launch_bounds__(256, 2) void linear_any_kernel(LinearArgs q) {
-  typedef Staged<T, KIND != WGRAD> SA;
-  typedef Staged<T, KIND == FORWARD> SB;
-  typedef typename std::conditional<KIND == WGRAD, float, T>::type C;
-  constexpr int P = SA::PLANES;
-  __shared__ __align__(16) unsigned char lds[2 * P * RT * RK * 2];
-  unsigned char *la = lds, *lb = lds + P * RT * RK * 2;
+// The part of an expert's rows that block `part` of `parts` takes: whole steps of 64.
+__device__ __forceinline__ void part_of(int part, int parts, int& begin, int& end) {
+  const int each = ((end - begin + parts - 1) / parts + 63) / 64 * 64;
+  begin = (int)min((long long)begin + (long long)part * each, (long long)end);
+  end = min(end - begin, each) + begin;
+}
+
+template <int KIND>
+__global__ __launch_bounds__(256, 2) void linear_fp32_kernel(LinearArgs q) {
+  typedef Staged<KIND != WGRAD> SA;
+  typedef Staged<KIND == FORWARD> SB;
+  __shared__ __align__(16) unsigned char lds[2 * 3 * RT * RK * 2];
+  unsigned char *la = lds, *lb = lds + 3 * RT * RK * 2;
 
   const int n_tiles = (q.n + RT - 1) / RT, n0 = (int)(blockIdx.x % n_tiles) * RT;
-  int group, m0, m_end, k_begin = 0, k_end = q.k;
+  int group, m0, m_end, k_begin = 0, k_end = q.k, part = 0;
   if (KIND == WGRAD) {
-    const int m_tiles = (q.m + RT - 1) / RT, t = blockIdx.x / n_tiles;
-    group = t / m_tiles;
+    const int m_tiles = (q.m + RT - 1) / RT, t = blockIdx.x / n_tiles, e = t / m_tiles;
+    part = e % q.parts;
+    group = e / q.parts;
     m0 = t % m_tiles * RT;
     m_end = q.m;
     group_rows(q.offs, q.groups, q.rows, group, k_begin, k_end);
+    part_of(part, q.parts, k_begin, k_end);
   } else {
     if (!find_tile(q.offs, q.groups, q.rows, RT, blockIdx.x / n_tiles, group, m0, m_end)) return;
     if (group == q.groups) k_end = 0;                             // rows of no expert: zeros
   }
-  const T* a = (const T*)q.a;
-  const T* b = (const T*)q.b + (KIND == WGRAD ? 0 : (long long)(group < q.groups ? group : 0) * q.b_group);
-  C* c = (C*)q.c + (KIND == WGRAD ? (long long)group * q.c_group : 0);
+  const float* a = (const float*)q.a;
+  const float* b = (const float*)q.b + (KIND == WGRAD ? 0 : (long long)(group < q.groups ? group : 0) * q.b_group);
+  float* c = (float*)q.c + (KIND == WGRAD ? part * q.part + (long long)group * q.c_group : 0);
 
   const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
   floatx4 acc[4][4], low[4][4];
@@ -148,8 +155,8 @@ __global__ __launch_bounds__(256, 2) void linear_any_kernel(LinearArgs q) {
   SA sa;
   SB sb;
   if (k_begin < k_end) {
-    sa.load(a, q.a_stride, m0, m_end, k_begin, k_end, q.vec & 1);
-    sb.load(b, q.b_stride, n0, q.n, k_begin, k_end, q.vec & 2);
+    sa.load(a, q.a_stride, m0, m_end, k_begin, k_end);
+    sb.load(b, q.b_stride, n0, q.n, k_begin, k_end);
   }
   for (int k0 = k_begin; k0 < k_end; k0 += RK) {
     __syncthreads();
@@ -157,44 +164,40 @@ __global__ __launch_bounds__(256, 2) void linear_any_kernel(LinearArgs q) {
     sb.store(lb);
     __syncthreads();
     if (k0 + RK < k_end) {
-      sa.load(a, q.a_stride, m0, m_end, k0 + RK, k_end, q.vec & 1);
-      sb.load(b, q.b_stride, n0, q.n, k0 + RK, k_end, q.vec & 2);
+      sa.load(a, q.a_stride, m0, m_end, k0 + RK, k_end);
+      sb.load(b, q.b_stride, n0, q.n, k0 + RK, k_end);
     }
-    u32x4 fa[4][P];
+    u32x4 fa[4][3];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int p = 0; p < P; ++p) fa[i][p] = SA::read(la + p * SA::PLANE, wm + i * 16);
+      for (int p = 0; p < 3; ++p) fa[i][p] = SA::read(la + p * SA::PLANE, wm + i * 16);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      u32x4 fb[P];
+      u32x4 fb[3];
 #pragma unroll
-      for (int p = 0; p < P; ++p) fb[p] = SB::read(lb + p * SB::PLANE, wn + j * 16);
+      for (int p = 0; p < 3; ++p) fb[p] = SB::read(lb + p * SB::PLANE, wn + j * 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {                               // (b first: a lane then holds four neighbouring columns of one row)
         mma(acc[i][j], fb[0], fa[i][0]);
-        if constexpr (P == 3) {
-          mma(low[i][j], fb[0], fa[i][1]);
-          mma(low[i][j], fb[1], fa[i][0]);
-          mma(low[i][j], fb[1], fa[i][1]);
-          mma(low[i][j], fb[0], fa[i][2]);
-          mma(low[i][j], fb[2], fa[i][0]);
-        }
+        mma(low[i][j], fb[0], fa[i][1]);
+        mma(low[i][j], fb[1], fa[i][0]);
+        mma(low[i][j], fb[1], fa[i][1]);
+        mma(low[i][j], fb[0], fa[i][2]);
+        mma(low[i][j], fb[2], fa[i][0]);
       }
     }
   }
 
-  bool again = false;                                             // fp32: a value out of the parts' range, an infinity or NaN
-  if constexpr (P == 3) {
+  bool again = false;                                             // a value out of the parts' range, an infinity or NaN
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        acc[i][j] = (acc[i][j] + low[i][j]) * SPLIT_UNSCALE;
+    for (int j = 0; j < 4; ++j) {
+      acc[i][j] = (acc[i][j] + low[i][j]) * SPLIT_UNSCALE;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) again |= !finite_bits(__float_as_uint(acc[i][j][e]) & 0x7fffffffu);
-      }
-  }
+      for (int e = 0; e < 4; ++e) again |= !finite_bits(__float_as_uint(acc[i][j][e]) & 0x7fffffffu);
+    }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int m = m0 + wm + i * 16 + (l & 15);
@@ -209,24 +212,23 @@ __global__ __launch_bounds__(256, 2) void linear_any_kernel(LinearArgs q) {
           if (n + e >= q.n) continue;
           float sum = 0.f;
           for (int k = k_begin; k < k_end; ++k) {
-            const float x = to_float(KIND == WGRAD ? a[(long long)k * q.a_stride + m] : a[(long long)m * q.a_stride + k]);
-            const float y = to_float(KIND == FORWARD ? b[(long long)(n + e) * q.b_stride + k] : b[(long long)k * q.b_stride + n + e]);
+            const float x = KIND == WGRAD ? a[(long long)k * q.a_stride + m] : a[(long long)m * q.a_stride + k];
+            const float y = KIND == FORWARD ? b[(long long)(n + e) * q.b_stride + k] : b[(long long)k * q.b_stride + n + e];
             sum = fmaf(x, y, sum);
           }
           v[e] = sum;
         }
       }
-      store_four<C>(c + (long long)m * q.c_stride + n, q.n - n, v, q.vec & 4);
+      store_four<float>(c + (long long)m * q.c_stride + n, q.n - n, v);
     }
   }
 }
 
-
-// ---- rows of multiples of 16 bytes: bf16, and 8 bits ----
+// ---- bf16 and 8 bits ----
 //
 // Tiles of BM x BN, 64 of the sum's index a step, in LDS as bf16: k-major operands in rows of 128 bytes, the others as 64 rows (sum indices) of BM or BN
-// values that are read with transposing reads.  bf16 operands are copied straight from memory while the step before the last is multiplied; 8-bit ones go through
-// registers, where a code times its block's power of two becomes the bf16 number that it is: every product is exact and every sum fp32.
+// values that are read with transposing reads.  bf16 operands are copied straight from memory while the step before the last is multiplied; those whose rows are
+// no multiples of 16 bytes go through registers, and so do 8-bit ones, where a code times its block's power of two becomes the bf16 number that it is: every product is exact and every sum fp32.
 // (The 8-bit MFMAs would take half the matrix-pipe time, but they add eight neighbouring products with what lies 2^-13 below the largest of them
 // cut off (2^16 + 2^2 is 2^16): 1.5e-5 of the result's norm on normal values, 5e-5 on codes of all sizes.)
 constexpr int STEP = 64;
@@ -263,7 +265,34 @@ struct Tile {
 
 __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(unsigned long long)(__attribute__((address_space(3))) const void*)p; }
 
-// A bf16 operand: copies.
+// Eight neighbouring bf16 values of any alignment, of which `n` are the row's last (more than eight, or none).  The last few of a row are read as the end of its
+// last eight (a row of fewer than eight: one by one), and shifted when they are used, so that nothing is waited for between the loads.
+__device__ __forceinline__ u32x4 load_last(const bf16_t* p, int n, bool short_row) {
+  u32x4 v = {0, 0, 0, 0};
+  if (short_row) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) v[i / 2] |= (unsigned)p[i].v << 16 * (i % 2);
+  } else if (n > 0) {
+    v = __builtin_bit_cast(u32x4, *reinterpret_cast<const Words<2>::T*>(p - max(8 - n, 0)));
+  }
+  return v;
+}
+__device__ __forceinline__ u32x4 shift_last(const u32x4& v, int n, bool short_row) {
+  if (n >= 8 || short_row) return v;
+  unsigned long long lo = v[0] | (unsigned long long)v[1] << 32, hi = v[2] | (unsigned long long)v[3] << 32;
+  const int bits = 16 * (8 - n);                                  // 16 or more
+  if (bits >= 64) {
+    lo = bits < 128 ? hi >> (bits - 64) : 0;
+    hi = 0;
+  } else {
+    lo = lo >> bits | hi << (64 - bits);
+    hi >>= bits;
+  }
+  return u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+
+// A bf16 operand whose rows are multiples of 16 bytes: copies.
 template <bool KMAJOR, int R, int NW>
 struct Copied : Tile<KMAJOR, R, NW> {
   typedef Tile<KMAJOR, R, NW> S;
@@ -298,6 +327,51 @@ struct Copied : Tile<KMAJOR, R, NW> {
     const int l = threadIdx.x & 63, piece = wave * S::PIECES + p;
     const int k = KMAJOR ? ((l & 7) ^ S::swap_of(piece * 8 + (l >> 3))) * 8 : piece * (64 / S::PER_ROW) + l / S::PER_ROW;
     load16_to_lds(memory, k < left ? off[p] : NO_ROW, 0, lds + piece * 1024);
+  }
+};
+
+// A bf16 operand of any alignment: chunks of eight elements, which are written to LDS a step after they were asked for.
+template <bool KMAJOR, int R, int NW>
+struct Loaded : Tile<KMAJOR, R, NW> {
+  typedef Tile<KMAJOR, R, NW> S;
+  typedef bf16_t T;
+  static constexpr bool COPIES = false;
+  static constexpr int CHUNKS = R * 8 / (64 * NW);
+  static constexpr int PIECES = CHUNKS;
+  static_assert(R * 8 % (64 * NW) == 0, "whole chunks");
+  u32x4 q[CHUNKS];
+  const T* at;                                                    // of the step that is asked for next
+  long long stride;
+  int rows, left;                                                 // and the sum indices from it on
+  bool short_row;
+
+  __device__ static __forceinline__ int row_of(int p) { return (threadIdx.x + p * 64 * NW) / (KMAJOR ? 8 : S::PER_ROW); }
+  __device__ static __forceinline__ int granule_of(int p) { return (threadIdx.x + p * 64 * NW) % (KMAJOR ? 8 : S::PER_ROW); }
+  // of a step with `left_` sum indices from it on, the elements from chunk p's first on
+  __device__ __forceinline__ int there(int p, int left_) const {
+    return row_of(p) < (KMAJOR ? rows : left_) ? (KMAJOR ? left_ : rows) - granule_of(p) * 8 : 0;
+  }
+  __device__ __forceinline__ void prepare(const T* base, const uint8_t*, long long stride_, int row0, int rows_, int k0, int k_end, int) {
+    stride = stride_;
+    rows = rows_;
+    at = base + (KMAJOR ? row0 * stride + k0 : k0 * stride + row0);
+    left = k_end - k0;
+    short_row = (KMAJOR ? k_end : row0 + rows) < 8;
+#pragma unroll
+    for (int p = 0; p < CHUNKS; ++p) ask(p);
+    step_on();
+  }
+  __device__ __forceinline__ void step_on() {
+    at += KMAJOR ? STEP : STEP * stride;
+    left -= STEP;
+  }
+  __device__ __forceinline__ void ask(int p) { q[p] = load_last(at + row_of(p) * stride + granule_of(p) * 8, there(p, left), short_row); }
+  __device__ __forceinline__ void next_step() {}
+  __device__ __forceinline__ void piece(int p, int, int, unsigned char* lds, unsigned) {
+    const int r = row_of(p), g = granule_of(p) ^ S::swap_of(r);
+    *reinterpret_cast<u32x4*>(lds + r * (KMAJOR ? 128 : R * 2) + g * 16) = shift_last(q[p], there(p, left + STEP), short_row);
+    ask(p);
+    if (p == CHUNKS - 1) step_on();
   }
 };
 
@@ -357,12 +431,18 @@ struct Converted : Tile<true, R, NW> {
   }
 };
 
+enum Form { ALIGNED, ANY, EIGHT_BITS };
+template <Form F, bool KMAJOR, int R, int NW> struct Operand { typedef Copied<KMAJOR, R, NW> type; };
+template <bool KMAJOR, int R, int NW> struct Operand<ANY, KMAJOR, R, NW> { typedef Loaded<KMAJOR, R, NW> type; };
+template <int R, int NW> struct Operand<EIGHT_BITS, true, R, NW> { typedef Converted<R, NW> type; };
+
 // One tile of expert `group` (q.groups: of none): rows m0 .. m_end - 1, columns n0 .., sum indices k_begin .. k_end - 1.
-template <bool EIGHT, int KIND, int BM, int BN, int WM, int WN, typename C>
-__device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char* lds, int group, int m0, int m_end, int n0, int k_begin, int k_end) {
+template <Form F, int KIND, int BM, int BN, int WM, int WN, typename C>
+__device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char* lds, int group, int part, int m0, int m_end, int n0, int k_begin, int k_end) {
   constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-  typedef typename std::conditional<EIGHT, Converted<BM, NW>, Copied<KIND != WGRAD, BM, NW>>::type CA;
-  typedef typename std::conditional<EIGHT, Converted<BN, NW>, Copied<KIND == FORWARD, BN, NW>>::type CB;
+  constexpr bool EIGHT = F == EIGHT_BITS;
+  typedef typename Operand<F, KIND != WGRAD, BM, NW>::type CA;
+  typedef typename Operand<F, KIND == FORWARD, BN, NW>::type CB;
   typedef typename CA::T T;
   constexpr int STAGE = CA::BYTES + CB::BYTES;                    // two of them
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
@@ -442,44 +522,35 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
 
   // Sixteen rows of a wave's columns at a time go through LDS, so that its lanes store whole rows, 16 bytes each: 64 lanes with four columns each of
   // sixteen rows would write 32 or 64 bytes of a row at a time, at 2.5 TB/s.
-  C* c = (C*)q.c + (KIND == WGRAD ? (long long)group * q.c_group : 0);
+  C* c = (C*)q.c + (KIND == WGRAD ? part * q.part + (long long)group * q.c_group : 0);
   constexpr int WIDE = TN * 16 * (int)sizeof(C), LANES = WIDE / 16, EACH = 16 / (int)sizeof(C);
   unsigned char* out = lds + wave * 16 * (WIDE + 16);
   static_assert(NW * 16 * (WIDE + 16) <= 2 * STAGE && 64 % LANES == 0, "the outputs' LDS");
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     if (m0 + wm + i * 16 >= m_end) break;
-    if (q.vec & 4) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-        store_four<C>((C*)(out + (l & 15) * (WIDE + 16)) + j * 16 + (l >> 4) * 4, 4, v, true);
-      }
-      __builtin_amdgcn_wave_barrier();
+    for (int j = 0; j < TN; ++j) {
+      const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+      unsigned char* at = out + (l & 15) * (WIDE + 16) + (j * 16 + (l >> 4) * 4) * (int)sizeof(C);
+      if constexpr (sizeof(C) == 4) *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
+      else *reinterpret_cast<uint2*>(at) = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
+    }
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int r = l / LANES; r < 16; r += 64 / LANES) {
-        const int m = m0 + wm + i * 16 + r, n = n0 + wn + l % LANES * EACH;
-        const uint4 v = *reinterpret_cast<const uint4*>(out + r * (WIDE + 16) + l % LANES * 16);
-        if (m >= m_end || n >= q.n) continue;
-        C* at = c + (long long)m * q.c_stride + n;
-        if (n + EACH <= q.n) {
-          *reinterpret_cast<uint4*>(at) = v;
-        } else {
-          const C* e = reinterpret_cast<const C*>(out + r * (WIDE + 16) + l % LANES * 16);
-          for (int k = 0; k < q.n - n; ++k) at[k] = e[k];
-        }
-      }
-      __builtin_amdgcn_wave_barrier();
-    } else {
-      const int m = m0 + wm + i * 16 + (l & 15);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int n = n0 + wn + j * 16 + (l >> 4) * 4;
-        if (m >= m_end || n >= q.n) continue;
-        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-        store_four<C>(c + (long long)m * q.c_stride + n, q.n - n, v, false);
+    for (int r = l / LANES; r < 16; r += 64 / LANES) {
+      const int m = m0 + wm + i * 16 + r, n = n0 + wn + l % LANES * EACH;
+      const uint4 v = *reinterpret_cast<const uint4*>(out + r * (WIDE + 16) + l % LANES * 16);
+      if (m >= m_end || n >= q.n) continue;
+      C* at = c + (long long)m * q.c_stride + n;
+      if (n + EACH <= q.n) {
+        *reinterpret_cast<typename Words<sizeof(C)>::T*>(at) = typename Words<sizeof(C)>::T{v.x, v.y, v.z, v.w};
+      } else {
+        const C* e = reinterpret_cast<const C*>(out + r * (WIDE + 16) + l % LANES * 16);
+        for (int k = 0; k < q.n - n; ++k) at[k] = e[k];
       }
     }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -494,7 +565,7 @@ __device__ __forceinline__ void banded(unsigned id, unsigned row_tiles, unsigned
 
 // Forward and dgrad.  Block b runs on XCD b % 8: each XCD takes one stretch of the whole tiles, then its share of the experts' shorter last ones, in
 // half the height where that is enough.
-template <bool EIGHT, int KIND, int BM, int BN, int WM, int WN, typename C>
+template <Form F, int KIND, int BM, int BN, int WM, int WN, typename C>
 __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearArgs q) {
   extern __shared__ __align__(1024) unsigned char lds[];
   unsigned whole, ends;
@@ -507,44 +578,289 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearArgs q) {
     unsigned r, c;
     banded(id, whole, cols, r, c);
     find_tile_of<false>(q.offs, q.groups, q.rows, BM, r, group, m0, m_end);
-    tile_product<EIGHT, KIND, BM, BN, WM, WN, C>(q, lds, group, m0, m_end, (int)c * BN, 0, group < q.groups ? q.k : 0);
+    tile_product<F, KIND, BM, BN, WM, WN, C>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, group < q.groups ? q.k : 0);
   } else {
     const unsigned id = (i - share) * 8 + xcd;
     if (id >= ends * cols) return;
     find_tile_of<true>(q.offs, q.groups, q.rows, BM, id / cols, group, m0, m_end);
     const int n0 = (int)(id % cols) * BN, k = group < q.groups ? q.k : 0;
-    if (m_end - m0 > BM / 2) tile_product<EIGHT, KIND, BM, BN, WM, WN, C>(q, lds, group, m0, m_end, n0, 0, k);
-    else tile_product<EIGHT, KIND, BM / 2, BN, WM, WN, C>(q, lds, group, m0, m_end, n0, 0, k);
+    if (m_end - m0 > BM / 2) tile_product<F, KIND, BM, BN, WM, WN, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
+    else tile_product<F, KIND, BM / 2, BN, WM, WN, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
   }
 }
 
-template <int BM, int BN, int WM, int WN>
+template <Form F, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void linear_wgrad_kernel(LinearArgs q) {
   extern __shared__ __align__(1024) unsigned char lds[];
-  const int n_tiles = (q.n + BN - 1) / BN, m_tiles = (q.m + BM - 1) / BM, t = blockIdx.x / n_tiles;
+  const int n_tiles = (q.n + BN - 1) / BN, m_tiles = (q.m + BM - 1) / BM, t = blockIdx.x / n_tiles, e = t / m_tiles, group = e / q.parts, part = e % q.parts;
   int begin, end;
-  group_rows(q.offs, q.groups, q.rows, t / m_tiles, begin, end);
-  tile_product<false, WGRAD, BM, BN, WM, WN, float>(q, lds, t / m_tiles, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
+  group_rows(q.offs, q.groups, q.rows, group, begin, end);
+  part_of(part, q.parts, begin, end);
+  tile_product<F, WGRAD, BM, BN, WM, WN, float>(q, lds, group, part, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
+}
+
+// dw = the parts, added in order
+__global__ __launch_bounds__(256) void sum_parts_kernel(const float* parts, float* dw, long long n, int count) {
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+    float s = parts[i];
+    for (int p = 1; p < count; ++p) s += parts[p * n + i];
+    dw[i] = s;
+  }
+}
+
+// ---- few rows ----
+//
+// Tiles of 16 TM rows and few columns, whose sum the block's waves share: wave w takes the chunks w, w + NW, ... of it, straight from memory into MFMA
+// operands, and the waves' sums are joined in order through LDS.  Bound by the weights' bytes: every lane has U loads of 16 bytes of them in flight and more of the rows.
+// A lane's 16 bytes of a k-major operand are one row's; of dgrad's weights, whose sum index is the row, they are neighbouring columns of one
+// row: column 8 c + j (bf16; 4 c + j in fp32) of the tile is column c = l % 16 of MFMA j.  fp32 goes through the fp32 MFMA.
+template <typename T> struct Few;                                 // EACH: elements of 16 bytes; DEEP: sum indices that four lanes' 16 bytes of a row cover
+template <> struct Few<float> { static constexpr int EACH = 4, DEEP = 16; };
+template <> struct Few<bf16_t> { static constexpr int EACH = 8, DEEP = 32; };
+template <> struct Few<uint8_t> { static constexpr int EACH = 16, DEEP = 64; };
+
+__device__ __forceinline__ u32x4 load16(const __amdgpu_buffer_rsrc_t& b, unsigned off) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, (int)off, 0, 0)); }
+
+// the first `left` of four fp32 values
+__device__ __forceinline__ u32x4 first_of(u32x4 v, int left) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = i < left ? v[i] : 0u;
+  return v;
+}
+
+struct Pair8 { u32x4 lo, hi; };
+__device__ __forceinline__ Pair8 to_bf16(const u32x4& q, int byte) {
+  const float f = power_of_two(byte);
+  Pair8 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    r.lo[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[i], f, false));
+    r.lo[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[i], f, true));
+    r.hi[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 + i], f, false));
+    r.hi[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 + i], f, true));
+  }
+  return r;
+}
+
+// Sums of the waves for each lane's Q quads of outputs, added in the waves' order; eight quads at a time.
+template <int Q, int NW, typename F>
+__device__ __forceinline__ void join_waves(const floatx4 (&acc)[Q], F&& write) {
+  constexpr int EIGHT = Q < 8 ? Q : 8;
+  static_assert(Q % EIGHT == 0, "whole eights");
+  __shared__ float4 part[NW][EIGHT][64];
+  const int wave = threadIdx.x >> 6, l = threadIdx.x & 63;
+#pragma unroll
+  for (int first = 0; first < Q; first += EIGHT) {
+    if (first) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < EIGHT; ++k) part[wave][k][l] = make_float4(acc[first + k][0], acc[first + k][1], acc[first + k][2], acc[first + k][3]);
+    __syncthreads();
+    for (int k = wave; k < EIGHT; k += NW) {
+      float4 v = part[0][k][l];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) {
+        const float4 o = part[w][k][l];
+        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+      }
+      const float f[4] = {v.x, v.y, v.z, v.w};
+      write(first + k, f);
+    }
+  }
+}
+
+// Forward: JT sixteens of columns; U chunks of DEEP sum indices a turn.
+template <typename T, int TM, int JT, int U, int NW, bool ANY_ROWS, typename C>
+__global__ __launch_bounds__(64 * NW) void linear_few_kernel(LinearArgs q) {
+  constexpr int EACH = Few<T>::EACH, DEEP = Few<T>::DEEP, ES = (int)sizeof(T);
+  const int cols = (q.n + 16 * JT - 1) / (16 * JT), n0 = (int)(blockIdx.x % cols) * 16 * JT;
+  int group, m0, m_end;
+  if (!find_tile(q.offs, q.groups, q.rows, 16 * TM, blockIdx.x / cols, group, m0, m_end)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+  floatx4 acc[TM * JT];
+#pragma unroll
+  for (int i = 0; i < TM * JT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  if (group < q.groups) {
+    const int rows = min(16 * TM, m_end - m0), outs = min(16 * JT, q.n - n0);
+    const T *x_rows = (const T*)q.a + m0 * q.a_stride, *w_rows = (const T*)q.b + group * q.b_group + n0 * q.b_stride;
+    const __amdgpu_buffer_rsrc_t x = buffer_of(x_rows, (unsigned long long)(((rows - 1) * q.a_stride + q.k) * ES));
+    const __amdgpu_buffer_rsrc_t w = buffer_of(w_rows, (unsigned long long)(((outs - 1) * q.b_stride + q.k) * ES));
+    const long long blocks = q.b_stride / BLOCK8;
+    const __amdgpu_buffer_rsrc_t xs = buffer_of(q.a_scale + m0 * blocks, (unsigned long long)(rows * blocks));
+    const __amdgpu_buffer_rsrc_t ws = buffer_of(q.b_scale + (group * (long long)q.n + n0) * blocks, (unsigned long long)(outs * blocks));
+    unsigned xo[TM], wo[JT];                                      // (rows that are none lie behind the buffers' ends)
+#pragma unroll
+    for (int i = 0; i < TM; ++i) xo[i] = (unsigned)((i * 16 + (l & 15)) * q.a_stride * ES);
+#pragma unroll
+    for (int j = 0; j < JT; ++j) wo[j] = (unsigned)((j * 16 + (l & 15)) * q.b_stride * ES);
+    // Neighbouring tiles of columns start at different places of the sum: with rows of 8 KiB all of them would ask the same few memory channels at a time.
+    const int turns = (q.k + NW * DEEP * U - 1) / (NW * DEEP * U), start = (int)(blockIdx.x % cols) % turns;
+    for (int turn = 0; turn < turns; ++turn) {
+      const int k0 = ((turn + start < turns ? turn + start : turn + start - turns) * NW + wave) * DEEP * U;
+      u32x4 fx[U][TM], fw[U][JT];
+      int bx[U][TM], bw[U][JT];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + u * DEEP + (l >> 4) * EACH;
+        const bool in = k < q.k;
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+          if constexpr (ANY_ROWS) fw[u][j] = load_last(w_rows + (long long)(j * 16 + (l & 15)) * q.b_stride + k, j * 16 + (l & 15) < outs ? q.k - k : 0, q.k < 8);
+          else fw[u][j] = load16(w, in ? wo[j] + k * ES : NO_ROW);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          if constexpr (ANY_ROWS) fx[u][i] = load_last(x_rows + (long long)(i * 16 + (l & 15)) * q.a_stride + k, i * 16 + (l & 15) < rows ? q.k - k : 0, q.k < 8);
+          else fx[u][i] = load16(x, in ? xo[i] + k * ES : NO_ROW);
+        }
+        if constexpr (ES == 1) {
+#pragma unroll
+          for (int j = 0; j < JT; ++j) bw[u][j] = __builtin_amdgcn_raw_buffer_load_b8(ws, in ? (j * 16 + (l & 15)) * (int)blocks + k / BLOCK8 : (int)NO_ROW, 0, 0);
+#pragma unroll
+          for (int i = 0; i < TM; ++i) bx[u][i] = __builtin_amdgcn_raw_buffer_load_b8(xs, in ? (i * 16 + (l & 15)) * (int)blocks + k / BLOCK8 : (int)NO_ROW, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);                          // (all of them in flight before the first is waited for)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if constexpr (ES == 4) {
+          const int left = q.k - (k0 + u * DEEP + (l >> 4) * EACH);
+          if (q.k % EACH) {                                       // (the values behind a row's last are the next row's)
+#pragma unroll
+            for (int j = 0; j < JT; ++j) fw[u][j] = first_of(fw[u][j], left);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fx[u][i] = first_of(fx[u][i], left);
+          }
+        }
+        if constexpr (ANY_ROWS) {
+          const int left = q.k - (k0 + u * DEEP + (l >> 4) * EACH);
+#pragma unroll
+          for (int j = 0; j < JT; ++j) fw[u][j] = shift_last(fw[u][j], left, q.k < 8);
+#pragma unroll
+          for (int i = 0; i < TM; ++i) fx[u][i] = shift_last(fx[u][i], left, q.k < 8);
+        }
+        Pair8 px[TM];
+        if constexpr (ES == 1)
+#pragma unroll
+          for (int i = 0; i < TM; ++i) px[i] = to_bf16(fx[u][i], bx[u][i]);
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+          if constexpr (ES == 1) {
+            const Pair8 pw = to_bf16(fw[u][j], bw[u][j]);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+              mma(acc[i * JT + j], pw.lo, px[i].lo);
+              mma(acc[i * JT + j], pw.hi, px[i].hi);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+              if constexpr (ES == 2) {
+                mma(acc[i * JT + j], fw[u][j], fx[u][i]);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  acc[i * JT + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fw[u][j][e]), __uint_as_float(fx[u][i][e]), acc[i * JT + j], 0, 0, 0);
+              }
+            }
+          }
+        }
+      }
+    }
+  }
+  join_waves<TM * JT, NW>(acc, [&](int k, const float (&v)[4]) {
+    const int m = m0 + k / JT * 16 + (l & 15), n = n0 + k % JT * 16 + (l >> 4) * 4;
+    if (m < m_end && n < q.n) store_four<C>((C*)q.c + (long long)m * q.c_stride + n, q.n - n, v);
+  });
+}
+
+// dgrad: sixteen lanes' 16 bytes of columns; 8 (bf16) or 4 (fp32) sum indices for each load of the rows.
+template <typename T, int TM, int U, int NW, bool ANY_ROWS>
+__global__ __launch_bounds__(64 * NW) void linear_few_dgrad_kernel(LinearArgs q) {
+  constexpr int EACH = Few<T>::EACH, DEEP = Few<T>::DEEP, ES = (int)sizeof(T), BN = 16 * EACH;
+  const int cols = (q.n + BN - 1) / BN, n0 = (int)(blockIdx.x % cols) * BN;
+  int group, m0, m_end;
+  if (!find_tile(q.offs, q.groups, q.rows, 16 * TM, blockIdx.x / cols, group, m0, m_end)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+  floatx4 acc[TM * EACH];
+#pragma unroll
+  for (int i = 0; i < TM * EACH; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  if (group < q.groups) {
+    const int rows = min(16 * TM, m_end - m0), col = n0 + (l & 15) * EACH;
+    const T *x_rows = (const T*)q.a + m0 * q.a_stride, *w_rows = (const T*)q.b + group * q.b_group;
+    const __amdgpu_buffer_rsrc_t x = buffer_of(x_rows, (unsigned long long)(((rows - 1) * q.a_stride + q.k) * ES));
+    const __amdgpu_buffer_rsrc_t w = buffer_of(w_rows, (unsigned long long)(((q.k - 1) * q.b_stride + q.n) * ES));
+    unsigned xo[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) xo[i] = (unsigned)((i * 16 + (l & 15)) * q.a_stride * ES);
+    for (int k0 = wave * DEEP * U; k0 < q.k; k0 += NW * DEEP * U) {
+      u32x4 fx[U][TM], fw[U][EACH];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + u * DEEP + (l >> 4) * EACH;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+          if constexpr (ANY_ROWS) fw[u][e] = load_last(w_rows + (k + e) * q.b_stride + col, k + e < q.k ? q.n - col : 0, q.n < 8);
+          else fw[u][e] = load16(w, k + e < q.k && col < q.n ? (unsigned)(((k + e) * q.b_stride + col) * ES) : NO_ROW);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          if constexpr (ANY_ROWS) fx[u][i] = load_last(x_rows + (long long)(i * 16 + (l & 15)) * q.a_stride + k, i * 16 + (l & 15) < rows ? q.k - k : 0, q.k < 8);
+          else fx[u][i] = load16(x, k < q.k ? xo[i] + k * ES : NO_ROW);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if constexpr (ANY_ROWS) {
+#pragma unroll
+          for (int e = 0; e < EACH; ++e) fw[u][e] = shift_last(fw[u][e], q.n - col, q.n < 8);
+#pragma unroll
+          for (int i = 0; i < TM; ++i) fx[u][i] = shift_last(fx[u][i], q.k - (k0 + u * DEEP + (l >> 4) * EACH), q.k < 8);
+        }
+        if constexpr (ES == 4) {
+          if (q.k % EACH)
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fx[u][i] = first_of(fx[u][i], q.k - (k0 + u * DEEP + (l >> 4) * EACH));
+#pragma unroll
+          for (int j = 0; j < EACH; ++j)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+              for (int e = 0; e < EACH; ++e)
+                acc[i * EACH + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fx[u][i][e]), __uint_as_float(fw[u][e][j]), acc[i * EACH + j], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int j = 0; j < EACH; ++j) {                        // column j of the lane's eight: element j of its eight loads
+            u32x4 b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = __builtin_amdgcn_perm(fw[u][2 * e + 1][j / 2], fw[u][2 * e][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) mma(acc[i * EACH + j], fx[u][i], b);
+          }
+        }
+      }
+    }
+  }
+  // acc[i][j][e]: row 16 i + 4 (l / 16) + e, column EACH (l % 16) + j; neighbouring columns together
+  floatx4 out[TM * EACH];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int h = 0; h < EACH / 4; ++h)
+        out[(i * 4 + e) * (EACH / 4) + h] = floatx4{acc[i * EACH + 4 * h][e], acc[i * EACH + 4 * h + 1][e], acc[i * EACH + 4 * h + 2][e], acc[i * EACH + 4 * h + 3][e]};
+  join_waves<TM * EACH, NW>(out, [&](int k, const float (&v)[4]) {
+    const int h = k % (EACH / 4), e = k / (EACH / 4) % 4, m = m0 + k / EACH * 16 + (l >> 4) * 4 + e, n = n0 + (l & 15) * EACH + 4 * h;
+    if (m < m_end && n < q.n) store_four<T>((T*)q.c + (long long)m * q.c_stride + n, q.n - n, v);
+  });
 }
 
 // ---- launches ----
 
 constexpr long long MOST_BLOCKS = 0x7fffffff;
 
-template <typename T>
-gan_status launch_any(int kind, const LinearArgs& q, hipStream_t st) {
-  const long long n_tiles = (q.n + RT - 1) / RT;
-  const long long blocks = n_tiles * (kind == WGRAD ? (long long)q.groups * ((q.m + RT - 1) / RT) : most_tiles(q.rows, q.groups, RT));
-  if (blocks > MOST_BLOCKS) return operator_fail(GAN_E_SHAPE, "more than 2^31 - 1 tiles");
-  const dim3 grid((unsigned)blocks), block(256);
-  if (kind == FORWARD) hipLaunchKernelGGL((linear_any_kernel<T, FORWARD>), grid, block, 0, st, q);
-  else if (kind == DGRAD) hipLaunchKernelGGL((linear_any_kernel<T, DGRAD>), grid, block, 0, st, q);
-  else hipLaunchKernelGGL((linear_any_kernel<T, WGRAD>), grid, block, 0, st, q);
-  return operator_launched();
-}
-
-template <typename F>
-gan_status launch(F* kernel, long long blocks, int threads, int lds, const LinearArgs& q, hipStream_t st) {
+gan_status launch(void (*kernel)(LinearArgs), long long blocks, int threads, int lds, const LinearArgs& q, hipStream_t st) {
   if (blocks > MOST_BLOCKS) return operator_fail(GAN_E_SHAPE, "more than 2^31 - 1 tiles");
   if (lds > 65536 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) {
     (void)hipGetLastError();
@@ -554,19 +870,66 @@ gan_status launch(F* kernel, long long blocks, int threads, int lds, const Linea
   return operator_launched();
 }
 
-template <bool EIGHT, int KIND, int BM, int BN, int WM, int WN, typename C>
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+// experts that have rows, at most
+long long most_groups(const LinearArgs& q) { return std::max(1, std::min(q.groups, q.rows)); }
+long long tiles(const LinearArgs& q, int height, int width) { return (q.rows / height + most_groups(q)) * ceil_div(q.n, width); }
+long long wgrad_tiles(long long groups, long long m, long long n, int side) { return groups * ceil_div(m, side) * ceil_div(n, side); }
+
+template <Form F, int KIND, int BM, int BN, int WM, int WN, typename C>
 gan_status launch_tiles(const LinearArgs& q, hipStream_t st) {
-  const long long cols = (q.n + BN - 1) / BN;
   constexpr int LDS = 2 * (BM + BN) * 128;
   if constexpr (KIND == WGRAD)
-    return launch(linear_wgrad_kernel<BM, BN, WM, WN>, q.groups * cols * ((q.m + BM - 1) / BM), 64 * WM * WN, LDS, q, st);
+    return launch(linear_wgrad_kernel<F, BM, BN, WM, WN>, q.parts * wgrad_tiles(q.groups, q.m, q.n, BM), 64 * WM * WN, LDS, q, st);
   else    // (whole tiles and ends are each shared among the eight XCDs)
-    return launch(linear_kernel<EIGHT, KIND, BM, BN, WM, WN, C>, 8 * ((most_tiles(q.rows, q.groups, BM) * cols + 7) / 8 + 1), 64 * WM * WN, LDS, q, st);
+    return launch(linear_kernel<F, KIND, BM, BN, WM, WN, C>, 8 * (ceil_div(most_tiles(q.rows, q.groups, BM) * ceil_div(q.n, BN), 8) + 1), 64 * WM * WN, LDS, q, st);
+}
+// 256 x 256 tiles where they fill the CUs, 128 x 128 where not
+template <Form F, int KIND, typename C>
+gan_status launch_large(const LinearArgs& q, hipStream_t st) {
+  const long long big = KIND == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, 256) : tiles(q, 256, 256);
+  if constexpr (F != ANY)
+    if (big >= 256) return launch_tiles<F, KIND, 256, 256, 2, 4, C>(q, st);
+  return launch_tiles<F, KIND, 128, 128, 2, 2, C>(q, st);
 }
 
-template <bool EIGHT, int KIND, typename C>
-gan_status launch_aligned(const LinearArgs& q, hipStream_t st) {
-  return launch_tiles<EIGHT, KIND, 256, 256, 2, 4, C>(q, st);
+template <typename T, int TM, int JT, int U, bool ANY_ROWS, typename C>
+gan_status launch_few_as(const LinearArgs& q, hipStream_t st) {
+  return launch(linear_few_kernel<T, TM, JT, U, 8, ANY_ROWS, C>, most_tiles(q.rows, q.groups, 16 * TM) * ceil_div(q.n, 16 * JT), 512, 0, q, st);
+}
+template <typename T, bool ANY_ROWS, typename C>
+gan_status launch_few(const LinearArgs& q, int sixteens, hipStream_t st) {
+  constexpr int U = sizeof(T) == 1 ? 2 : 4;
+  if (sixteens == 2) return launch_few_as<T, 2, 2, U, ANY_ROWS, C>(q, st);
+  return most_groups(q) * ceil_div(q.n, 32) <= 1024 ? launch_few_as<T, 1, 1, U, ANY_ROWS, C>(q, st) : launch_few_as<T, 1, 2, U, ANY_ROWS, C>(q, st);
+}
+template <typename T, int TM, int U, bool ANY_ROWS>
+gan_status launch_few_dgrad_as(const LinearArgs& q, hipStream_t st) {
+  return launch(linear_few_dgrad_kernel<T, TM, U, 8, ANY_ROWS>, most_tiles(q.rows, q.groups, 16 * TM) * ceil_div(q.n, 16 * Few<T>::EACH), 512, 0, q, st);
+}
+template <typename T, bool ANY_ROWS>
+gan_status launch_few_dgrad(const LinearArgs& q, int sixteens, hipStream_t st) {
+  constexpr int U = sizeof(T) == 4 ? 4 : 2;
+  return sixteens == 2 ? launch_few_dgrad_as<T, 2, U, ANY_ROWS>(q, st) : launch_few_dgrad_as<T, 1, U, ANY_ROWS>(q, st);
+}
+
+// Sixteens of rows for the kernel for few rows, or 0 where tiles are faster.
+int few_rows(const LinearArgs& q, int kind, int esize) {
+  const long long each = q.rows / most_groups(q);
+  if (each <= 8) return 1;
+  if (esize == 4) return tiles(q, 128, 128) < 256 ? (kind == DGRAD ? 1 : 2) : 0;
+  return (long long)q.rows * q.n <= 1 << 19 ? 2 : 0;
+}
+
+gan_status launch_fp32(int kind, const LinearArgs& q, hipStream_t st) {
+  const long long blocks = kind == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, RT) : ceil_div(q.n, RT) * most_tiles(q.rows, q.groups, RT);
+  return launch(kind == FORWARD ? linear_fp32_kernel<FORWARD> : kind == DGRAD ? linear_fp32_kernel<DGRAD> : linear_fp32_kernel<WGRAD>, blocks, 256, 0, q, st);
+}
+
+// Into how many parts the weight gradient takes an expert's rows: few tiles of long sums would leave most CUs idle.
+int wgrad_parts(int groups, long long rows, int n_in, int n_out) {
+  const long long blocks = wgrad_tiles(groups, n_out, n_in, 128), each = rows / std::max(1, groups);
+  return (int)std::max(1ll, std::min({512 / std::max(1ll, blocks), each / 256, 64ll}));
 }
 
 gan_status check(int32_t precision, const void* x, const void* w, const int32_t* offs, int32_t groups, int64_t rows, int32_t n_in, int32_t n_out, const void* out) {
@@ -591,12 +954,13 @@ extern "C" gan_status gan_group_linear(int32_t precision, const void* x, int64_t
   if (x_stride < n_in || y_stride < n_out) return operator_fail(GAN_E_ARG, "x_stride is below n_in, or y_stride below n_out");
   if (rows == 0) return GAN_OK;
   const int e = precision == GAN_FP32 ? 4 : 2;
-  const bool va = rows_aligned16(x, x_stride, e) && n_in % 8 == 0, vb = rows_aligned16(w, n_in, e) && n_in % 8 == 0;
-  const LinearArgs q = {x, w, nullptr, nullptr, y, offs, x_stride, n_in, y_stride, (long long)n_in * n_out, 0, groups, (int)rows, 0, n_out, n_in,
-                        (va ? 1 : 0) | (vb ? 2 : 0) | (rows_aligned16(y, y_stride, e) ? 4 : 0)};
+  const LinearArgs q = {x, w, nullptr, nullptr, y, offs, x_stride, n_in, y_stride, (long long)n_in * n_out, 0, groups, (int)rows, 0, n_out, n_in, 1, 0};
   const hipStream_t st = (hipStream_t)hip_stream;
-  if (precision == GAN_FP32) return launch_any<float>(FORWARD, q, st);
-  return va && vb && short_rows(x_stride, e) && short_rows(n_in, e) ? launch_aligned<false, FORWARD, bf16_t>(q, st) : launch_any<bf16_t>(FORWARD, q, st);
+  const bool small = short_rows(x_stride, e) && short_rows(n_in, e), aligned = small && n_in % 8 == 0 && rows_aligned16(x, x_stride, e) && aligned16(w);
+  const int few = few_rows(q, FORWARD, e);
+  if (precision == GAN_FP32) return few && small ? launch_few<float, false, float>(q, few, st) : launch_fp32(FORWARD, q, st);
+  if (few && small) return aligned ? launch_few<bf16_t, false, bf16_t>(q, few, st) : launch_few<bf16_t, true, bf16_t>(q, few, st);
+  return aligned ? launch_large<ALIGNED, FORWARD, bf16_t>(q, st) : launch_large<ANY, FORWARD, bf16_t>(q, st);
 }
 
 extern "C" gan_status gan_group_linear_dgrad(int32_t precision, const void* dy, int64_t dy_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows,
@@ -605,32 +969,37 @@ extern "C" gan_status gan_group_linear_dgrad(int32_t precision, const void* dy, 
   if (dy_stride < n_out || dx_stride < n_in) return operator_fail(GAN_E_ARG, "dy_stride is below n_out, or dx_stride below n_in");
   if (rows == 0) return GAN_OK;
   const int e = precision == GAN_FP32 ? 4 : 2;
-  const bool va = rows_aligned16(dy, dy_stride, e) && n_out % 8 == 0, vb = rows_aligned16(w, n_in, e) && n_in % 8 == 0;
-  const LinearArgs q = {dy, w, nullptr, nullptr, dx, offs, dy_stride, n_in, dx_stride, (long long)n_in * n_out, 0, groups, (int)rows, 0, n_in, n_out,
-                        (va ? 1 : 0) | (vb ? 2 : 0) | (rows_aligned16(dx, dx_stride, e) ? 4 : 0)};
+  const LinearArgs q = {dy, w, nullptr, nullptr, dx, offs, dy_stride, n_in, dx_stride, (long long)n_in * n_out, 0, groups, (int)rows, 0, n_in, n_out, 1, 0};
   const hipStream_t st = (hipStream_t)hip_stream;
-  if (precision == GAN_FP32) return launch_any<float>(DGRAD, q, st);
-  return va && vb && short_rows(dy_stride, e) && short_rows(n_in, e) ? launch_aligned<false, DGRAD, bf16_t>(q, st) : launch_any<bf16_t>(DGRAD, q, st);
+  const bool small = short_rows(dy_stride, e) && short_rows(n_in, e), aligned = small && n_out % 8 == 0 && n_in % 8 == 0 && rows_aligned16(dy, dy_stride, e) && aligned16(w);
+  const int few = small && (long long)n_in * n_out * e < 1ll << 31 ? few_rows(q, DGRAD, e) : 0;
+  if (precision == GAN_FP32) return few ? launch_few_dgrad<float, false>(q, few, st) : launch_fp32(DGRAD, q, st);
+  if (few) return aligned ? launch_few_dgrad<bf16_t, false>(q, few, st) : launch_few_dgrad<bf16_t, true>(q, few, st);
+  return aligned ? launch_large<ALIGNED, DGRAD, bf16_t>(q, st) : launch_large<ANY, DGRAD, bf16_t>(q, st);
 }
 
 extern "C" int64_t gan_group_linear_wgrad_bytes(int32_t groups, int64_t rows, int32_t n_in, int32_t n_out) {
-  return 0;
+  if (groups < 1 || rows < 1 || n_in < 1 || n_out < 1) return 0;
+  const int parts = wgrad_parts(groups, rows, n_in, n_out);
+  return parts > 1 ? (int64_t)parts * groups * n_in * n_out * (int64_t)sizeof(float) : 0;
 }
 
 extern "C" gan_status gan_group_linear_wgrad(int32_t precision, const void* x, int64_t x_stride, const void* dy, int64_t dy_stride, const int32_t* offs,
                                              int32_t groups, int64_t rows, int32_t n_in, int32_t n_out, float* dw, void* work, int64_t work_bytes, void* hip_stream) {
   if (const gan_status s = check(precision, x, dy, offs, groups, rows, n_in, n_out, dw)) return s;
   if (x_stride < n_in || dy_stride < n_out) return operator_fail(GAN_E_ARG, "x_stride is below n_in, or dy_stride below n_out");
-  if (work_bytes < gan_group_linear_wgrad_bytes(groups, rows, n_in, n_out) || !aligned16(work))
-    return operator_fail(GAN_E_ARG, "work is smaller than gan_group_linear_wgrad_bytes, or not 16-byte aligned");
+  const int64_t need = gan_group_linear_wgrad_bytes(groups, rows, n_in, n_out);
+  if (work_bytes < need || (need > 0 && !work) || !aligned16(work)) return operator_fail(GAN_E_ARG, "work is smaller than gan_group_linear_wgrad_bytes, or not 16-byte aligned");
   if (groups == 0) return GAN_OK;
-  const int e = precision == GAN_FP32 ? 4 : 2;
-  const bool va = rows_aligned16(dy, dy_stride, e) && n_out % 8 == 0, vb = rows_aligned16(x, x_stride, e) && n_in % 8 == 0;
-  const LinearArgs q = {dy, x, nullptr, nullptr, dw, offs, dy_stride, x_stride, n_in, 0, (long long)n_in * n_out, groups, (int)rows, n_out, n_in, 0,
-                        (va ? 1 : 0) | (vb ? 2 : 0) | (rows_aligned16(dw, n_in, 4) ? 4 : 0)};
+  const int e = precision == GAN_FP32 ? 4 : 2, parts = rows > 0 ? wgrad_parts(groups, rows, n_in, n_out) : 1;
+  const long long n = (long long)groups * n_in * n_out;
+  const LinearArgs q = {dy, x, nullptr, nullptr, parts > 1 ? work : dw, offs, dy_stride, x_stride, n_in, 0, (long long)n_in * n_out, groups, (int)rows, n_out, n_in, 0, parts, n};
   const hipStream_t st = (hipStream_t)hip_stream;
-  if (precision == GAN_FP32) return launch_any<float>(WGRAD, q, st);
-  return va && vb && short_rows(x_stride, e) && short_rows(dy_stride, e) ? launch_aligned<false, WGRAD, float>(q, st) : launch_any<bf16_t>(WGRAD, q, st);
+  const bool aligned = short_rows(x_stride, e) && short_rows(dy_stride, e) && n_in % 8 == 0 && n_out % 8 == 0 && rows_aligned16(x, x_stride, e) && rows_aligned16(dy, dy_stride, e);
+  const gan_status s = precision == GAN_FP32 ? launch_fp32(WGRAD, q, st) : aligned ? launch_large<ALIGNED, WGRAD, float>(q, st) : launch_large<ANY, WGRAD, float>(q, st);
+  if (s != GAN_OK || parts == 1) return s;
+  hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)std::min(ceil_div(n, 256), 4096ll)), dim3(256), 0, st, (const float*)work, dw, n, parts);
+  return operator_launched();
 }
 
 extern "C" gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scale, const uint8_t* w8, const uint8_t* w_scale, const int32_t* offs, int32_t groups,
@@ -642,9 +1011,9 @@ extern "C" gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scal
   const long long k = padded8(n_in);
   if (!short_rows(k, 1)) return operator_fail(GAN_E_SHAPE, "more than 2^22 inputs in 8 bits");
   if (rows == 0) return GAN_OK;
-  const int e = y_precision == GAN_FP32 ? 4 : 2;
-  const LinearArgs q = {x8, w8, x_scale, w_scale, y, offs, k, k, y_stride, k * n_out, 0, groups, (int)rows, 0, n_out, (int)k,
-                        rows_aligned16(y, y_stride, e) ? 7 : 3};
+  const LinearArgs q = {x8, w8, x_scale, w_scale, y, offs, k, k, y_stride, k * n_out, 0, groups, (int)rows, 0, n_out, (int)k, 1, 0};
   const hipStream_t st = (hipStream_t)hip_stream;
-  return y_precision == GAN_FP32 ? launch_aligned<true, FORWARD, float>(q, st) : launch_aligned<true, FORWARD, bf16_t>(q, st);
+  if (const int few = few_rows(q, FORWARD, 1))
+    return y_precision == GAN_FP32 ? launch_few<uint8_t, false, float>(q, few, st) : launch_few<uint8_t, false, bf16_t>(q, few, st);
+  return y_precision == GAN_FP32 ? launch_large<EIGHT_BITS, FORWARD, float>(q, st) : launch_large<EIGHT_BITS, FORWARD, bf16_t>(q, st);
 }

@@ -12,43 +12,67 @@ gan_status operator_launched();                                   // GAN_OK, or 
 constexpr int BLOCK8 = 128;                                       // neighbours that share a scale
 __host__ __device__ inline long long padded8(long long cols) { return (cols + BLOCK8 - 1) / BLOCK8 * BLOCK8; }
 
-// Eight neighbouring elements as fp32, from 16-byte aligned memory (VEC), or one by one where fewer than eight are left or the
-// memory is not aligned; what is missing is zero.
+// Eight neighbouring elements as fp32, from 16-byte aligned memory (VEC, where none or all eight are left) or any; one by one
+// where fewer than eight are left.  What is missing is zero.
+template <int ALIGN> struct Words;
+template <> struct Words<16> { typedef unsigned T __attribute__((ext_vector_type(4))); };
+template <> struct Words<4> { typedef unsigned T __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Words<2> { typedef unsigned T __attribute__((ext_vector_type(4), aligned(2))); };
+
+template <typename T, int ALIGN>
+__device__ __forceinline__ void load_whole8(const T* p, float (&v)[8]) {
+  typedef typename Words<ALIGN>::T words;
+  const words a = reinterpret_cast<const words*>(p)[0];
+  if constexpr (sizeof(T) == 4) {
+    const words b = *reinterpret_cast<const words*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = __uint_as_float(a[i]);
+      v[4 + i] = __uint_as_float(b[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(a[i] << 16);
+      v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+    }
+  }
+}
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
   if constexpr (VEC) {
     if (left <= 0) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    } else if constexpr (sizeof(T) == 4) {
-      const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     } else {
-      const uint4 a = *reinterpret_cast<const uint4*>(p);
-      const unsigned w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
+      load_whole8<T, 16>(p, v);
     }
   } else {
+    if (left >= 8) {
+      load_whole8<T, sizeof(T)>(p, v);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.f;
+      for (int i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.f;
+    }
   }
 }
 
+template <typename T, int ALIGN>
+__device__ __forceinline__ void store_whole8(T* p, const float (&v)[8]) {
+  typedef typename Words<ALIGN>::T words;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<words*>(p) = words{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    *reinterpret_cast<words*>(p + 4) = words{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+  } else {
+    *reinterpret_cast<words*>(p) = words{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+  }
+}
 template <typename T, bool VEC>
 __device__ __forceinline__ void store8(T* p, int left, const float (&v)[8]) {
   if constexpr (VEC) {
-    if (left <= 0) return;
-    if constexpr (sizeof(T) == 4) {
-      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      *reinterpret_cast<uint4*>(p) = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
-    }
+    if (left > 0) store_whole8<T, 16>(p, v);
+  } else if (left >= 8) {
+    store_whole8<T, sizeof(T)>(p, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
