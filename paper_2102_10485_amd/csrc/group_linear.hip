@@ -437,14 +437,14 @@ template <bool KMAJOR, int R, int NW> struct Operand<ANY, KMAJOR, R, NW> { typed
 template <int R, int NW> struct Operand<EIGHT_BITS, true, R, NW> { typedef Converted<R, NW> type; };
 
 // One tile of expert `group` (q.groups: of none): rows m0 .. m_end - 1, columns n0 .., sum indices k_begin .. k_end - 1.
-template <Form F, int KIND, int BM, int BN, int WM, int WN, typename C>
+template <Form F, int KIND, int BM, int BN, int WM, int WN, int S, typename C>
 __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char* lds, int group, int part, int m0, int m_end, int n0, int k_begin, int k_end) {
   constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   constexpr bool EIGHT = F == EIGHT_BITS;
   typedef typename Operand<F, KIND != WGRAD, BM, NW>::type CA;
   typedef typename Operand<F, KIND == FORWARD, BN, NW>::type CB;
   typedef typename CA::T T;
-  constexpr int STAGE = CA::BYTES + CB::BYTES;                    // two of them
+  constexpr int STAGE = CA::BYTES + CB::BYTES;                    // S of them
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   const int steps = (k_end - k_begin + STEP - 1) / STEP;
@@ -471,8 +471,8 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
     };
 
     // Half a step is multiplied while the operands of the next half are read from LDS, so that the matrix pipe sees no wait: the second half's during the
-    // first, and during the second those of the next step, whose copies have then had a whole step to arrive.  The barrier between the halves
-    // says that they have, and that no wave reads this step's stage any more, which the copies of the step after the next overwrite.
+    // first, and during the second those of the next step, whose copies have then had S - 1 steps to arrive.  The barrier between the halves
+    // says that they have, and that no wave reads this step's stage any more, which the copies of step s + S overwrite.
     struct Operands { u32x4 a[TM], b[TN]; };
     Operands f0, f1;
     auto read_piece = [&](Operands& f, int p, int stage, int h) {
@@ -481,13 +481,13 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
       else f.a[p - TN] = CA::read(at, wm + (p - TN) * 16, h);
     };
     constexpr int SLOTS = TM > 2 ? TM - 1 : TM;                   // rows of products that reads and copies are issued between
-    // products of `f`; meanwhile the operands `next` of half h of `stage`, and (COPY) the copies of another step into the other stage
-    auto half_step = [&](const Operands& f, Operands& next, int stage, int h, auto copy) {
+    // products of `f`; meanwhile the operands `next` of half h of `stage`, and (copy) the copies of another step into `into`
+    auto half_step = [&](const Operands& f, Operands& next, int stage, int h, auto copy, int into) {
       static_for<0, TM>([&](auto iv) {
         constexpr int i = iv.value;
         static_for<i * (TM + TN) / SLOTS, (i + 1) * (TM + TN) / SLOTS>([&](auto p) { if constexpr (p.value < TM + TN) read_piece(next, p.value, stage, h); });
         if constexpr (copy.value)
-          static_for<i * PIECES / SLOTS, (i + 1) * PIECES / SLOTS>([&](auto p) { if constexpr (p.value < PIECES) copy_piece(p.value, stage ^ 1); });
+          static_for<i * PIECES / SLOTS, (i + 1) * PIECES / SLOTS>([&](auto p) { if constexpr (p.value < PIECES) copy_piece(p.value, into); });
 #pragma unroll
         for (int j = 0; j < TN; ++j) mma(acc[i][j], f.b[j], f.a[i]);
         __builtin_amdgcn_sched_barrier(0);
@@ -495,26 +495,28 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
     };
 
     // (Copies behind the last step ask for nothing and fill the stage with zeros; its operands are read and not multiplied.)
+    static_assert(CA::COPIES || S == 2, "operands that go through registers are a step ahead");
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < S; ++s) {
       ca.next_step();
       cb.next_step();
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) copy_piece(p, s);
       left -= STEP;
     }
-    if constexpr (CA::COPIES) wait_vm<0>();
+    if constexpr (CA::COPIES) wait_vm<(S - 1) * PIECES>();
     __syncthreads();
     static_for<0, TM + TN>([&](auto p) { read_piece(f0, p.value, 0, 0); });
-    for (int s = 0; s < steps; ++s) {
-      const int stage = s & 1;
-      half_step(f0, f1, stage, 1, std::false_type());
-      if constexpr (CA::COPIES) wait_vm<0>();
+    for (int s = 0, stage = 0; s < steps; ++s) {
+      const int next = stage + 1 < S ? stage + 1 : 0;
+      half_step(f0, f1, stage, 1, std::false_type(), 0);
+      if constexpr (CA::COPIES) wait_vm<(S - 2) * PIECES>();
       __syncthreads();
       ca.next_step();
       cb.next_step();
-      half_step(f1, f0, stage ^ 1, 0, std::true_type());
+      half_step(f1, f0, next, 0, std::true_type(), stage);
       left -= STEP;
+      stage = next;
     }
     if constexpr (CA::COPIES) wait_vm<0>();
     __syncthreads();                                              // nothing is written to LDS any more, or read
@@ -554,6 +556,18 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
   }
 }
 
+// Stages of a tile: what LDS holds of them where a block has a CU for itself (tiles of 256 columns), or two blocks share one.
+constexpr int stages(Form f, int height, int width) {
+  const int most = (width == 256 ? 160 : 80) * 1024 / ((height + width) * 128);
+  return f != ALIGNED || most < 2 ? 2 : most > 4 ? 4 : most;
+}
+constexpr int lds_bytes(Form f, int height, int width) {
+  int most = 0;
+  for (int h = height; h >= height / 4; h /= 2)
+    if (stages(f, h, width) * (h + width) * 128 > most) most = stages(f, h, width) * (h + width) * 128;
+  return most;
+}
+
 // Rows of tiles in bands of 8, columns by 4 within a band: 32 tiles in a row, which the CUs of one XCD work on together, then read 8 + 4
 // panels through its L2 in place of 64.
 __device__ __forceinline__ void banded(unsigned id, unsigned row_tiles, unsigned col_tiles, unsigned& r, unsigned& c) {
@@ -563,30 +577,42 @@ __device__ __forceinline__ void banded(unsigned id, unsigned row_tiles, unsigned
   c = four * 4 + in_four / high;
 }
 
-// Forward and dgrad.  Block b runs on XCD b % 8: each XCD takes one stretch of the whole tiles, then its share of the experts' shorter last ones, in
-// half the height where that is enough.
+// Forward and dgrad.  Block b runs on XCD b % 8.  Each XCD takes one stretch of the tiles of full height (the whole ones, then experts' last ones of more than half
+// of it), then its share of the last ones that half the height is enough for, then of those for a quarter, so that the shortest blocks end the launch.
 template <Form F, int KIND, int BM, int BN, int WM, int WN, typename C>
 __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearArgs q) {
   extern __shared__ __align__(1024) unsigned char lds[];
-  unsigned whole, ends;
-  count_tiles(q.offs, q.groups, q.rows, BM, whole, ends);
-  const unsigned cols = (unsigned)(q.n + BN - 1) / BN, xcd = blockIdx.x & 7, i = blockIdx.x >> 3, share = (whole * cols + 7) / 8;
-  int group, m0, m_end;
+  unsigned count[SORTS];
+  count_tiles(q.offs, q.groups, q.rows, BM, count);
+  const unsigned cols = (unsigned)(q.n + BN - 1) / BN, xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
+  const unsigned full = (count[WHOLE] + count[HIGH]) * cols, share = (full + 7) / 8;
+  unsigned r, c, id = i < share ? xcd * share + i : (i - share) * 8 + xcd;
+  int sort;
   if (i < share) {
-    const unsigned id = xcd * share + i;
-    if (id >= whole * cols) return;
-    unsigned r, c;
-    banded(id, whole, cols, r, c);
-    find_tile_of<false>(q.offs, q.groups, q.rows, BM, r, group, m0, m_end);
-    tile_product<F, KIND, BM, BN, WM, WN, C>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, group < q.groups ? q.k : 0);
+    if (id >= full) return;
+    sort = id < count[WHOLE] * cols ? WHOLE : HIGH;
+    if (sort == HIGH) id -= count[WHOLE] * cols;
   } else {
-    const unsigned id = (i - share) * 8 + xcd;
-    if (id >= ends * cols) return;
-    find_tile_of<true>(q.offs, q.groups, q.rows, BM, id / cols, group, m0, m_end);
-    const int n0 = (int)(id % cols) * BN, k = group < q.groups ? q.k : 0;
-    if (m_end - m0 > BM / 2) tile_product<F, KIND, BM, BN, WM, WN, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
-    else tile_product<F, KIND, BM / 2, BN, WM, WN, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
+    sort = id < count[HALF] * cols ? HALF : LOW;
+    if (sort == LOW) id -= count[HALF] * cols;
+    if (id >= count[sort] * cols) return;
   }
+  if (sort == WHOLE) {
+    banded(id, count[WHOLE], cols, r, c);
+  } else {
+    r = id / cols;
+    c = id % cols;
+  }
+  int group, m0, m_end;
+  find_tile_of(sort, q.offs, q.groups, q.rows, BM, r, group, m0, m_end);
+  const int n0 = (int)c * BN, k = group < q.groups ? q.k : 0;
+  if (sort == WHOLE) m_end = min(m_end, m0 + BM);
+  if (sort <= HIGH)
+    tile_product<F, KIND, BM, BN, WM, WN, stages(F, BM, BN), C>(q, lds, group, 0, m0, m_end, n0, 0, k);
+  else if (F == EIGHT_BITS || sort == HALF)                       // (8-bit codes are loaded for 128 rows at least, by 512 threads)
+    tile_product<F, KIND, BM / 2, BN, WM, WN, stages(F, BM / 2, BN), C>(q, lds, group, 0, m0, m_end, n0, 0, k);
+  else if constexpr (F != EIGHT_BITS)
+    tile_product<F, KIND, BM / 4, BN, WM, WN, stages(F, BM / 4, BN), C>(q, lds, group, 0, m0, m_end, n0, 0, k);
 }
 
 template <Form F, int BM, int BN, int WM, int WN>
@@ -596,7 +622,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_wgrad_kernel(LinearArgs q
   int begin, end;
   group_rows(q.offs, q.groups, q.rows, group, begin, end);
   part_of(part, q.parts, begin, end);
-  tile_product<F, WGRAD, BM, BN, WM, WN, float>(q, lds, group, part, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
+  tile_product<F, WGRAD, BM, BN, WM, WN, stages(F, BM, BN), float>(q, lds, group, part, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
 }
 
 // dw = the parts, added in order
@@ -878,10 +904,10 @@ long long wgrad_tiles(long long groups, long long m, long long n, int side) { re
 
 template <Form F, int KIND, int BM, int BN, int WM, int WN, typename C>
 gan_status launch_tiles(const LinearArgs& q, hipStream_t st) {
-  constexpr int LDS = 2 * (BM + BN) * 128;
+  constexpr int LDS = KIND == WGRAD ? stages(F, BM, BN) * (BM + BN) * 128 : lds_bytes(F, BM, BN);
   if constexpr (KIND == WGRAD)
     return launch(linear_wgrad_kernel<F, BM, BN, WM, WN>, q.parts * wgrad_tiles(q.groups, q.m, q.n, BM), 64 * WM * WN, LDS, q, st);
-  else    // (whole tiles and ends are each shared among the eight XCDs)
+  else    // (full tiles and lower ones are each shared among the eight XCDs)
     return launch(linear_kernel<F, KIND, BM, BN, WM, WN, C>, 8 * (ceil_div(most_tiles(q.rows, q.groups, BM) * ceil_div(q.n, BN), 8) + 1), 64 * WM * WN, LDS, q, st);
 }
 // 256 x 256 tiles where they fill the CUs, 128 x 128 where not

@@ -54,33 +54,40 @@ __device__ __forceinline__ bool find_tile(const int* offs, int groups, int rows,
   return false;
 }
 
-// How many tiles of `height` rows there are: whole ones, and shorter ones at the experts' ends.  All 64 lanes of a wave call it.
-__device__ __forceinline__ void count_tiles(const int* offs, int groups, int rows, int height, unsigned& whole, unsigned& ends) {
+// Tiles of `height` rows: whole ones, and each expert's shorter last one: of more than height / 2 rows (HIGH), more than height / 4 (HALF), or fewer.
+enum TileSort { WHOLE, HIGH, HALF, LOW, SORTS };
+
+__device__ __forceinline__ unsigned tiles_of(int sort, unsigned rows, unsigned height) {
+  const unsigned rest = rows % height;
+  return sort == WHOLE ? rows / height : sort == HIGH ? rest > height / 2 : sort == HALF ? rest > height / 4 && rest <= height / 2 : rest > 0 && rest <= height / 4;
+}
+
+// How many of each there are.  All 64 lanes of a wave call it.
+__device__ __forceinline__ void count_tiles(const int* offs, int groups, int rows, int height, unsigned (&count)[SORTS]) {
   const int l = threadIdx.x & 63;
   int done = 0;
-  unsigned w = 0, e = 0;                                          // this lane's
+#pragma unroll
+  for (int s = 0; s < SORTS; ++s) count[s] = 0;                   // (this lane's)
   for (int g0 = 0; g0 <= groups; g0 += 64) {
     const int g = g0 + l;
     int hi = g < groups ? min(max(offs[g + 1], 0), rows) : rows;
     hi = max(wave_scan_max(hi), done);
     int lo = __shfl_up(hi, 1);
     if (l == 0) lo = done;
-    w += (unsigned)(hi - lo) / height;
-    e += (unsigned)(hi - lo) % height != 0;
+#pragma unroll
+    for (int s = 0; s < SORTS; ++s) count[s] += tiles_of(s, (unsigned)(hi - lo), height);
     done = __shfl(hi, 63);
   }
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    w += (unsigned)__shfl_xor((int)w, d);
-    e += (unsigned)__shfl_xor((int)e, d);
-  }
-  whole = (unsigned)__builtin_amdgcn_readfirstlane((int)w);
-  ends = (unsigned)__builtin_amdgcn_readfirstlane((int)e);
+  for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+    for (int s = 0; s < SORTS; ++s) count[s] += (unsigned)__shfl_xor((int)count[s], d);
+#pragma unroll
+  for (int s = 0; s < SORTS; ++s) count[s] = (unsigned)__builtin_amdgcn_readfirstlane((int)count[s]);
 }
 
-// The t-th whole tile (END: the t-th shorter one) of those: its expert (`groups`: rows of none), its first row, and the end of the expert's rows.
-template <bool END>
-__device__ __forceinline__ void find_tile_of(const int* offs, int groups, int rows, int height, unsigned t, int& group, int& row, int& end) {
+// The t-th tile of a sort: its expert (`groups`: rows of none), its first row, and the end of the expert's rows.
+__device__ __forceinline__ void find_tile_of(int sort, const int* offs, int groups, int rows, int height, unsigned t, int& group, int& row, int& end) {
   const int l = threadIdx.x & 63;
   int done = 0;
   unsigned before = 0;
@@ -90,12 +97,12 @@ __device__ __forceinline__ void find_tile_of(const int* offs, int groups, int ro
     hi = max(wave_scan_max(hi), done);
     int lo = __shfl_up(hi, 1);
     if (l == 0) lo = done;
-    const unsigned whole = (unsigned)(hi - lo) / height, tiles = END ? (unsigned)(hi - lo) % height != 0 : whole;
+    const unsigned n = (unsigned)(hi - lo), tiles = tiles_of(sort, n, height);
     const unsigned upto = before + (unsigned)wave_scan_add((int)tiles);
     const unsigned long long past = __ballot(upto > t);
     if (past) {
       const int src = __ffsll((unsigned long long)past) - 1;
-      const unsigned at = END ? whole : t - (upto - tiles);
+      const unsigned at = sort == WHOLE ? t - (upto - tiles) : n / height;
       group = __builtin_amdgcn_readfirstlane(g0 + src);
       row = __builtin_amdgcn_readfirstlane(__shfl(lo + (int)at * height, src));
       end = __builtin_amdgcn_readfirstlane(__shfl(hi, src));
