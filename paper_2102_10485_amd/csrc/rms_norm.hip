@@ -135,11 +135,14 @@ void launch_norm(const NormArgs& a, hipStream_t st) {
   const long long cols = a.cols;
   const unsigned rows = (unsigned)a.rows, by4 = (unsigned)((a.rows + 3) / 4);
 #define GAN_NORM(W, C) hipLaunchKernelGGL((norm_kernel<T, W, C, VEC>), dim3(W == 1 ? by4 : rows), dim3(W == 1 ? 256 : 64 * W), 0, st, a)
+  // Times on an MI355X.  Up to 1024 elements a wave per row has no barrier (bf16, 6400 x 1024: 13.5 us, four waves a row 15.6), but few rows
+  // are done sooner by more waves (fp32, 1117 x 1000: 6.4 and 6.0).  Above, one chunk a lane is faster than more of them in fewer waves (bf16, 6400 x 2048: 22.8 us by four
+  // waves, 28.7 by one; 4096 x 8192: 48.6 by sixteen, 52.9 by four).
   if (cols <= 512) GAN_NORM(1, 1);
-  else if (cols <= 1024) GAN_NORM(1, 2);
-  else if (cols <= 2048) GAN_NORM(1, 4);
+  else if (cols <= 1024 && a.rows >= 4096) GAN_NORM(1, 2);
+  else if (cols <= 2048) GAN_NORM(4, 1);
   else if (cols <= 4096) GAN_NORM(4, 2);
-  else if (cols <= 8192) GAN_NORM(4, 4);
+  else if (cols <= 8192) GAN_NORM(16, 1);
   else if (cols <= 16384) GAN_NORM(16, 2);
   else if (cols <= 32768) GAN_NORM(16, 4);
   else hipLaunchKernelGGL((norm_long_kernel<T, VEC>), dim3(rows), dim3(1024), 0, st, a);
@@ -157,8 +160,33 @@ struct NormBackArgs {
   int cols;
 };
 
-// A row's share of the gain's gradient stays in its lanes' registers over all rows of the wave; four waves of one row each are joined
-// at the end.
+// What a lane holds of a row as it is stored: eight elements.
+template <typename T> struct Raw { uint4 v[sizeof(T) / 2]; };
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw<T> load_raw(const T* p, int left) {
+  Raw<T> r;
+  if (left >= 8) {
+    typedef typename Words<VEC ? 16 : sizeof(T)>::T words;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = __builtin_bit_cast(uint4, reinterpret_cast<const words*>(p)[i]);
+  } else {
+    T e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = !VEC && i < left ? p[i] : from_float<T>(0.f);
+    __builtin_memcpy(&r, e, sizeof(r));
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const Raw<T>& r, float (&v)[E]) {
+  T e[8];
+  __builtin_memcpy(e, &r, sizeof(r));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = to_float(e[i]);
+}
+
+// A row's share of the gain's gradient stays in its lanes' registers over all rows of the wave, and the next row is loaded while this one is worked on (both launches of 6400 x 2048 in bf16: 47.9 -> 28.8 us); four
+// waves of one row each are joined at the end.
 template <typename T, int WAVES, int CHUNKS, bool VEC>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_back_kernel(NormBackArgs a) {
   __shared__ float scratch[WAVES == 1 ? 4 * 64 * E : WAVES];
@@ -170,40 +198,46 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_back_kerne
   for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
     for (int i = 0; i < E; ++i) dg[c][i] = 0.f;
-  for (long long row = WAVES == 1 ? (long long)blockIdx.x * 4 + wave : blockIdx.x; row < a.rows; row += step) {
-    const float inv = a.inv_rms[row];
-    float s[CHUNKS][E], h[CHUNKS][E], dot = 0.f;
+  struct Row { Raw<T> dy[CHUNKS], s[CHUNKS], ds[CHUNKS]; float inv; } next;
+  auto load_row = [&](long long row) {
+    next.inv = a.inv_rms[row];
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-      const int col = (c * 64 * WAVES + lane) * E;
-      load8<T, VEC>((const T*)a.dy + row * a.dy_stride + col, a.cols - col, h[c]);
-      load8<T, VEC>((const T*)a.sum + row * a.sum_stride + col, a.cols - col, s[c]);
+      const int col = (c * 64 * WAVES + lane) * E, left = a.cols - col;
+      next.dy[c] = load_raw<T, VEC>((const T*)a.dy + row * a.dy_stride + col, left);
+      next.s[c] = load_raw<T, VEC>((const T*)a.sum + row * a.sum_stride + col, left);
+      next.ds[c] = load_raw<T, VEC>((const T*)a.dsum + row * a.dsum_stride + col, a.dsum ? left : 0);
     }
+  };
+  long long row = WAVES == 1 ? (long long)blockIdx.x * 4 + wave : blockIdx.x;
+  if (row < a.rows) load_row(row);
+  for (; row < a.rows; row += step) {
+    if (WAVES == 16 && row >= gridDim.x) load_row(row);           // (no registers for two rows)
+    const Row now = next;
+    if (WAVES < 16 && row + step < a.rows) load_row(row + step);
+    float s[CHUNKS][E], h[CHUNKS][E], dot = 0.f;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
       const int col = (c * 64 * WAVES + lane) * E;
       float g[E];
       load8<float, VEC>(a.gain + col, a.cols - col, g);
+      unpack<T>(now.dy[c], h[c]);
+      unpack<T>(now.s[c], s[c]);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        dg[c][i] += h[c][i] * (s[c][i] * inv);
+        dg[c][i] += h[c][i] * (s[c][i] * now.inv);
         h[c][i] *= g[i];
         dot += h[c][i] * s[c][i];
       }
     }
-    const float k = inv * inv * (row_total<WAVES>(dot, scratch) / (float)a.cols);
+    const float k = now.inv * now.inv * (row_total<WAVES>(dot, scratch) / (float)a.cols);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
       const int col = (c * 64 * WAVES + lane) * E;
       float d[E];
-      if (a.dsum) {
-        load8<T, VEC>((const T*)a.dsum + row * a.dsum_stride + col, a.cols - col, d);
-      } else {
+      unpack<T>(now.ds[c], d);
 #pragma unroll
-        for (int i = 0; i < E; ++i) d[i] = 0.f;
-      }
-#pragma unroll
-      for (int i = 0; i < E; ++i) d[i] += inv * (h[c][i] - s[c][i] * k);
+      for (int i = 0; i < E; ++i) d[i] += now.inv * (h[c][i] - s[c][i] * k);
       store8<T, VEC>((T*)a.dx + row * a.dx_stride + col, a.cols - col, d);
     }
   }
@@ -270,13 +304,19 @@ __global__ __launch_bounds__(256) void gain_long_kernel(NormBackArgs a) {
   a.partial[(long long)blockIdx.y * a.cols + col] = d;
 }
 
-// dgain[c] = the blocks' partial sums, added in 32 chains that are joined in order
+// dgain[c] = the blocks' partial sums, added in 32 chains that are joined in order; eight loads of a chain in flight
 __global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, float* dgain, int blocks, int cols) {
   __shared__ float part[32][33];
   const int c = threadIdx.x & 31, k = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
   float d = 0.f;
   if (col < cols)
-    for (int b = k; b < blocks; b += 32) d += partial[(long long)b * cols + col];
+    for (int b = k; b < blocks; b += 256) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = b + 32 * i < blocks ? partial[(long long)(b + 32 * i) * cols + col] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d += v[i];
+    }
   part[k][c] = d;
   __syncthreads();
   if (k == 0 && col < cols) {
@@ -288,10 +328,11 @@ __global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, fl
 
 constexpr int REGISTER_COLS = 16384;                              // rows that norm_back_kernel holds
 
-// Blocks of the gradient: each leaves a row of partial sums.
+// Blocks of the gradient: each leaves a row of partial sums, which twice as many would make slower to add than they gain (bf16, 16384 x 4096: 98 us with 512
+// blocks, 109 with 1024).
 int back_blocks(long long rows, int cols) {
   if (cols > REGISTER_COLS) return (int)(rows < 64 ? rows : 64);
-  const long long per = cols <= 2048 ? 4 : 1, blocks = (rows + per - 1) / per, most = cols <= 8192 ? 1024 : 256;
+  const long long per = cols <= 1024 ? 4 : 1, blocks = (rows + per - 1) / per, most = cols > 1024 && cols <= 2048 ? 1024 : cols <= 8192 ? 512 : 256;
   return (int)(blocks < most ? blocks : most);
 }
 
@@ -299,9 +340,10 @@ template <typename T, bool VEC>
 void launch_back(const NormBackArgs& a, hipStream_t st) {
   const unsigned blocks = (unsigned)back_blocks(a.rows, a.cols);
 #define GAN_BACK(W, C) hipLaunchKernelGGL((norm_back_kernel<T, W, C, VEC>), dim3(blocks), dim3(W == 1 ? 256 : 64 * W), 0, st, a)
+  // (bf16, 6400 x 1024: 17.1 us with a wave a row, 20.1 with four; fp32, 4000 x 2048: 32.8 us with four, 36.7 with one)
   if (a.cols <= 512) GAN_BACK(1, 1);
   else if (a.cols <= 1024) GAN_BACK(1, 2);
-  else if (a.cols <= 2048) GAN_BACK(1, 4);
+  else if (a.cols <= 2048) GAN_BACK(4, 1);
   else if (a.cols <= 4096) GAN_BACK(4, 2);
   else if (a.cols <= 8192) GAN_BACK(4, 4);
   else if (a.cols <= REGISTER_COLS) GAN_BACK(16, 2);
