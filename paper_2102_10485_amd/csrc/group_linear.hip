@@ -120,6 +120,42 @@ __device__ __forceinline__ void part_of(int part, int parts, int& begin, int& en
   end = min(end - begin, each) + begin;
 }
 
+// A wave's outputs, rows m .. (of m_end) and columns n .. (of n_end), as MFMAs with the columns first leave them.  Sixteen rows at a time go through LDS (the wave's
+// own), so that its lanes store whole rows, 16 bytes each: 64 lanes with four columns each of sixteen rows would write 32 or 64 bytes of a row at a time (the weight
+// gradient of a hundred experts of 1024 x 1024: 173 us, 125 by rows).
+template <typename C, int TM, int TN>
+__device__ __forceinline__ void store_rows(const floatx4 (&acc)[TM][TN], C* c, long long stride, unsigned char* lds, int m0, int m_end, int n0, int n_end) {
+  constexpr int WIDE = TN * 16 * (int)sizeof(C), LANES = WIDE / 16, EACH = 16 / (int)sizeof(C);
+  static_assert(64 % LANES == 0, "whole rows");
+  typedef typename Words<sizeof(C)>::T words;
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    if (m0 + i * 16 >= m_end) break;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      unsigned char* at = lds + (l & 15) * (WIDE + 16) + (j * 16 + (l >> 4) * 4) * (int)sizeof(C);
+      if constexpr (sizeof(C) == 4) *reinterpret_cast<floatx4*>(at) = acc[i][j];
+      else *reinterpret_cast<uint2*>(at) = make_uint2(pack2_bf16(acc[i][j][0], acc[i][j][1]), pack2_bf16(acc[i][j][2], acc[i][j][3]));
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int r = l / LANES; r < 16; r += 64 / LANES) {
+      const int m = m0 + i * 16 + r, n = n0 + l % LANES * EACH;
+      const unsigned char* from = lds + r * (WIDE + 16) + l % LANES * 16;
+      const uint4 v = *reinterpret_cast<const uint4*>(from);
+      if (m >= m_end || n >= n_end) continue;
+      C* at = c + (long long)m * stride + n;
+      if (n + EACH <= n_end) {
+        *reinterpret_cast<words*>(at) = words{v.x, v.y, v.z, v.w};
+      } else {
+        for (int k = 0; k < n_end - n; ++k) at[k] = reinterpret_cast<const C*>(from)[k];
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 template <int KIND>
 __global__ __launch_bounds__(256, 2) void linear_fp32_kernel(LinearArgs q) {
   typedef Staged<KIND != WGRAD> SA;
@@ -198,30 +234,26 @@ __global__ __launch_bounds__(256, 2) void linear_fp32_kernel(LinearArgs q) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) again |= !finite_bits(__float_as_uint(acc[i][j][e]) & 0x7fffffffu);
     }
+  if (again) {                                                    // this lane's outputs as chains of fp32 multiply-adds
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + wm + i * 16 + (l & 15);
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + wn + j * 16 + (l >> 4) * 4;
-      if (m >= m_end || n >= q.n) continue;
-      float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-      if (again) {                                                // this lane's outputs as chains of fp32 multiply-adds
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (n + e >= q.n) continue;
+          const int m = m0 + wm + i * 16 + (l & 15), n = n0 + wn + j * 16 + (l >> 4) * 4 + e;
+          if (m >= m_end || n >= q.n) continue;
           float sum = 0.f;
           for (int k = k_begin; k < k_end; ++k) {
             const float x = KIND == WGRAD ? a[(long long)k * q.a_stride + m] : a[(long long)m * q.a_stride + k];
-            const float y = KIND == FORWARD ? b[(long long)(n + e) * q.b_stride + k] : b[(long long)k * q.b_stride + n + e];
+            const float y = KIND == FORWARD ? b[(long long)n * q.b_stride + k] : b[(long long)k * q.b_stride + n];
             sum = fmaf(x, y, sum);
           }
-          v[e] = sum;
+          acc[i][j][e] = sum;
         }
-      }
-      store_four<float>(c + (long long)m * q.c_stride + n, q.n - n, v);
-    }
   }
+  __syncthreads();
+  store_rows<float, 4, 4>(acc, c, q.c_stride, lds + wave * 16 * (64 * 4 + 16), m0 + wm, m_end, n0 + wn, q.n);
 }
 
 // ---- bf16 and 8 bits ----
@@ -445,7 +477,7 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
   typedef typename Operand<F, KIND == FORWARD, BN, NW>::type CB;
   typedef typename CA::T T;
   constexpr int STAGE = CA::BYTES + CB::BYTES;                    // S of them
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   const int steps = (k_end - k_begin + STEP - 1) / STEP;
   int left = k_end - k_begin;
@@ -522,38 +554,9 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
     __syncthreads();                                              // nothing is written to LDS any more, or read
   }
 
-  // Sixteen rows of a wave's columns at a time go through LDS, so that its lanes store whole rows, 16 bytes each: 64 lanes with four columns each of
-  // sixteen rows would write 32 or 64 bytes of a row at a time, at 2.5 TB/s.
   C* c = (C*)q.c + (KIND == WGRAD ? part * q.part + (long long)group * q.c_group : 0);
-  constexpr int WIDE = TN * 16 * (int)sizeof(C), LANES = WIDE / 16, EACH = 16 / (int)sizeof(C);
-  unsigned char* out = lds + wave * 16 * (WIDE + 16);
-  static_assert(NW * 16 * (WIDE + 16) <= 2 * STAGE && 64 % LANES == 0, "the outputs' LDS");
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    if (m0 + wm + i * 16 >= m_end) break;
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-      unsigned char* at = out + (l & 15) * (WIDE + 16) + (j * 16 + (l >> 4) * 4) * (int)sizeof(C);
-      if constexpr (sizeof(C) == 4) *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
-      else *reinterpret_cast<uint2*>(at) = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
-    }
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int r = l / LANES; r < 16; r += 64 / LANES) {
-      const int m = m0 + wm + i * 16 + r, n = n0 + wn + l % LANES * EACH;
-      const uint4 v = *reinterpret_cast<const uint4*>(out + r * (WIDE + 16) + l % LANES * 16);
-      if (m >= m_end || n >= q.n) continue;
-      C* at = c + (long long)m * q.c_stride + n;
-      if (n + EACH <= q.n) {
-        *reinterpret_cast<typename Words<sizeof(C)>::T*>(at) = typename Words<sizeof(C)>::T{v.x, v.y, v.z, v.w};
-      } else {
-        const C* e = reinterpret_cast<const C*>(out + r * (WIDE + 16) + l % LANES * 16);
-        for (int k = 0; k < q.n - n; ++k) at[k] = e[k];
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
+  static_assert(NW * 16 * (TN * 16 * (int)sizeof(C) + 16) <= 2 * STAGE, "the outputs' LDS");
+  store_rows<C, TM, TN>(acc, c, q.c_stride, lds + wave * 16 * (TN * 16 * (int)sizeof(C) + 16), m0 + wm, m_end, n0 + wn, q.n);
 }
 
 // Stages of a tile: what LDS holds of them where a block has a CU for itself (tiles of 256 columns), or two blocks share one.
@@ -698,7 +701,8 @@ __device__ __forceinline__ void join_waves(const floatx4 (&acc)[Q], F&& write) {
 template <typename T, int TM, int JT, int U, int NW, bool ANY_ROWS, typename C>
 __global__ __launch_bounds__(64 * NW) void linear_few_kernel(LinearArgs q) {
   constexpr int EACH = Few<T>::EACH, DEEP = Few<T>::DEEP, ES = (int)sizeof(T);
-  const int cols = (q.n + 16 * JT - 1) / (16 * JT), n0 = (int)(blockIdx.x % cols) * 16 * JT;
+  const int cols = (q.n + 16 * JT - 1) / (16 * JT);
+  const int column = (int)(blockIdx.x % cols), n0 = column * 16 * JT;
   int group, m0, m_end;
   if (!find_tile(q.offs, q.groups, q.rows, 16 * TM, blockIdx.x / cols, group, m0, m_end)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
@@ -719,7 +723,7 @@ __global__ __launch_bounds__(64 * NW) void linear_few_kernel(LinearArgs q) {
 #pragma unroll
     for (int j = 0; j < JT; ++j) wo[j] = (unsigned)((j * 16 + (l & 15)) * q.b_stride * ES);
     // Neighbouring tiles of columns start at different places of the sum: with rows of 8 KiB all of them would ask the same few memory channels at a time.
-    const int turns = (q.k + NW * DEEP * U - 1) / (NW * DEEP * U), start = (int)(blockIdx.x % cols) % turns;
+    const int turns = (q.k + NW * DEEP * U - 1) / (NW * DEEP * U), start = column % turns;
     for (int turn = 0; turn < turns; ++turn) {
       const int k0 = ((turn + start < turns ? turn + start : turn + start - turns) * NW + wave) * DEEP * U;
       u32x4 fx[U][TM], fw[U][JT];
@@ -803,7 +807,8 @@ __global__ __launch_bounds__(64 * NW) void linear_few_kernel(LinearArgs q) {
 template <typename T, int TM, int U, int NW, bool ANY_ROWS>
 __global__ __launch_bounds__(64 * NW) void linear_few_dgrad_kernel(LinearArgs q) {
   constexpr int EACH = Few<T>::EACH, DEEP = Few<T>::DEEP, ES = (int)sizeof(T), BN = 16 * EACH;
-  const int cols = (q.n + BN - 1) / BN, n0 = (int)(blockIdx.x % cols) * BN;
+  const int cols = (q.n + BN - 1) / BN;
+  const int n0 = (int)(blockIdx.x % cols) * BN;
   int group, m0, m_end;
   if (!find_tile(q.offs, q.groups, q.rows, 16 * TM, blockIdx.x / cols, group, m0, m_end)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
@@ -856,7 +861,7 @@ __global__ __launch_bounds__(64 * NW) void linear_few_dgrad_kernel(LinearArgs q)
                 acc[i * EACH + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fx[u][i][e]), __uint_as_float(fw[u][e][j]), acc[i * EACH + j], 0, 0, 0);
         } else {
 #pragma unroll
-          for (int j = 0; j < EACH; ++j) {                        // column j of the lane's eight: element j of its eight loads
+          for (int j = 0; j < EACH; ++j) {                          // column j of the lane's: element j of its eight loads
             u32x4 b;
 #pragma unroll
             for (int e = 0; e < 4; ++e) b[e] = __builtin_amdgcn_perm(fw[u][2 * e + 1][j / 2], fw[u][2 * e][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
@@ -929,14 +934,14 @@ gan_status launch_few(const LinearArgs& q, int sixteens, hipStream_t st) {
   if (sixteens == 2) return launch_few_as<T, 2, 2, U, ANY_ROWS, C>(q, st);
   return most_groups(q) * ceil_div(q.n, 32) <= 1024 ? launch_few_as<T, 1, 1, U, ANY_ROWS, C>(q, st) : launch_few_as<T, 1, 2, U, ANY_ROWS, C>(q, st);
 }
-template <typename T, int TM, int U, bool ANY_ROWS>
+template <typename T, int TM, int U, int NW, bool ANY_ROWS>
 gan_status launch_few_dgrad_as(const LinearArgs& q, hipStream_t st) {
-  return launch(linear_few_dgrad_kernel<T, TM, U, 8, ANY_ROWS>, most_tiles(q.rows, q.groups, 16 * TM) * ceil_div(q.n, 16 * Few<T>::EACH), 512, 0, q, st);
+  return launch(linear_few_dgrad_kernel<T, TM, U, NW, ANY_ROWS>, most_tiles(q.rows, q.groups, 16 * TM) * ceil_div(q.n, 16 * Few<T>::EACH), 64 * NW, 0, q, st);
 }
 template <typename T, bool ANY_ROWS>
 gan_status launch_few_dgrad(const LinearArgs& q, int sixteens, hipStream_t st) {
-  constexpr int U = sizeof(T) == 4 ? 4 : 2;
-  return sixteens == 2 ? launch_few_dgrad_as<T, 2, U, ANY_ROWS>(q, st) : launch_few_dgrad_as<T, 1, U, ANY_ROWS>(q, st);
+  if constexpr (sizeof(T) == 4) return launch_few_dgrad_as<T, 1, 2, 8, false>(q, st);
+  else return sixteens == 2 ? launch_few_dgrad_as<T, 2, 2, 8, ANY_ROWS>(q, st) : launch_few_dgrad_as<T, 1, 2, 8, ANY_ROWS>(q, st);
 }
 
 // Sixteens of rows for the kernel for few rows, or 0 where tiles are faster.
