@@ -136,3 +136,26 @@ def test_eight_bit_moments_follow_the_32_bit_ones():
     assert abs((root ** 2).mean() / exact - 1) <= 0.125 ** 2 / 4 + 6 * 0.006 * 2
     first = R.decode(m.cpu().numpy().reshape(-1, 128), ms.cpu().numpy()[:, None])
     assert abs(first.mean() / 1e-3 - 1) <= 0.02
+
+
+def test_moments_beyond_2_to_the_32():
+    """A tensor behind one of 2^32 values: its moments' indices, and the bits mixed from them, pass 32 bits."""
+    torch = U.torch_mod()
+    sizes = [1 << 32, 300]
+    p, g = torch.zeros(sizes[0], device="cuda"), torch.zeros(sizes[0], dtype=torch.bfloat16, device="cuda")
+    rng = np.random.default_rng(2)
+    p2, g2 = rng.normal(size=300).astype(np.float32), U.round_to(rng.normal(size=300) * 1e-2, True)
+    tp, tg = torch.from_numpy(p2).cuda(), torch.from_numpy(g2).cuda().bfloat16()
+    blocks = B.adamw_blocks(sizes)
+    m, v = (torch.zeros(blocks * 128, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ms, vs = (torch.zeros(blocks, dtype=torch.uint8, device="cuda") for _ in range(2))
+    plan = B.AdamW(sizes, [p.data_ptr(), tp.data_ptr()], [g.data_ptr(), tg.data_ptr()], B.BF16, None, None, 8, m.data_ptr(), v.data_ptr(), ms.data_ptr(), vs.data_ptr())
+    g[-1] = 1.0
+    plan.step(HYPER["lr"], HYPER["beta1"], HYPER["beta2"], HYPER["eps"], 1, 5)
+    z, zs = np.zeros(384, np.uint8), np.zeros(3, np.uint8)
+    want = R.adamw(p2, g2, z, z, zs, zs, 0.0, step=1, seed=5, eight=True, first=1 << 32, **HYPER)
+    first = 1 << 32
+    assert np.array_equal(tp.cpu().numpy(), want[0])
+    assert np.array_equal(m[first:].cpu().numpy(), want[1]) and np.array_equal(v[first:].cpu().numpy(), want[2])
+    assert np.array_equal(ms[first // 128:].cpu().numpy(), want[3]) and np.array_equal(vs[first // 128:].cpu().numpy(), want[4])
+    assert float(p[-1]) < 0 and not bool(p[-2])                      # only the value that has a gradient moved
