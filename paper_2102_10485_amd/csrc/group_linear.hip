@@ -915,12 +915,14 @@ gan_status launch_tiles(const LinearArgs& q, hipStream_t st) {
   else    // (full tiles and lower ones are each shared among the eight XCDs)
     return launch(linear_kernel<F, KIND, BM, BN, WM, WN, C>, 8 * (ceil_div(most_tiles(q.rows, q.groups, BM) * ceil_div(q.n, BN), 8) + 1), 64 * WM * WN, LDS, q, st);
 }
-// 256 x 256 tiles where they fill the CUs, 128 x 128 where not
+// 256 x 256 tiles where they fill the CUs and experts have more than 32 rows on average, 128 x 128 where not.  Both sides, us on an MI355X from cold memory (256, 128):
+// 32 experts of 128 rows, 2048 -> 2048, forward 77, 97; 64 of 47, 1024 -> 1024, dgrad 31, 34; 128 of 14, 2361 -> 384, 8 bits 59, 43; four of 175, 4096 -> 4096 (64 tiles
+// of 256), forward 100, 67; weight gradient of 64 experts, 2816 -> 512: 109, 138.
 template <Form F, int KIND, typename C>
 gan_status launch_large(const LinearArgs& q, hipStream_t st) {
-  const long long big = KIND == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, 256) : tiles(q, 256, 256);
+  const bool big = KIND == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, 256) >= 256 : tiles(q, 256, 256) >= 256 && q.rows / most_groups(q) > 32;
   if constexpr (F != ANY)
-    if (big >= 256) return launch_tiles<F, KIND, 256, 256, 2, 4, C>(q, st);
+    if (big) return launch_tiles<F, KIND, 256, 256, 2, 4, C>(q, st);
   return launch_tiles<F, KIND, 128, 128, 2, 2, C>(q, st);
 }
 
@@ -932,6 +934,7 @@ template <typename T, bool ANY_ROWS, typename C>
 gan_status launch_few(const LinearArgs& q, int sixteens, hipStream_t st) {
   constexpr int U = sizeof(T) == 1 ? 2 : 4;
   if (sixteens == 2) return launch_few_as<T, 2, 2, U, ANY_ROWS, C>(q, st);
+  // sixteen columns a block where 32 make few blocks: eight rows of eight experts, 4096 -> 4096, 28 us (32 columns: 35); four rows of a hundred, 1024 -> 1024, 47 (36)
   return most_groups(q) * ceil_div(q.n, 32) <= 1024 ? launch_few_as<T, 1, 1, U, ANY_ROWS, C>(q, st) : launch_few_as<T, 1, 2, U, ANY_ROWS, C>(q, st);
 }
 template <typename T, int TM, int U, int NW, bool ANY_ROWS>
@@ -944,7 +947,9 @@ gan_status launch_few_dgrad(const LinearArgs& q, int sixteens, hipStream_t st) {
   else return sixteens == 2 ? launch_few_dgrad_as<T, 2, 2, 8, ANY_ROWS>(q, st) : launch_few_dgrad_as<T, 1, 2, 8, ANY_ROWS>(q, st);
 }
 
-// Sixteens of rows for the kernel for few rows, or 0 where tiles are faster.
+// Sixteens of rows for the kernel for few rows, or 0 where tiles are faster: up to 8 rows an expert, whose weights then are the time (a hundred experts of 4 rows,
+// 1024 -> 1024, forward: 43 us, 45 in 128 x 128 tiles; one row of one, 4096 -> 4096: 7.5, 37), and where there are few outputs (one expert of 200 rows, 4096 -> 1024: 18 us, 49;
+// four of 175, 4096 -> 4096: 171, 66).  In fp32 wherever 128 x 128 tiles would leave CUs idle (ten experts of 111 rows, 6272 -> 110: 48 us, 674; 512 -> 784: 23, 38).
 int few_rows(const LinearArgs& q, int kind, int esize) {
   const long long each = q.rows / most_groups(q);
   if (each <= 8) return 1;
