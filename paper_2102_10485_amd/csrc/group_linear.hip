@@ -366,6 +366,7 @@ struct Copied : Tile<KMAJOR, R, NW> {
 template <bool KMAJOR, int R, int NW>
 struct Loaded : Tile<KMAJOR, R, NW> {
   typedef Tile<KMAJOR, R, NW> S;
+  __device__ static __forceinline__ int thread() { return threadIdx.x & (64 * NW - 1); }      // among the waves of the operand
   typedef bf16_t T;
   static constexpr bool COPIES = false;
   static constexpr int CHUNKS = R * 8 / (64 * NW);
@@ -377,8 +378,8 @@ struct Loaded : Tile<KMAJOR, R, NW> {
   int rows, left;                                                 // and the sum indices from it on
   bool short_row;
 
-  __device__ static __forceinline__ int row_of(int p) { return (threadIdx.x + p * 64 * NW) / (KMAJOR ? 8 : S::PER_ROW); }
-  __device__ static __forceinline__ int granule_of(int p) { return (threadIdx.x + p * 64 * NW) % (KMAJOR ? 8 : S::PER_ROW); }
+  __device__ static __forceinline__ int row_of(int p) { return (thread() + p * 64 * NW) / (KMAJOR ? 8 : S::PER_ROW); }
+  __device__ static __forceinline__ int granule_of(int p) { return (thread() + p * 64 * NW) % (KMAJOR ? 8 : S::PER_ROW); }
   // of a step with `left_` sum indices from it on, the elements from chunk p's first on
   __device__ __forceinline__ int there(int p, int left_) const {
     return row_of(p) < (KMAJOR ? rows : left_) ? (KMAJOR ? left_ : rows) - granule_of(p) * 8 : 0;
@@ -412,6 +413,7 @@ struct Loaded : Tile<KMAJOR, R, NW> {
 template <int R, int NW>
 struct Converted : Tile<true, R, NW> {
   typedef Tile<true, R, NW> S;
+  __device__ static __forceinline__ int thread() { return threadIdx.x & (64 * NW - 1); }      // among the waves of the operand
   typedef uint8_t T;
   static constexpr bool COPIES = false;
   static constexpr int CHUNKS = R * 4 / (64 * NW);
@@ -421,7 +423,7 @@ struct Converted : Tile<true, R, NW> {
   int byte[CHUNKS];
   __amdgpu_buffer_rsrc_t codes, scales;
   unsigned off[CHUNKS], scale_off[CHUNKS];
-  int k;                                                          // of the step that is asked for next
+  int k, first;                                                   // of the step that is asked for next, and of the first
 
   __device__ __forceinline__ void prepare(const T* base, const uint8_t* scale, long long stride, int row0, int rows, int k0, int k_end, int) {
     const long long blocks = stride / BLOCK8;
@@ -429,23 +431,23 @@ struct Converted : Tile<true, R, NW> {
     scales = buffer_of(scale + row0 * blocks, (unsigned long long)(rows * blocks));
 #pragma unroll
     for (int p = 0; p < CHUNKS; ++p) {
-      const int r = threadIdx.x / 4 + p * (16 * NW);
-      off[p] = r < rows ? (unsigned)(r * stride) + threadIdx.x % 4 * 16 : NO_ROW;
+      const int r = thread() / 4 + p * (16 * NW);
+      off[p] = r < rows ? (unsigned)(r * stride) + thread() % 4 * 16 : NO_ROW;
       scale_off[p] = r < rows ? (unsigned)(r * blocks) : NO_ROW;
     }
-    k = 0;
+    k = first = k0;
 #pragma unroll
     for (int p = 0; p < CHUNKS; ++p) ask(p);
-    k = STEP;
+    k += STEP;
   }
   __device__ __forceinline__ void ask(int p) {
-    // (behind the last step: the start of the rows again, which is not used)
+    // (behind the last step: the first again, which is not used)
     q[p] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)off[p], k, 0));
     byte[p] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_off[p], k / BLOCK8, 0);
   }
   __device__ __forceinline__ void next_step() {}
   __device__ __forceinline__ void piece(int p, int, int left, unsigned char* lds, unsigned) {
-    const int r = threadIdx.x / 4 + p * (16 * NW), c = threadIdx.x % 4 * 2;
+    const int r = thread() / 4 + p * (16 * NW), c = thread() % 4 * 2;
     const float f = power_of_two(byte[p]);
     const unsigned w[4] = {q[p].x, q[p].y, q[p].z, q[p].w};
     u32x4 lo, hi;
@@ -459,7 +461,7 @@ struct Converted : Tile<true, R, NW> {
     *reinterpret_cast<u32x4*>(lds + r * 128 + ((c ^ S::swap_of(r)) * 16)) = lo;
     *reinterpret_cast<u32x4*>(lds + r * 128 + (((c + 1) ^ S::swap_of(r)) * 16)) = hi;
     ask(p);
-    if (p == CHUNKS - 1) k = left > 2 * STEP ? k + STEP : 0;
+    if (p == CHUNKS - 1) k = left > 2 * STEP ? k + STEP : first;
   }
 };
 
@@ -469,7 +471,7 @@ template <bool KMAJOR, int R, int NW> struct Operand<ANY, KMAJOR, R, NW> { typed
 template <int R, int NW> struct Operand<EIGHT_BITS, true, R, NW> { typedef Converted<R, NW> type; };
 
 // One tile of expert `group` (q.groups: of none): rows m0 .. m_end - 1, columns n0 .., sum indices k_begin .. k_end - 1.
-template <Form F, int KIND, int BM, int BN, int WM, int WN, int S, typename C>
+template <Form F, int KIND, int BM, int BN, int WM, int WN, int S, int SPLIT, typename C>
 __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char* lds, int group, int part, int m0, int m_end, int n0, int k_begin, int k_end) {
   constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   constexpr bool EIGHT = F == EIGHT_BITS;
@@ -477,9 +479,14 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
   typedef typename Operand<F, KIND == FORWARD, BN, NW>::type CB;
   typedef typename CA::T T;
   constexpr int STAGE = CA::BYTES + CB::BYTES;                    // S of them
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // SPLIT = 2: two sets of waves take half of the sum each, with stages of their own
+  const int set = SPLIT == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-  const int steps = (k_end - k_begin + STEP - 1) / STEP;
+  const int all_steps = (k_end - k_begin + STEP - 1) / STEP, steps = (all_steps + SPLIT - 1) / SPLIT;
+  if (SPLIT > 1) {
+    k_begin = min(k_begin + set * steps * STEP, k_end);
+    k_end = min(k_begin + steps * STEP, k_end);
+  }
   int left = k_end - k_begin;
 
   floatx4 acc[TM][TN];
@@ -495,6 +502,8 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
     const long long blocks8 = (long long)q.n * (q.b_stride / BLOCK8);
     ca.prepare((const T*)q.a, q.a_scale, q.a_stride, m0, min(BM, m_end - m0), k_begin, k_end, wave);
     cb.prepare((const T*)q.b + expert * q.b_group, EIGHT ? q.b_scale + expert * blocks8 : nullptr, q.b_stride, n0, min(BN, q.n - n0), k_begin, k_end, wave);
+    unsigned char* const whole_lds = lds;
+    if (SPLIT > 1) lds += set * S * STAGE;
     const unsigned lds0 = lds_address(lds);
     constexpr int PIECES = CA::PIECES + CB::PIECES;
     auto copy_piece = [&](int p, int stage) {
@@ -552,10 +561,24 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
     }
     if constexpr (CA::COPIES) wait_vm<0>();
     __syncthreads();                                              // nothing is written to LDS any more, or read
+    lds = whole_lds;
   }
 
+  if constexpr (SPLIT > 1) {                                      // the second set's sums are added to the first's
+    floatx4* at = reinterpret_cast<floatx4*>(lds) + wave * 64 + (threadIdx.x & 63);
+    static_assert(SPLIT == 2 && TM * TN * NW * 1024 <= 2 * S * STAGE, "the sums' LDS");
+    if (set == 1)
+#pragma unroll
+      for (int i = 0; i < TM * TN; ++i) at[i * NW * 64] = acc[i / TN][i % TN];
+    __syncthreads();
+    if (set == 0)
+#pragma unroll
+      for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] += at[i * NW * 64];
+    __syncthreads();
+    if (set == 1) return;
+  }
   C* c = (C*)q.c + (KIND == WGRAD ? part * q.part + (long long)group * q.c_group : 0);
-  static_assert(NW * 16 * (TN * 16 * (int)sizeof(C) + 16) <= 2 * STAGE, "the outputs' LDS");
+  static_assert(NW * 16 * (TN * 16 * (int)sizeof(C) + 16) <= S * STAGE, "the outputs' LDS");
   store_rows<C, TM, TN>(acc, c, q.c_stride, lds + wave * 16 * (TN * 16 * (int)sizeof(C) + 16), m0 + wm, m_end, n0 + wn, q.n);
 }
 
@@ -582,8 +605,8 @@ __device__ __forceinline__ void banded(unsigned id, unsigned row_tiles, unsigned
 
 // Forward and dgrad.  Block b runs on XCD b % 8.  Each XCD takes one stretch of the tiles of full height (the whole ones, then experts' last ones of more than half
 // of it), then its share of the last ones that half the height is enough for, then of those for a quarter, so that the shortest blocks end the launch.
-template <Form F, int KIND, int BM, int BN, int WM, int WN, typename C>
-__global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearArgs q) {
+template <Form F, int KIND, int BM, int BN, int WM, int WN, int SPLIT, typename C>
+__global__ __launch_bounds__(64 * WM * WN * SPLIT) void linear_kernel(LinearArgs q) {
   extern __shared__ __align__(1024) unsigned char lds[];
   unsigned count[SORTS];
   count_tiles(q.offs, q.groups, q.rows, BM, count);
@@ -611,11 +634,11 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearArgs q) {
   const int n0 = (int)c * BN, k = group < q.groups ? q.k : 0;
   if (sort == WHOLE) m_end = min(m_end, m0 + BM);
   if (sort <= HIGH)
-    tile_product<F, KIND, BM, BN, WM, WN, stages(F, BM, BN), C>(q, lds, group, 0, m0, m_end, n0, 0, k);
+    tile_product<F, KIND, BM, BN, WM, WN, stages(F, BM, BN), SPLIT, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
   else if (F == EIGHT_BITS || sort == HALF)                       // (8-bit codes are loaded for 128 rows at least, by 512 threads)
-    tile_product<F, KIND, BM / 2, BN, WM, WN, stages(F, BM / 2, BN), C>(q, lds, group, 0, m0, m_end, n0, 0, k);
+    tile_product<F, KIND, BM / 2, BN, WM, WN, stages(F, BM / 2, BN), SPLIT, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
   else if constexpr (F != EIGHT_BITS)
-    tile_product<F, KIND, BM / 4, BN, WM, WN, stages(F, BM / 4, BN), C>(q, lds, group, 0, m0, m_end, n0, 0, k);
+    tile_product<F, KIND, BM / 4, BN, WM, WN, stages(F, BM / 4, BN), SPLIT, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
 }
 
 template <Form F, int BM, int BN, int WM, int WN>
@@ -625,7 +648,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_wgrad_kernel(LinearArgs q
   int begin, end;
   group_rows(q.offs, q.groups, q.rows, group, begin, end);
   part_of(part, q.parts, begin, end);
-  tile_product<F, WGRAD, BM, BN, WM, WN, stages(F, BM, BN), float>(q, lds, group, part, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
+  tile_product<F, WGRAD, BM, BN, WM, WN, stages(F, BM, BN), 1, float>(q, lds, group, part, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
 }
 
 // dw = the parts, added in order
@@ -907,23 +930,26 @@ long long most_groups(const LinearArgs& q) { return std::max(1, std::min(q.group
 long long tiles(const LinearArgs& q, int height, int width) { return (q.rows / height + most_groups(q)) * ceil_div(q.n, width); }
 long long wgrad_tiles(long long groups, long long m, long long n, int side) { return groups * ceil_div(m, side) * ceil_div(n, side); }
 
-template <Form F, int KIND, int BM, int BN, int WM, int WN, typename C>
+template <Form F, int KIND, int BM, int BN, int WM, int WN, int SPLIT, typename C>
 gan_status launch_tiles(const LinearArgs& q, hipStream_t st) {
-  constexpr int LDS = KIND == WGRAD ? stages(F, BM, BN) * (BM + BN) * 128 : lds_bytes(F, BM, BN);
+  constexpr int LDS = KIND == WGRAD ? stages(F, BM, BN) * (BM + BN) * 128 : SPLIT * lds_bytes(F, BM, BN);
   if constexpr (KIND == WGRAD)
     return launch(linear_wgrad_kernel<F, BM, BN, WM, WN>, q.parts * wgrad_tiles(q.groups, q.m, q.n, BM), 64 * WM * WN, LDS, q, st);
   else    // (full tiles and lower ones are each shared among the eight XCDs)
-    return launch(linear_kernel<F, KIND, BM, BN, WM, WN, C>, 8 * (ceil_div(most_tiles(q.rows, q.groups, BM) * ceil_div(q.n, BN), 8) + 1), 64 * WM * WN, LDS, q, st);
+    return launch(linear_kernel<F, KIND, BM, BN, WM, WN, SPLIT, C>, 8 * (ceil_div(most_tiles(q.rows, q.groups, BM) * ceil_div(q.n, BN), 8) + 1), 64 * WM * WN * SPLIT, LDS, q, st);
 }
 // 256 x 256 tiles where they fill the CUs and experts have more than 32 rows on average, 128 x 128 where not.  Both sides, us on an MI355X from cold memory (256, 128):
 // 32 experts of 128 rows, 2048 -> 2048, forward 77, 97; 64 of 47, 1024 -> 1024, dgrad 31, 34; 128 of 14, 2361 -> 384, 8 bits 59, 43; four of 175, 4096 -> 4096 (64 tiles
-// of 256), forward 100, 67; weight gradient of 64 experts, 2816 -> 512: 109, 138.
+// of 256), forward 100, 67; weight gradient of 64 experts, 2816 -> 512: 109, 138.  Where those leave about one block to a CU and the sum is long, two sets of waves take half of
+// it each (without, with): one expert of 1000 rows, 4096 -> 4096: 62, 53, in 8 bits 60, 43; one of 600, 1024 -> 1024: 16.9, 14.2; ten of 128, 512 -> 1024 (8 steps): 11.7, 11.8.
 template <Form F, int KIND, typename C>
 gan_status launch_large(const LinearArgs& q, hipStream_t st) {
   const bool big = KIND == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, 256) >= 256 : tiles(q, 256, 256) >= 256 && q.rows / most_groups(q) > 32;
   if constexpr (F != ANY)
-    if (big) return launch_tiles<F, KIND, 256, 256, 2, 4, C>(q, st);
-  return launch_tiles<F, KIND, 128, 128, 2, 2, C>(q, st);
+    if (big) return launch_tiles<F, KIND, 256, 256, 2, 4, 1, C>(q, st);
+  if constexpr (KIND != WGRAD)
+    if (tiles(q, 128, 128) <= 288 && q.k >= 512) return launch_tiles<F, KIND, 128, 128, 2, 2, 2, C>(q, st);
+  return launch_tiles<F, KIND, 128, 128, 2, 2, 1, C>(q, st);
 }
 
 template <typename T, int TM, int JT, int U, bool ANY_ROWS, typename C>
