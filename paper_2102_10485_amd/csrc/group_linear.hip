@@ -362,47 +362,53 @@ struct Copied : Tile<KMAJOR, R, NW> {
   }
 };
 
-// A bf16 operand of any alignment: chunks of eight elements, which are written to LDS a step after they were asked for.
+// A bf16 operand of any alignment: chunks of eight elements, which are written to LDS a step after they were asked for.  Rows and columns that are not there are
+// others again (their products are not stored); sum indices that are not there are zero.
 template <bool KMAJOR, int R, int NW>
 struct Loaded : Tile<KMAJOR, R, NW> {
   typedef Tile<KMAJOR, R, NW> S;
-  __device__ static __forceinline__ int thread() { return threadIdx.x & (64 * NW - 1); }      // among the waves of the operand
   typedef bf16_t T;
   static constexpr bool COPIES = false;
-  static constexpr int CHUNKS = R * 8 / (64 * NW);
+  static constexpr int CHUNKS = R * 8 / (64 * NW), ROW_CHUNKS = KMAJOR ? 8 : S::PER_ROW;
   static constexpr int PIECES = CHUNKS;
-  static_assert(R * 8 % (64 * NW) == 0, "whole chunks");
+  static_assert(R * 8 % (64 * NW) == 0 && 64 * NW % ROW_CHUNKS == 0, "whole chunks, and a thread's all at one place of their rows");
   u32x4 q[CHUNKS];
-  const T* at;                                                    // of the step that is asked for next
-  long long stride;
-  int rows, left;                                                 // and the sum indices from it on
+  const T* at[CHUNKS];                                            // of the step that is asked for next
+  long long move;
+  int left;                                                       // the sum indices from it on
+  int column_tail;                                                // elements of the row from the chunk on (other than k-major; 8 or more: all)
   bool short_row;
 
-  __device__ static __forceinline__ int row_of(int p) { return (thread() + p * 64 * NW) / (KMAJOR ? 8 : S::PER_ROW); }
-  __device__ static __forceinline__ int granule_of(int p) { return (thread() + p * 64 * NW) % (KMAJOR ? 8 : S::PER_ROW); }
-  // of a step with `left_` sum indices from it on, the elements from chunk p's first on
-  __device__ __forceinline__ int there(int p, int left_) const {
-    return row_of(p) < (KMAJOR ? rows : left_) ? (KMAJOR ? left_ : rows) - granule_of(p) * 8 : 0;
-  }
-  __device__ __forceinline__ void prepare(const T* base, const uint8_t*, long long stride_, int row0, int rows_, int k0, int k_end, int) {
-    stride = stride_;
-    rows = rows_;
-    at = base + (KMAJOR ? row0 * stride + k0 : k0 * stride + row0);
+  __device__ static __forceinline__ int thread() { return threadIdx.x & (64 * NW - 1); }      // among the waves of the operand
+  __device__ static __forceinline__ int row_of(int p) { return (thread() + p * 64 * NW) / ROW_CHUNKS; }
+  __device__ static __forceinline__ int granule() { return thread() % ROW_CHUNKS; }
+  __device__ __forceinline__ void prepare(const T* base, const uint8_t*, long long stride, int row0, int rows, int k0, int k_end, int) {
     left = k_end - k0;
     short_row = (KMAJOR ? k_end : row0 + rows) < 8;
+    move = KMAJOR ? STEP : STEP * stride;
+    const int c = KMAJOR ? granule() * 8 : min(granule() * 8, (rows - 1) / 8 * 8);
+    column_tail = KMAJOR ? 8 : rows - c;
 #pragma unroll
-    for (int p = 0; p < CHUNKS; ++p) ask(p);
+    for (int p = 0; p < CHUNKS; ++p) {
+      at[p] = base + (KMAJOR ? (row0 + min(row_of(p), rows - 1)) * stride + k0 : (k0 + row_of(p)) * stride + row0) + c;
+      if (!short_row) at[p] -= max(8 - column_tail, 0);
+      ask(p);
+    }
     step_on();
   }
   __device__ __forceinline__ void step_on() {
-    at += KMAJOR ? STEP : STEP * stride;
+#pragma unroll
+    for (int p = 0; p < CHUNKS; ++p) at[p] += move;
     left -= STEP;
   }
-  __device__ __forceinline__ void ask(int p) { q[p] = load_last(at + row_of(p) * stride + granule_of(p) * 8, there(p, left), short_row); }
+  __device__ __forceinline__ void ask(int p) {
+    if constexpr (KMAJOR) q[p] = load_last(at[p], left - granule() * 8, short_row);
+    else q[p] = load_last(at[p], row_of(p) < left ? short_row ? column_tail : 8 : 0, short_row);
+  }
   __device__ __forceinline__ void next_step() {}
   __device__ __forceinline__ void piece(int p, int, int, unsigned char* lds, unsigned) {
-    const int r = row_of(p), g = granule_of(p) ^ S::swap_of(r);
-    *reinterpret_cast<u32x4*>(lds + r * (KMAJOR ? 128 : R * 2) + g * 16) = shift_last(q[p], there(p, left + STEP), short_row);
+    const int r = row_of(p), g = granule() ^ S::swap_of(r);
+    *reinterpret_cast<u32x4*>(lds + r * (KMAJOR ? 128 : R * 2) + g * 16) = shift_last(q[p], KMAJOR ? left + STEP - granule() * 8 : column_tail, short_row);
     ask(p);
     if (p == CHUNKS - 1) step_on();
   }
@@ -606,7 +612,7 @@ __device__ __forceinline__ void banded(unsigned id, unsigned row_tiles, unsigned
 // Forward and dgrad.  Block b runs on XCD b % 8.  Each XCD takes one stretch of the tiles of full height (the whole ones, then experts' last ones of more than half
 // of it), then its share of the last ones that half the height is enough for, then of those for a quarter, so that the shortest blocks end the launch.
 template <Form F, int KIND, int BM, int BN, int WM, int WN, int SPLIT, typename C>
-__global__ __launch_bounds__(64 * WM * WN * SPLIT) void linear_kernel(LinearArgs q) {
+__global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void linear_kernel(LinearArgs q) {
   extern __shared__ __align__(1024) unsigned char lds[];
   unsigned count[SORTS];
   count_tiles(q.offs, q.groups, q.rows, BM, count);
@@ -642,7 +648,7 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT) void linear_kernel(LinearArgs
 }
 
 template <Form F, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void linear_wgrad_kernel(LinearArgs q) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void linear_wgrad_kernel(LinearArgs q) {
   extern __shared__ __align__(1024) unsigned char lds[];
   const int n_tiles = (q.n + BN - 1) / BN, m_tiles = (q.m + BM - 1) / BM, t = blockIdx.x / n_tiles, e = t / m_tiles, group = e / q.parts, part = e % q.parts;
   int begin, end;
