@@ -36,31 +36,29 @@ struct LinearArgs {
 
 // ---- fp32 ----
 //
-// 128 x 128 tiles, 32 of the sum's index at a time: loaded into registers while the last ones are multiplied, then written to LDS as three planes of bf16
+// RT x RT tiles (128 or 64), 32 of the sum's index at a time: loaded into registers while the last ones are multiplied, then written to LDS as three planes of bf16
 // parts (split_mfma.h).  What has the sum's index as its row is kept that way and read with transposing LDS reads.
-constexpr int RT = 128, RK = 32;
+constexpr int RK = 32;
 
-template <bool KMAJOR>
+template <bool KMAJOR, int RT>
 struct Staged {
-  static constexpr int PLANE = RT * RK * 2;
-  float v[2][8];
+  static constexpr int PLANE = RT * RK * 2, CHUNKS = RT / 64, PER_ROW = KMAJOR ? RK / 8 : RT / 8;
+  float v[CHUNKS][8];
 
-  // thread t's two chunks of eight: k-major row t / 4 (+ 64), elements 8 (t % 4) ..; else sum index t / 16 (+ 16), columns 8 (t % 16) ..
+  // thread t's chunks of eight: k-major row t / 4 (+ 64), elements 8 (t % 4) ..; else sum index t / PER_ROW (+ 16), columns 8 (t % PER_ROW) ..
+  __device__ static __forceinline__ int row_of(int h) { return (threadIdx.x + h * 256) / PER_ROW; }
   __device__ __forceinline__ void load(const float* p, long long stride, int row0, int rows, int k0, int k_end) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = KMAJOR ? row0 + threadIdx.x / 4 + 64 * h : k0 + threadIdx.x / 16 + 16 * h;
-      const int c = KMAJOR ? k0 + threadIdx.x % 4 * 8 : row0 + threadIdx.x % 16 * 8;
+    for (int h = 0; h < CHUNKS; ++h) {
+      const int r = (KMAJOR ? row0 : k0) + row_of(h), c = (KMAJOR ? k0 : row0) + threadIdx.x % PER_ROW * 8;
       const int left = r < (KMAJOR ? rows : k_end) ? (KMAJOR ? k_end : rows) - c : 0;
       load8<float, false>(p + (long long)r * stride + c, left, v[h]);
     }
   }
   __device__ __forceinline__ void store(unsigned char* lds) const {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = KMAJOR ? threadIdx.x / 4 + 64 * h : threadIdx.x / 16 + 16 * h;
-      const int g = KMAJOR ? threadIdx.x % 4 : threadIdx.x % 16;
-      unsigned char* at = lds + offset(r, g);
+    for (int h = 0; h < CHUNKS; ++h) {
+      unsigned char* at = lds + offset(row_of(h), threadIdx.x % PER_ROW);
       u32x4 lo, hi;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -74,9 +72,13 @@ struct Staged {
     }
   }
   // Granules of eight elements are exchanged within a row so that the lanes of a read fall into different banks: rows of 64 bytes (k-major), read
-  // sixteen rows at a time, and of 256, read with eight sum indices at a time.
-  __device__ static __forceinline__ int swap_of(int r) { return KMAJOR ? (r >> 2) & 3 : ((r & 3) | ((r >> 3) & 1) << 2) << 1; }
-  __device__ static __forceinline__ int offset(int r, int granule) { return r * (KMAJOR ? RK * 2 : RT * 2) + (granule ^ swap_of(r)) * 16; }
+  // sixteen rows at a time, and of 256 or 128, read with eight sum indices at a time.
+  __device__ static __forceinline__ int swap_of(int r) {
+    if constexpr (KMAJOR) return (r >> 2) & 3;
+    else if constexpr (PER_ROW >= 16) return ((r & 3) | ((r >> 3) & 1) << 2) << 1;
+    else return (((r >> 1) & 1) | ((r >> 3) & 1) << 1) << 1;
+  }
+  __device__ static __forceinline__ int offset(int r, int granule) { return r * (PER_ROW * 16) + (granule ^ swap_of(r)) * 16; }
 
   // the MFMA operand of rows row .. row + 15: lane l has row l % 16, sum indices 8 (l / 16) .. + 7
   __device__ static __forceinline__ u32x4 read(const unsigned char* lds, int row) {
@@ -156,10 +158,11 @@ __device__ __forceinline__ void store_rows(const floatx4 (&acc)[TM][TN], C* c, l
   }
 }
 
-template <int KIND>
-__global__ __launch_bounds__(256, 2) void linear_fp32_kernel(LinearArgs q) {
-  typedef Staged<KIND != WGRAD> SA;
-  typedef Staged<KIND == FORWARD> SB;
+template <int KIND, int RT>
+__global__ __launch_bounds__(256, RT == 128 ? 2 : 4) void linear_fp32_kernel(LinearArgs q) {
+  typedef Staged<KIND != WGRAD, RT> SA;
+  typedef Staged<KIND == FORWARD, RT> SB;
+  constexpr int TW = RT / 32;                                     // sixteens of a wave's rows, and of its columns
   __shared__ __align__(16) unsigned char lds[2 * 3 * RT * RK * 2];
   unsigned char *la = lds, *lb = lds + 3 * RT * RK * 2;
 
@@ -181,12 +184,12 @@ __global__ __launch_bounds__(256, 2) void linear_fp32_kernel(LinearArgs q) {
   const float* b = (const float*)q.b + (KIND == WGRAD ? 0 : (long long)(group < q.groups ? group : 0) * q.b_group);
   float* c = (float*)q.c + (KIND == WGRAD ? part * q.part + (long long)group * q.c_group : 0);
 
-  const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-  floatx4 acc[4][4], low[4][4];
+  const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, wm = (wave >> 1) * (RT / 2), wn = (wave & 1) * (RT / 2);
+  floatx4 acc[TW][TW], low[TW][TW];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < TW; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = low[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < TW; ++j) acc[i][j] = low[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
   SA sa;
   SB sb;
@@ -203,18 +206,18 @@ __global__ __launch_bounds__(256, 2) void linear_fp32_kernel(LinearArgs q) {
       sa.load(a, q.a_stride, m0, m_end, k0 + RK, k_end);
       sb.load(b, q.b_stride, n0, q.n, k0 + RK, k_end);
     }
-    u32x4 fa[4][3];
+    u32x4 fa[TW][3];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < TW; ++i)
 #pragma unroll
       for (int p = 0; p < 3; ++p) fa[i][p] = SA::read(la + p * SA::PLANE, wm + i * 16);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < TW; ++j) {
       u32x4 fb[3];
 #pragma unroll
       for (int p = 0; p < 3; ++p) fb[p] = SB::read(lb + p * SB::PLANE, wn + j * 16);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {                               // (b first: a lane then holds four neighbouring columns of one row)
+      for (int i = 0; i < TW; ++i) {                               // (b first: a lane then holds four neighbouring columns of one row)
         mma(acc[i][j], fb[0], fa[i][0]);
         mma(low[i][j], fb[0], fa[i][1]);
         mma(low[i][j], fb[1], fa[i][0]);
@@ -227,18 +230,18 @@ __global__ __launch_bounds__(256, 2) void linear_fp32_kernel(LinearArgs q) {
 
   bool again = false;                                             // a value out of the parts' range, an infinity or NaN
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < TW; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < TW; ++j) {
       acc[i][j] = (acc[i][j] + low[i][j]) * SPLIT_UNSCALE;
 #pragma unroll
       for (int e = 0; e < 4; ++e) again |= !finite_bits(__float_as_uint(acc[i][j][e]) & 0x7fffffffu);
     }
   if (again) {                                                    // this lane's outputs as chains of fp32 multiply-adds
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < TW; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < TW; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int m = m0 + wm + i * 16 + (l & 15), n = n0 + wn + j * 16 + (l >> 4) * 4 + e;
@@ -253,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void linear_fp32_kernel(LinearArgs q) {
         }
   }
   __syncthreads();
-  store_rows<float, 4, 4>(acc, c, q.c_stride, lds + wave * 16 * (64 * 4 + 16), m0 + wm, m_end, n0 + wn, q.n);
+  store_rows<float, TW, TW>(acc, c, q.c_stride, lds + wave * 16 * (TW * 64 + 16), m0 + wm, m_end, n0 + wn, q.n);
 }
 
 // ---- bf16 and 8 bits ----
@@ -958,6 +961,8 @@ gan_status launch_large(const LinearArgs& q, hipStream_t st) {
   return launch_tiles<F, KIND, 128, 128, 2, 2, 1, C>(q, st);
 }
 
+// blocks of 32 columns, at most
+long long few_blocks(const LinearArgs& q) { return most_groups(q) * ceil_div(q.n, 32); }
 template <typename T, int TM, int JT, int U, bool ANY_ROWS, typename C>
 gan_status launch_few_as(const LinearArgs& q, hipStream_t st) {
   return launch(linear_few_kernel<T, TM, JT, U, 8, ANY_ROWS, C>, most_tiles(q.rows, q.groups, 16 * TM) * ceil_div(q.n, 16 * JT), 512, 0, q, st);
@@ -966,8 +971,11 @@ template <typename T, bool ANY_ROWS, typename C>
 gan_status launch_few(const LinearArgs& q, int sixteens, hipStream_t st) {
   constexpr int U = sizeof(T) == 1 ? 2 : 4;
   if (sixteens == 2) return launch_few_as<T, 2, 2, U, ANY_ROWS, C>(q, st);
-  // sixteen columns a block where 32 make few blocks: eight rows of eight experts, 4096 -> 4096, 28 us (32 columns: 35); four rows of a hundred, 1024 -> 1024, 47 (36)
-  return most_groups(q) * ceil_div(q.n, 32) <= 1024 ? launch_few_as<T, 1, 1, U, ANY_ROWS, C>(q, st) : launch_few_as<T, 1, 2, U, ANY_ROWS, C>(q, st);
+  // sixteen columns a block where 32 make few blocks: eight rows of eight experts, 4096 -> 4096, 28 us (32 columns: 35); four rows of a hundred, 1024 -> 1024, 47 (36).  A turn
+  // of the eight waves takes in 1024 sum indices of bf16, or half of that where there are fewer than two such (ten rows of a hundred experts, 1024 -> 1024: 9.2 -> 7.9;
+  // but eight of eight, 4096 -> 4096: 31 -> 39)
+  if (few_blocks(q) <= 1024) return q.k < 2048 ? launch_few_as<T, 1, 1, 2, ANY_ROWS, C>(q, st) : launch_few_as<T, 1, 1, U, ANY_ROWS, C>(q, st);
+  return launch_few_as<T, 1, 2, 2, ANY_ROWS, C>(q, st);
 }
 template <typename T, int TM, int U, int NW, bool ANY_ROWS>
 gan_status launch_few_dgrad_as(const LinearArgs& q, hipStream_t st) {
@@ -984,14 +992,21 @@ gan_status launch_few_dgrad(const LinearArgs& q, int sixteens, hipStream_t st) {
 // four of 175, 4096 -> 4096: 171, 66).  In fp32 wherever 128 x 128 tiles would leave CUs idle (ten experts of 111 rows, 6272 -> 110: 48 us, 674; 512 -> 784: 23, 38).
 int few_rows(const LinearArgs& q, int kind, int esize) {
   const long long each = q.rows / most_groups(q);
+  // short sums of many outputs give the waves little to share (128 experts of 3.5 rows, 256 -> 896: 32 us, 21 in tiles; fp32, eight of 128, 64 -> 896: 15.3, 5.6)
+  if (q.k < 512 && (few_blocks(q) > 1024 || (esize == 4 && each > 8))) return 0;
   if (each <= 8) return 1;
   if (esize == 4) return tiles(q, 128, 128) < 256 ? (kind == DGRAD ? 1 : 2) : 0;
   return (long long)q.rows * q.n <= 1 << 19 ? 2 : 0;
 }
 
-gan_status launch_fp32(int kind, const LinearArgs& q, hipStream_t st) {
+template <int RT>
+gan_status launch_fp32_as(int kind, const LinearArgs& q, hipStream_t st) {
   const long long blocks = kind == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, RT) : ceil_div(q.n, RT) * most_tiles(q.rows, q.groups, RT);
-  return launch(kind == FORWARD ? linear_fp32_kernel<FORWARD> : kind == DGRAD ? linear_fp32_kernel<DGRAD> : linear_fp32_kernel<WGRAD>, blocks, 256, 0, q, st);
+  return launch(kind == FORWARD ? linear_fp32_kernel<FORWARD, RT> : kind == DGRAD ? linear_fp32_kernel<DGRAD, RT> : linear_fp32_kernel<WGRAD, RT>, blocks, 256, 0, q, st);
+}
+gan_status launch_fp32(int kind, const LinearArgs& q, hipStream_t st) {
+  const long long large = kind == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, 128) : tiles(q, 128, 128);
+  return large >= (kind == WGRAD ? 400 : 1024) ? launch_fp32_as<128>(kind, q, st) : launch_fp32_as<64>(kind, q, st);
 }
 
 // Into how many parts the weight gradient takes an expert's rows: few tiles of long sums would leave most CUs idle.
