@@ -2,7 +2,8 @@
 //
 //   m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2;  p = p (1 - lr decay) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
-// Bound by memory: 28 bytes a value with fp32 gradients and moments (30 with the bf16 copy), 16 with bf16 gradients, moments of 8 bits and the copy.
+// Bound by memory: 30 bytes a value with fp32 gradients, fp32 moments and the bf16 copy, 16 with bf16 gradients, moments of 8 bits and the copy.  A
+// hundred million values on an MI355X: 551 us and 298 us, 5.4 TB/s both (a plain copy: 4.9 of reads and writes); 210 million in four tensors, 8 bits: 613 us.
 // A block takes CHUNK values of one tensor; which ones it reads off a table that the handle laid out once, so that small and
 // large tensors share the launch.  In 8 bits the moments of 128 values, which sixteen lanes hold, share a power of two (operators.h): m as it is and the
 // square root of v, whose range is half of v's.  Both are rounded by chance: with b2 = 0.999 a step moves sqrt(v) by 0.05 % of its distance

@@ -7,6 +7,12 @@
 //
 // "k-major" below: the sum's index runs along memory (both operands of the forward product, dy of dgrad); the others have it as the row.
 // Which expert a tile of rows belongs to every wave finds itself from the offsets, so that a call is one launch.
+//
+// Times on an MI355X (its library's product of 8192^3: 1.34 PFLOP/s in bf16; a copy: 4.9 TB/s).  bf16 tiles: 8192^3 as one expert 1.26-1.37 PFLOP/s, forward, dgrad and wgrad, 1.35
+// from 8 bits: bound by the matrix pipe and the clock that its power leaves (its share of the cycles at eight experts of 2048 rows, 4096 -> 4096: 0.55; LDS
+// bank conflicts, all from the stores, 3 % of its cycles).  There 491 us, where the experts' last tiles cost a fifth (equal experts: 437), and 470 from 8 bits; weight gradient 505, of which
+// 537 MB of fp32 results are 110.  A hundred experts of unequal sizes, 1024 -> 1024, cold weights: 78 us forward, 48 dgrad (weights cached), 111 wgrad (4 TB/s): bound by the
+// weights' bytes.  Few rows: ten rows of a hundred experts 7 us (21 MB of weights), eight of eight experts in 8 bits 26 us (90 MB).
 #include "group_tiles.h"
 #include "lds_copy.h"
 #include "operators.h"
@@ -36,6 +42,8 @@ struct LinearArgs {
 
 // ---- fp32 ----
 //
+// Bound by the matrix pipe, which six bf16 products a value keep busy, and the vector instructions that split the operands: eight experts of 1024 rows, 2048 -> 2048, 445 us
+// forward, 433 dgrad, 379 wgrad = 154-181 TFLOP/s (the library's fp32 product: 133).
 // RT x RT tiles (128 or 64), 32 of the sum's index at a time: loaded into registers while the last ones are multiplied, then written to LDS as three planes of bf16
 // parts (split_mfma.h).  What has the sum's index as its row is kept that way and read with transposing LDS reads.
 constexpr int RK = 32;

@@ -2,7 +2,8 @@
 //
 //   sum = round(x + residual), inv = 1 / sqrt(mean(sum^2) + eps), y = sum * inv * gain
 //
-// Bound by memory: one pass over x and residual, six operations an element.  A row is held in registers between the sum of its squares and
+// Bound by memory: one pass over x and residual, six operations an element; bf16 on an MI355X: 16384 x 4096 into 8 bits 85 us (5.5 TB/s), 6400 x 2048 forward 21 us and
+// gradient 26 us from cold memory (5.1 and 4.1 TB/s; a plain copy 4.9), four rows of 1024 3.2 us.  A row is held in registers between the sum of its squares and
 // its output, by one wave (rows up to 2048 elements, where no barrier is needed), a block of four waves, or one of sixteen; rows beyond
 // 32768 elements (16384 in the gradient) are read a second time.
 #include "operators.h"
