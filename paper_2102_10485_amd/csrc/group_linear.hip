@@ -10,7 +10,7 @@
 //
 // Times on an MI355X (its library's product of 8192^3: 1.34 PFLOP/s in bf16; a copy: 4.9 TB/s).  bf16 tiles: 8192^3 as one expert 1.26-1.37 PFLOP/s, forward, dgrad and wgrad, 1.35
 // from 8 bits: bound by the matrix pipe and the clock that its power leaves (its share of the cycles at eight experts of 2048 rows, 4096 -> 4096: 0.55; LDS
-// bank conflicts, all from the stores, 3 % of its cycles).  There 491 us, where the experts' last tiles cost a fifth (equal experts: 437), and 470 from 8 bits; weight gradient 505, of which
+// bank conflicts, all from the stores, 3 % of its cycles).  With drawn sizes of 2048 rows on average 478 us, where the experts' last tiles cost a tenth (equal experts: 437), and 456 from 8 bits; weight gradient 505, of which
 // 537 MB of fp32 results are 110.  A hundred experts of unequal sizes, 1024 -> 1024, cold weights: 78 us forward, 48 dgrad (weights cached), 111 wgrad (4 TB/s): bound by the
 // weights' bytes.  Few rows: ten rows of a hundred experts 7 us (21 MB of weights), eight of eight experts in 8 bits 26 us (90 MB).
 #include "group_tiles.h"
@@ -599,17 +599,27 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
   store_rows<C, TM, TN>(acc, c, q.c_stride, lds + wave * 16 * (TN * 16 * (int)sizeof(C) + 16), m0 + wm, m_end, n0 + wn, q.n);
 }
 
-// Stages of a tile: what LDS holds of them where a block has a CU for itself (tiles of 256 columns), or two blocks share one.
-constexpr int stages(Form f, int height, int width) {
-  const int most = (width == 256 ? 160 : 80) * 1024 / ((height + width) * 128);
+// Stages of a tile in a share of LDS
+constexpr int stages(Form f, int height, int width, int kib) {
+  const int most = kib * 1024 / ((height + width) * 128);
   return f != ALIGNED || most < 2 ? 2 : most > 4 ? 4 : most;
 }
-constexpr int lds_bytes(Form f, int height, int width) {
-  int most = 0;
-  for (int h = height; h >= height / 4; h /= 2)
-    if (stages(f, h, width) * (h + width) * 128 > most) most = stages(f, h, width) * (h + width) * 128;
-  return most;
-}
+// How a launch with tiles of BM x BN by WM x WN waves (SPLIT = 2: and as many again) takes experts' last rows: in half and a quarter of the height.  Next to many
+// 256 x 256 tiles, which have a CU for themselves, half the columns by two sets of four waves, twice the blocks of half the length, end a launch sooner (eight experts of
+// 2048 rows, 4096 -> 4096: 489 -> 478 us, in 8 bits 486 -> 456); where they are most of the launch, they read the weights less well (32 of 128, 2048 -> 2048: 79 -> 92).
+template <Form F, int BM, int BN, int WM, int WN, int SPLIT>
+struct Shapes {
+  static constexpr bool NARROW = BM == 256;
+  static constexpr int KIB = NARROW ? 160 : 80, S = stages(F, BM, BN, KIB);
+  static constexpr int S_HALF = stages(F, BM / 2, BN, KIB), S_QUARTER = stages(F, BM / 4, BN, KIB);
+  static constexpr int S_NARROW_HALF = stages(F, BM / 2, BN / 2, KIB / 2), S_NARROW_QUARTER = stages(F, BM / 4, BN / 2, KIB / 2);
+  static constexpr bool QUARTERS = F != EIGHT_BITS;               // (8-bit codes are loaded for a row by four lanes: eight waves have 128 rows at least)
+  static constexpr int bytes(int height, int width, int s, int sets) { return (height + width) * 128 * s * sets; }
+  static constexpr int most(int a, int b) { return a > b ? a : b; }
+  static constexpr int WIDE_LDS = most(bytes(BM, BN, S, SPLIT), most(bytes(BM / 2, BN, S_HALF, SPLIT), bytes(BM / 4, BN, S_QUARTER, SPLIT)));
+  static constexpr int LDS = NARROW ? most(WIDE_LDS, most(bytes(BM / 2, BN / 2, S_NARROW_HALF, 2), bytes(BM / 4, BN / 2, S_NARROW_QUARTER, 2))) : WIDE_LDS;
+  static_assert(LDS <= 160 * 1024, "LDS");
+};
 
 // Rows of tiles in bands of 8, columns by 4 within a band: 32 tiles in a row, which the CUs of one XCD work on together, then read 8 + 4
 // panels through its L2 in place of 64.
@@ -625,9 +635,11 @@ __device__ __forceinline__ void banded(unsigned id, unsigned row_tiles, unsigned
 template <Form F, int KIND, int BM, int BN, int WM, int WN, int SPLIT, typename C>
 __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void linear_kernel(LinearArgs q) {
   extern __shared__ __align__(1024) unsigned char lds[];
+  typedef Shapes<F, BM, BN, WM, WN, SPLIT> P;
   unsigned count[SORTS];
   count_tiles(q.offs, q.groups, q.rows, BM, count);
-  const unsigned cols = (unsigned)(q.n + BN - 1) / BN, xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
+  const bool narrow = P::NARROW && 4 * (count[HALF] + count[LOW]) <= count[WHOLE] + count[HIGH];
+  const unsigned cols = (unsigned)(q.n + BN - 1) / BN, end_cols = narrow ? (unsigned)(q.n + BN / 2 - 1) / (BN / 2) : cols, xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
   const unsigned full = (count[WHOLE] + count[HIGH]) * cols, share = (full + 7) / 8;
   unsigned r, c, id = i < share ? xcd * share + i : (i - share) * 8 + xcd;
   int sort;
@@ -636,26 +648,32 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void linear_kernel(LinearA
     sort = id < count[WHOLE] * cols ? WHOLE : HIGH;
     if (sort == HIGH) id -= count[WHOLE] * cols;
   } else {
-    sort = id < count[HALF] * cols ? HALF : LOW;
-    if (sort == LOW) id -= count[HALF] * cols;
-    if (id >= count[sort] * cols) return;
+    sort = id < count[HALF] * end_cols ? HALF : LOW;
+    if (sort == LOW) id -= count[HALF] * end_cols;
+    if (id >= count[sort] * end_cols) return;
   }
   if (sort == WHOLE) {
     banded(id, count[WHOLE], cols, r, c);
   } else {
-    r = id / cols;
-    c = id % cols;
+    r = id / (sort == HIGH ? cols : end_cols);
+    c = id % (sort == HIGH ? cols : end_cols);
   }
   int group, m0, m_end;
   find_tile_of(sort, q.offs, q.groups, q.rows, BM, r, group, m0, m_end);
-  const int n0 = (int)c * BN, k = group < q.groups ? q.k : 0;
+  const int k = group < q.groups ? q.k : 0;
   if (sort == WHOLE) m_end = min(m_end, m0 + BM);
   if (sort <= HIGH)
-    tile_product<F, KIND, BM, BN, WM, WN, stages(F, BM, BN), SPLIT, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
-  else if (F == EIGHT_BITS || sort == HALF)                       // (8-bit codes are loaded for 128 rows at least, by 512 threads)
-    tile_product<F, KIND, BM / 2, BN, WM, WN, stages(F, BM / 2, BN), SPLIT, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
-  else if constexpr (F != EIGHT_BITS)
-    tile_product<F, KIND, BM / 4, BN, WM, WN, stages(F, BM / 4, BN), SPLIT, C>(q, lds, group, 0, m0, m_end, n0, 0, k);
+    tile_product<F, KIND, BM, BN, WM, WN, P::S, SPLIT, C>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, k);
+  else if (narrow) {
+    if constexpr (P::NARROW) {
+      if (sort == HALF) tile_product<F, KIND, BM / 2, BN / 2, WM, WN / 2, P::S_NARROW_HALF, 2, C>(q, lds, group, 0, m0, m_end, (int)c * (BN / 2), 0, k);
+      else tile_product<F, KIND, BM / 4, BN / 2, WM, WN / 2, P::S_NARROW_QUARTER, 2, C>(q, lds, group, 0, m0, m_end, (int)c * (BN / 2), 0, k);
+    }
+  } else if (!P::QUARTERS || sort == HALF) {
+    tile_product<F, KIND, BM / 2, BN, WM, WN, P::S_HALF, SPLIT, C>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, k);
+  } else if constexpr (P::QUARTERS) {
+    tile_product<F, KIND, BM / 4, BN, WM, WN, P::S_QUARTER, SPLIT, C>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, k);
+  }
 }
 
 template <Form F, int BM, int BN, int WM, int WN>
@@ -665,7 +683,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void linear_wgrad_kernel(LinearArg
   int begin, end;
   group_rows(q.offs, q.groups, q.rows, group, begin, end);
   part_of(part, q.parts, begin, end);
-  tile_product<F, WGRAD, BM, BN, WM, WN, stages(F, BM, BN), 1, float>(q, lds, group, part, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
+  tile_product<F, WGRAD, BM, BN, WM, WN, Shapes<F, BM, BN, WM, WN, 1>::S, 1, float>(q, lds, group, part, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
 }
 
 // dw = the parts, added in order
@@ -949,12 +967,16 @@ long long wgrad_tiles(long long groups, long long m, long long n, int side) { re
 
 template <Form F, int KIND, int BM, int BN, int WM, int WN, int SPLIT, typename C>
 gan_status launch_tiles(const LinearArgs& q, hipStream_t st) {
-  constexpr int LDS = KIND == WGRAD ? stages(F, BM, BN) * (BM + BN) * 128 : SPLIT * lds_bytes(F, BM, BN);
-  if constexpr (KIND == WGRAD)
-    return launch(linear_wgrad_kernel<F, BM, BN, WM, WN>, q.parts * wgrad_tiles(q.groups, q.m, q.n, BM), 64 * WM * WN, LDS, q, st);
-  else    // (full tiles and lower ones are each shared among the eight XCDs)
-    return launch(linear_kernel<F, KIND, BM, BN, WM, WN, SPLIT, C>, 8 * (ceil_div(most_tiles(q.rows, q.groups, BM) * ceil_div(q.n, BN), 8) + 1), 64 * WM * WN * SPLIT, LDS, q, st);
+  typedef Shapes<F, BM, BN, WM, WN, SPLIT> P;
+  if constexpr (KIND == WGRAD) {
+    return launch(linear_wgrad_kernel<F, BM, BN, WM, WN>, q.parts * wgrad_tiles(q.groups, q.m, q.n, BM), 64 * WM * WN, P::bytes(BM, BN, P::S, 1), q, st);
+  } else {
+    // Full tiles and lower ones are each shared among the eight XCDs; narrow ones are twice as many, but then a fifth of the tiles at most.
+    const long long high = most_tiles(q.rows, q.groups, BM), blocks = (high + (P::NARROW ? ceil_div(high, 5) : 0)) * ceil_div(q.n, BN);
+    return launch(linear_kernel<F, KIND, BM, BN, WM, WN, SPLIT, C>, 8 * (ceil_div(blocks, 8) + 1), 64 * WM * WN * SPLIT, P::LDS, q, st);
+  }
 }
+
 // 256 x 256 tiles where they fill the CUs and experts have more than 32 rows on average, 128 x 128 where not.  Both sides, us on an MI355X from cold memory (256, 128):
 // 32 experts of 128 rows, 2048 -> 2048, forward 77, 97; 64 of 47, 1024 -> 1024, dgrad 31, 34; 128 of 14, 2361 -> 384, 8 bits 59, 43; four of 175, 4096 -> 4096 (64 tiles
 // of 256), forward 100, 67; weight gradient of 64 experts, 2816 -> 512: 109, 138.  Where those leave about one block to a CU and the sum is long, two sets of waves take half of

@@ -27,6 +27,9 @@ CASES = {
     "long": (offsets([1, 1999]), 264, 2056),
     "parts": (offsets([3, 1900]), 96, 200),
     "odd parts": (offsets([5, 0, 2500]), 101, 77),
+    # many whole tiles of 256, and last ones of a half and of a quarter
+    "few ends, outputs": (offsets([1300, 1124]), 72, 6008),
+    "few ends, inputs": (offsets([1300, 1124]), 6008, 72),
 }
 
 
@@ -80,7 +83,7 @@ def test_values_that_are_not_finite_stay_with_their_expert(name, bf16):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("name", ["many", "odd", "long", "wide outputs", "odd inputs"])
+@pytest.mark.parametrize("name", ["many", "odd", "long", "wide outputs", "odd inputs", "few ends, outputs"])
 def test_eight_bits(name, bf16):
     offs, n_in, n_out = CASES[name]
     x8, xs, w8, ws = problem8(offs, n_in, n_out, 5)
