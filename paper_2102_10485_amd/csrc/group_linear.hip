@@ -133,7 +133,9 @@ __device__ __forceinline__ void part_of(int part, int parts, int& begin, int& en
 // A wave's outputs, rows m .. (of m_end) and columns n .. (of n_end), as MFMAs with the columns first leave them.  Sixteen rows at a time go through LDS (the wave's
 // own), so that its lanes store whole rows, 16 bytes each: 64 lanes with four columns each of sixteen rows would write 32 or 64 bytes of a row at a time (the weight
 // gradient of a hundred experts of 1024 x 1024: 173 us, 125 by rows).
-template <typename C, int TM, int TN>
+// PAST: past the caches.  A weight gradient's results are more than what they are made of and push it out of them (a hundred experts of 1024 x 1024: 124 us, 92 past
+// the caches; eight of 4096 x 4096: 527, 493; ten of 512 x 784: 11, 9.3).  A layer's outputs are read next, and stay.
+template <typename C, bool PAST, int TM, int TN>
 __device__ __forceinline__ void store_rows(const floatx4 (&acc)[TM][TN], C* c, long long stride, unsigned char* lds, int m0, int m_end, int n0, int n_end) {
   constexpr int WIDE = TN * 16 * (int)sizeof(C), LANES = WIDE / 16, EACH = 16 / (int)sizeof(C);
   static_assert(64 % LANES == 0, "whole rows");
@@ -157,7 +159,9 @@ __device__ __forceinline__ void store_rows(const floatx4 (&acc)[TM][TN], C* c, l
       if (m >= m_end || n >= n_end) continue;
       C* at = c + (long long)m * stride + n;
       if (n + EACH <= n_end) {
-        *reinterpret_cast<words*>(at) = words{v.x, v.y, v.z, v.w};
+        const words o = {v.x, v.y, v.z, v.w};
+        if constexpr (PAST) __builtin_nontemporal_store(o, reinterpret_cast<words*>(at));
+        else *reinterpret_cast<words*>(at) = o;
       } else {
         for (int k = 0; k < n_end - n; ++k) at[k] = reinterpret_cast<const C*>(from)[k];
       }
@@ -264,7 +268,7 @@ __global__ __launch_bounds__(256, RT == 128 ? 2 : 4) void linear_fp32_kernel(Lin
         }
   }
   __syncthreads();
-  store_rows<float, TW, TW>(acc, c, q.c_stride, lds + wave * 16 * (TW * 64 + 16), m0 + wm, m_end, n0 + wn, q.n);
+  store_rows<float, KIND == WGRAD, TW, TW>(acc, c, q.c_stride, lds + wave * 16 * (TW * 64 + 16), m0 + wm, m_end, n0 + wn, q.n);
 }
 
 // ---- bf16 and 8 bits ----
@@ -596,7 +600,7 @@ __device__ __forceinline__ void tile_product(const LinearArgs& q, unsigned char*
   }
   C* c = (C*)q.c + (KIND == WGRAD ? part * q.part + (long long)group * q.c_group : 0);
   static_assert(NW * 16 * (TN * 16 * (int)sizeof(C) + 16) <= S * STAGE, "the outputs' LDS");
-  store_rows<C, TM, TN>(acc, c, q.c_stride, lds + wave * 16 * (TN * 16 * (int)sizeof(C) + 16), m0 + wm, m_end, n0 + wn, q.n);
+  store_rows<C, KIND == WGRAD, TM, TN>(acc, c, q.c_stride, lds + wave * 16 * (TN * 16 * (int)sizeof(C) + 16), m0 + wm, m_end, n0 + wn, q.n);
 }
 
 // Stages of a tile in a share of LDS

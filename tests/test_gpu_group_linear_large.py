@@ -30,6 +30,7 @@ CASES = {
     # many whole tiles of 256, and last ones of a half and of a quarter
     "few ends, outputs": (offsets([1300, 1124]), 72, 6008),
     "few ends, inputs": (offsets([1300, 1124]), 6008, 72),
+    "few ends, one step": (offsets([1300, 1124]), 40, 6008),
 }
 
 
