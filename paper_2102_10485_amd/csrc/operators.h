@@ -57,27 +57,38 @@ __device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
   }
 }
 
-template <typename T, int ALIGN>
+// PAST: past the caches
+template <typename T, int ALIGN, bool PAST>
 __device__ __forceinline__ void store_whole8(T* p, const float (&v)[8]) {
   typedef typename Words<ALIGN>::T words;
-  if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<words*>(p) = words{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-    *reinterpret_cast<words*>(p + 4) = words{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
-  } else {
-    *reinterpret_cast<words*>(p) = words{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+  words* to = reinterpret_cast<words*>(p);
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+    words w;
+    if constexpr (sizeof(T) == 4) w = words{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+    else w = words{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+    if constexpr (PAST) __builtin_nontemporal_store(w, to + i);
+    else to[i] = w;
   }
 }
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool PAST = false>
 __device__ __forceinline__ void store8(T* p, int left, const float (&v)[8]) {
   if constexpr (VEC) {
-    if (left > 0) store_whole8<T, 16>(p, v);
+    if (left > 0) store_whole8<T, 16, PAST>(p, v);
   } else if (left >= 8) {
-    store_whole8<T, sizeof(T)>(p, v);
+    store_whole8<T, sizeof(T), PAST>(p, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < left) p[i] = from_float<T>(v[i]);
   }
+}
+
+template <bool PAST>
+__device__ __forceinline__ void store_codes(uint8_t* p, uint2 q) {                // eight of them, aligned
+  const uint64_t w = q.x | (uint64_t)q.y << 32;
+  if constexpr (PAST) __builtin_nontemporal_store(w, reinterpret_cast<uint64_t*>(p));
+  else *reinterpret_cast<uint64_t*>(p) = w;
 }
 
 // ---- the 8-bit format: e4m3 times one power of two for 128 neighbours, which 16 lanes hold, eight each ----

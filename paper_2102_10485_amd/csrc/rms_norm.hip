@@ -39,6 +39,11 @@ struct NormArgs {
   float eps;
 };
 
+// Results of more bytes than this go past the caches, which would not hold them all for their reader (bf16 with the sum, us through the caches and past them:
+// 16384 x 4096 94.6, 76.2, into 8 bits 86.7, 70.3; 65536 x 512 48.5, 39.5; 12000 x 2048 37.5, 34.3; a norm and two products of four experts on 16384 x 4096
+// 950, 942).  Smaller ones stay for it (norm and products of eight experts of 128 rows of 1024: 34.4, past the caches 36.9).
+constexpr long long PAST_CACHES = 64 << 20;
+
 template <typename T, bool VEC>
 __device__ __forceinline__ void add_rounded(float (&v)[E], const T* residual, int left) {
   float r[E];
@@ -47,23 +52,23 @@ __device__ __forceinline__ void add_rounded(float (&v)[E], const T* residual, in
   for (int i = 0; i < E; ++i) v[i] = to_float(from_float<T>(v[i] + r[i]));
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool PAST>
 __device__ __forceinline__ void write_chunk(const NormArgs& a, long long row, int col, const float (&s)[E], float inv) {
   float g[E], y[E];
   load8<float, VEC>(a.gain + col, a.cols - col, g);
 #pragma unroll
   for (int i = 0; i < E; ++i) y[i] = s[i] * inv * g[i];
-  if (a.y) store8<T, VEC>((T*)a.y + row * a.y_stride + col, a.cols - col, y);
+  if (a.y) store8<T, VEC, PAST>((T*)a.y + row * a.y_stride + col, a.cols - col, y);
   if (a.y8) {                                                     // the sixteen lanes of a block of 128 are here together, or none is
     const long long padded = padded8(a.cols);
     const int byte = scale_byte(y);
-    *reinterpret_cast<uint2*>(a.y8 + row * padded + col) = to_e4m3_x8(y, byte);
+    store_codes<PAST>(a.y8 + row * padded + col, to_e4m3_x8(y, byte));
     if ((threadIdx.x & 15) == 0) a.y8_scale[(row * padded + col) / BLOCK8] = (uint8_t)byte;
   }
 }
 
 // WAVES waves a row, lane l of them holding the chunks l, l + 64 WAVES, ...; blocks of four rows where a row is a wave's
-template <typename T, int WAVES, int CHUNKS, bool VEC>
+template <typename T, int WAVES, int CHUNKS, bool VEC, bool PAST>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_kernel(NormArgs a) {
   __shared__ float scratch[WAVES];
   const long long row = WAVES == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
@@ -85,7 +90,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_kernel(Nor
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int col = (c * 64 * WAVES + lane) * E;
-    if (a.sum) store8<T, VEC>((T*)a.sum + row * a.sum_stride + col, a.cols - col, s[c]);
+    if (a.sum) store8<T, VEC, PAST>((T*)a.sum + row * a.sum_stride + col, a.cols - col, s[c]);
 #pragma unroll
     for (int i = 0; i < E; ++i) q += s[c][i] * s[c][i];
   }
@@ -96,7 +101,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_kernel(Nor
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int col = (c * 64 * WAVES + lane) * E;
-    if (col < wide) write_chunk<T, VEC>(a, row, col, s[c], inv);
+    if (col < wide) write_chunk<T, VEC, PAST>(a, row, col, s[c], inv);
   }
 }
 
@@ -127,15 +132,15 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
       load8<T, VEC>(x + col, a.cols - col, s);
       if (residual) add_rounded<T, VEC>(s, residual + col, a.cols - col);
     }
-    write_chunk<T, VEC>(a, row, col, s, inv);
+    write_chunk<T, VEC, false>(a, row, col, s, inv);
   }
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool PAST>
 void launch_norm(const NormArgs& a, hipStream_t st) {
   const long long cols = a.cols;
   const unsigned rows = (unsigned)a.rows, by4 = (unsigned)((a.rows + 3) / 4);
-#define GAN_NORM(W, C) hipLaunchKernelGGL((norm_kernel<T, W, C, VEC>), dim3(W == 1 ? by4 : rows), dim3(W == 1 ? 256 : 64 * W), 0, st, a)
+#define GAN_NORM(W, C) hipLaunchKernelGGL((norm_kernel<T, W, C, VEC, PAST>), dim3(W == 1 ? by4 : rows), dim3(W == 1 ? 256 : 64 * W), 0, st, a)
   // Times on an MI355X.  Up to 1024 elements a wave per row has no barrier (bf16, 6400 x 1024: 13.5 us, four waves a row 15.6), but few rows
   // are done sooner by more waves (fp32, 1117 x 1000: 6.4 and 6.0).  Above, one chunk a lane is faster than more of them in fewer waves (bf16, 6400 x 2048: 22.8 us by four
   // waves, 28.7 by one; 4096 x 8192: 48.6 by sixteen, 52.9 by four).
@@ -408,8 +413,14 @@ extern "C" gan_status gan_rms_norm(int32_t precision, const void* x, int64_t x_s
                    (!sum || rows_aligned16(sum, sum_stride, e)) && (!y || rows_aligned16(y, y_stride, e));
   const NormArgs a = {x, residual, gain, sum, y, y8, y8_scale, inv_rms, x_stride, residual_stride, sum_stride, y_stride, rows, cols, eps};
   const hipStream_t st = (hipStream_t)hip_stream;
-  if (precision == GAN_FP32) vec ? launch_norm<float, true>(a, st) : launch_norm<float, false>(a, st);
-  else vec ? launch_norm<bf16_t, true>(a, st) : launch_norm<bf16_t, false>(a, st);
+  const auto go = [&](auto t) {
+    typedef decltype(t) T;
+    if (!vec) launch_norm<T, false, false>(a, st);
+    else if (rows * cols * ((sum ? e : 0) + (y ? e : 0) + (y8 ? 1 : 0)) > PAST_CACHES) launch_norm<T, true, true>(a, st);
+    else launch_norm<T, true, false>(a, st);
+  };
+  if (precision == GAN_FP32) go(float());
+  else go(bf16_t());
   return operator_launched();
 }
 
