@@ -10,8 +10,8 @@
 //
 // Times on an MI355X (its library's product of 8192^3: 1.34 PFLOP/s in bf16; a copy: 4.9 TB/s).  bf16 tiles: 8192^3 as one expert 1.26-1.37 PFLOP/s, forward, dgrad and wgrad, 1.35
 // from 8 bits: bound by the matrix pipe and the clock that its power leaves (its share of the cycles at eight experts of 2048 rows, 4096 -> 4096: 0.55; LDS
-// bank conflicts, all from the stores, 3 % of its cycles).  With drawn sizes of 2048 rows on average 478 us, where the experts' last tiles cost a tenth (equal experts: 437), and 456 from 8 bits; weight gradient 505, of which
-// 537 MB of fp32 results are 110.  A hundred experts of unequal sizes, 1024 -> 1024, cold weights: 78 us forward, 48 dgrad (weights cached), 111 wgrad (4 TB/s): bound by the
+// bank conflicts, all from the stores, 3 % of its cycles).  With drawn sizes of 2048 rows on average 478 us, where the experts' last tiles cost a tenth (equal experts: 437), and 456 from 8 bits; weight gradient 493-509, of which
+// 537 MB of fp32 results are 110.  A hundred experts of unequal sizes, 1024 -> 1024, cold weights: 78 us forward, 48 dgrad (weights cached), 90 wgrad (4.9 TB/s): bound by the
 // weights' bytes.  Few rows: ten rows of a hundred experts 7 us (21 MB of weights), eight of eight experts in 8 bits 26 us (90 MB).
 #include "group_tiles.h"
 #include "lds_copy.h"

@@ -2,7 +2,7 @@
 //
 //   sum = round(x + residual), inv = 1 / sqrt(mean(sum^2) + eps), y = sum * inv * gain
 //
-// Bound by memory: one pass over x and residual, six operations an element; bf16 on an MI355X: 16384 x 4096 into 8 bits 85 us (5.5 TB/s), 6400 x 2048 forward 21 us and
+// Bound by memory: one pass over x and residual, six operations an element; bf16 on an MI355X: 16384 x 4096 into 8 bits 81 us (5.8 TB/s), 6400 x 2048 forward 21 us and
 // gradient 26 us from cold memory (5.1 and 4.1 TB/s; a plain copy 4.9), four rows of 1024 3.2 us.  A row is held in registers between the sum of its squares and
 // its output, by one wave (rows up to 2048 elements, where no barrier is needed), a block of four waves, or one of sixteen; rows beyond
 // 32768 elements (16384 in the gradient) are read a second time.
@@ -41,7 +41,7 @@ struct NormArgs {
 
 // Results of more bytes than this go past the caches, which would not hold them all for their reader (bf16 with the sum, us through the caches and past them:
 // 16384 x 4096 94.6, 76.2, into 8 bits 86.7, 70.3; 65536 x 512 48.5, 39.5; 12000 x 2048 37.5, 34.3; a norm and two products of four experts on 16384 x 4096
-// 950, 942).  Smaller ones stay for it (norm and products of eight experts of 128 rows of 1024: 34.4, past the caches 36.9).
+// 950, 942; the gradient of 40000 x 1024 58.7, 50.5, of 16384 x 4096 98, 96).  Smaller ones stay for it (norm and products of eight experts of 128 rows of 1024: 34.4, past the caches 36.9).
 constexpr long long PAST_CACHES = 64 << 20;
 
 template <typename T, bool VEC>
@@ -193,7 +193,7 @@ __device__ __forceinline__ void unpack(const Raw<T>& r, float (&v)[E]) {
 
 // A row's share of the gain's gradient stays in its lanes' registers over all rows of the wave, and the next row is loaded while this one is worked on (both launches of 6400 x 2048 in bf16: 47.9 -> 28.8 us); four
 // waves of one row each are joined at the end.
-template <typename T, int WAVES, int CHUNKS, bool VEC>
+template <typename T, int WAVES, int CHUNKS, bool VEC, bool PAST>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_back_kernel(NormBackArgs a) {
   __shared__ float scratch[WAVES == 1 ? 4 * 64 * E : WAVES];
   const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_back_kerne
       unpack<T>(now.ds[c], d);
 #pragma unroll
       for (int i = 0; i < E; ++i) d[i] += now.inv * (h[c][i] - s[c][i] * k);
-      store8<T, VEC>((T*)a.dx + row * a.dx_stride + col, a.cols - col, d);
+      store8<T, VEC, PAST>((T*)a.dx + row * a.dx_stride + col, a.cols - col, d);
     }
   }
   if (!a.partial) return;
@@ -342,10 +342,10 @@ int back_blocks(long long rows, int cols) {
   return (int)(blocks < most ? blocks : most);
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool PAST>
 void launch_back(const NormBackArgs& a, hipStream_t st) {
   const unsigned blocks = (unsigned)back_blocks(a.rows, a.cols);
-#define GAN_BACK(W, C) hipLaunchKernelGGL((norm_back_kernel<T, W, C, VEC>), dim3(blocks), dim3(W == 1 ? 256 : 64 * W), 0, st, a)
+#define GAN_BACK(W, C) hipLaunchKernelGGL((norm_back_kernel<T, W, C, VEC, PAST>), dim3(blocks), dim3(W == 1 ? 256 : 64 * W), 0, st, a)
   // (bf16, 6400 x 1024: 17.1 us with a wave a row, 20.1 with four; fp32, 4000 x 2048: 32.8 us with four, 36.7 with one)
   if (a.cols <= 512) GAN_BACK(1, 1);
   else if (a.cols <= 1024) GAN_BACK(1, 2);
@@ -445,8 +445,14 @@ extern "C" gan_status gan_rms_norm_backward(int32_t precision, const void* dy, i
     const bool vec = cols % E == 0 && rows_aligned16(dy, dy_stride, e) && rows_aligned16(sum, sum_stride, e) && (!dsum || rows_aligned16(dsum, dsum_stride, e)) &&
                      rows_aligned16(dx, dx_stride, e) && aligned16(gain);
     const NormBackArgs a = {dy, sum, dsum, gain, inv_rms, dx, dgain ? (float*)work : nullptr, dy_stride, sum_stride, dsum_stride, dx_stride, rows, cols};
-    if (precision == GAN_FP32) vec ? launch_back<float, true>(a, st) : launch_back<float, false>(a, st);
-    else vec ? launch_back<bf16_t, true>(a, st) : launch_back<bf16_t, false>(a, st);
+    const auto go = [&](auto t) {
+      typedef decltype(t) T;
+      if (!vec) launch_back<T, false, false>(a, st);
+      else if (rows * cols * e > PAST_CACHES) launch_back<T, true, true>(a, st);
+      else launch_back<T, true, false>(a, st);
+    };
+    if (precision == GAN_FP32) go(float());
+    else go(bf16_t());
   }
   if (dgain)
     hipLaunchKernelGGL(gain_sum_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, (const float*)work, dgain, rows > 0 ? back_blocks(rows, cols) : 0, cols);

@@ -199,3 +199,31 @@ def test_in_place(cols):
     B.rms_norm_backward(B.BF16, ty.data_ptr(), cols, tx.data_ptr(), cols, tg.data_ptr(), tinv.data_ptr(), tr.data_ptr(), cols, 5, cols, ty.data_ptr(), cols,
                         dg2.data_ptr(), work.data_ptr(), n)
     assert torch.equal(dx, ty) and torch.equal(dg, dg2)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("cols", [512, 1536, 4096, 8192, 16384, 40000])
+def test_results_of_many_megabytes_are_those_of_each_row(cols, bf16):
+    """Twelve rows again and again, more than 64 MiB of them: each has the bits that a call on the twelve gives, forward, into 8 bits and backward."""
+    torch = U.torch_mod()
+    kind, e, n = (torch.bfloat16, 2, 12) if bf16 else (torch.float32, 4, 12)
+    times = 80 * 2 ** 20 // (n * cols * e) + 1
+    x, r, gain = inputs(n, cols, bf16, 4)
+    dy = U.round_to(np.random.default_rng(cols).normal(size=(n, cols)), bf16)
+    g = torch.from_numpy(gain).cuda()
+
+    def run(times):
+        rows, wide = n * times, R.padded(cols)
+        tx, tr, tdy = (torch.from_numpy(a).to(kind).cuda().repeat(times, 1) for a in (x, r, dy))
+        s, y, dx = (torch.full_like(tx, float("nan")) for _ in range(3))
+        q, sc = (torch.full(k, 77, dtype=torch.uint8, device="cuda") for k in ((rows, wide), (rows, wide // 128)))
+        inv = torch.zeros(rows, device="cuda")
+        precision = B.BF16 if bf16 else B.FP32
+        B.rms_norm(precision, tx.data_ptr(), cols, tr.data_ptr(), cols, g.data_ptr(), EPS, rows, cols, s.data_ptr(), cols, y.data_ptr(), cols, q.data_ptr(),
+                   sc.data_ptr(), inv.data_ptr())
+        B.rms_norm_backward(precision, tdy.data_ptr(), cols, s.data_ptr(), cols, g.data_ptr(), inv.data_ptr(), tr.data_ptr(), cols, rows, cols, dx.data_ptr(),
+                            cols, 0, 0, 0)
+        return s, y, q, sc, inv, dx
+
+    for one, many in zip(run(1), run(times)):
+        assert bool((many.view(times, *one.shape) == one).all())
