@@ -11,7 +11,7 @@
 // Times on an MI355X (its library's product of 8192^3: 1.34 PFLOP/s in bf16; a copy: 4.9 TB/s).  bf16 tiles: 8192^3 as one expert 1.26-1.37 PFLOP/s, forward, dgrad and wgrad, 1.35
 // from 8 bits: bound by the matrix pipe and the clock that its power leaves (its share of the cycles at eight experts of 2048 rows, 4096 -> 4096: 0.55; LDS
 // bank conflicts, all from the stores, 3 % of its cycles).  With drawn sizes of 2048 rows on average 478 us, where the experts' last tiles cost a tenth (equal experts: 437), and 456 from 8 bits; weight gradient 493-509, of which
-// 537 MB of fp32 results are 110.  A hundred experts of unequal sizes, 1024 -> 1024, cold weights: 78 us forward, 48 dgrad (weights cached), 90 wgrad (4.9 TB/s): bound by the
+// 537 MB of fp32 results are 110.  A hundred experts of unequal sizes, 1024 -> 1024, cold weights: 57 us forward, 49 dgrad, 95 wgrad (4.7 TB/s): bound by the
 // weights' bytes.  Few rows: ten rows of a hundred experts 7 us (21 MB of weights), eight of eight experts in 8 bits 26 us (90 MB).
 #include "group_tiles.h"
 #include "lds_copy.h"
@@ -983,7 +983,7 @@ gan_status launch_tiles(const LinearArgs& q, hipStream_t st) {
 
 // 256 x 256 tiles where they fill the CUs and experts have more than 32 rows on average, 128 x 128 where not.  Both sides, us on an MI355X from cold memory (256, 128):
 // 32 experts of 128 rows, 2048 -> 2048, forward 77, 97; 64 of 47, 1024 -> 1024, dgrad 31, 34; 128 of 14, 2361 -> 384, 8 bits 59, 43; four of 175, 4096 -> 4096 (64 tiles
-// of 256), forward 100, 67; weight gradient of 64 experts, 2816 -> 512: 109, 138.  Where those leave about one block to a CU and the sum is long, two sets of waves take half of
+// of 256), forward 100, 67; weight gradient of 64 experts, 2816 -> 512: 109, 138 (through the caches).  Where those leave about one block to a CU and the sum is long, two sets of waves take half of
 // it each (without, with): one expert of 1000 rows, 4096 -> 4096: 62, 53, in 8 bits 60, 43; one of 600, 1024 -> 1024: 16.9, 14.2; ten of 128, 512 -> 1024 (8 steps): 11.7, 11.8.
 template <Form F, int KIND, typename C>
 gan_status launch_large(const LinearArgs& q, hipStream_t st) {
