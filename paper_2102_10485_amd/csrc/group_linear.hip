@@ -1023,13 +1023,19 @@ gan_status launch_few_dgrad(const LinearArgs& q, int sixteens, hipStream_t st) {
 
 // Sixteens of rows for the kernel for few rows, or 0 where tiles are faster: up to 8 rows an expert, whose weights then are the time (a hundred experts of 4 rows,
 // 1024 -> 1024, forward: 43 us, 45 in 128 x 128 tiles; one row of one, 4096 -> 4096: 7.5, 37), and where there are few outputs (one expert of 200 rows, 4096 -> 1024: 18 us, 49;
-// four of 175, 4096 -> 4096: 171, 66).  In fp32 wherever 128 x 128 tiles would leave CUs idle (ten experts of 111 rows, 6272 -> 110: 48 us, 674; 512 -> 784: 23, 38).
+// four of 175, 4096 -> 4096: 171, 66).
+// In fp32 (us by this kernel, in tiles) up to 24 rows an expert forward (16 experts of 25, 2048 -> 2048: 76, 93; a hundred of 24, 1024 -> 1024: 122, 122; 32 of 29,
+// 640 -> 2176: 82, 62) and up to 32 in dgrad (a hundred of 24: 107, 121; 32 of 29, 640 <- 2176: 69, 91).  Beyond, where 64 x 64 tiles are few, forward: four of 100, 2048 -> 2048
+// (320 tiles): 64, 73; 32 of 25, 512 -> 512 (352): 16, 19.5; four of 175, 2048 -> 2048 (480): 94, 81; two of 1000, 1024 -> 1024 (530): 62, 44.  And where 128 x 128 tiles
+// are few in dgrad, whose columns this kernel reads more widely: ten of 111, 110 <- 6272: 47, 222; eight of 244, 1024 <- 2808 (184): 132, 153; ten of 640, 784 <- 512 (420): 71, 53.
 int few_rows(const LinearArgs& q, int kind, int esize) {
   const long long each = q.rows / most_groups(q);
   // short sums of many outputs give the waves little to share (128 experts of 3.5 rows, 256 -> 896: 32 us, 21 in tiles; fp32, eight of 128, 64 -> 896: 15.3, 5.6)
   if (q.k < 512 && (few_blocks(q) > 1024 || (esize == 4 && each > 8))) return 0;
   if (each <= 8) return 1;
-  if (esize == 4) return tiles(q, 128, 128) < 256 ? (kind == DGRAD ? 1 : 2) : 0;
+  if (esize == 4 && kind == DGRAD) return each <= 32 || tiles(q, 128, 128) < 256 ? 1 : 0;
+  // (twelve rows each of a hundred, 1024 -> 1024: 103 us by sixteens, 113 by 32; twenty: 104, 87)
+  if (esize == 4) return each <= 12 ? 1 : each <= 24 || tiles(q, 64, 64) <= 384 ? 2 : 0;
   return (long long)q.rows * q.n <= 1 << 19 ? 2 : 0;
 }
 
