@@ -13,6 +13,7 @@
 // bank conflicts, all from the stores, 3 % of its cycles).  With drawn sizes of 2048 rows on average 478 us, where the experts' last tiles cost a tenth (equal experts: 437), and 456 from 8 bits; weight gradient 493-509, of which
 // 537 MB of fp32 results are 110.  A hundred experts of unequal sizes, 1024 -> 1024, cold weights: 57 us forward, 49 dgrad, 95 wgrad (4.7 TB/s): bound by the
 // weights' bytes.  Few rows: ten rows of a hundred experts 7 us (21 MB of weights), eight of eight experts in 8 bits 26 us (90 MB).
+#include "code_walk.h"
 #include "group_tiles.h"
 #include "lds_copy.h"
 #include "operators.h"
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(256, RT == 128 ? 2 : 4) void linear_fp32_kernel(Lin
 // no multiples of 16 bytes go through registers, and so do 8-bit ones, where a code times its block's power of two becomes the bf16 number that it is: every product is exact and every sum fp32.
 // (The 8-bit MFMAs would take half the matrix-pipe time, but they add eight neighbouring products with what lies 2^-13 below the largest of them
 // cut off (2^16 + 2^2 is 2^16): 1.5e-5 of the result's norm on normal values, 5e-5 on codes of all sizes.)
-constexpr int STEP = 64;
+constexpr int STEP = CODE_STEP;
 
 // One operand's tile: R rows (or columns) of it, NW waves copying.
 template <bool KMAJOR, int R, int NW>
@@ -444,7 +445,7 @@ struct Converted : Tile<true, R, NW> {
   int byte[CHUNKS];
   __amdgpu_buffer_rsrc_t codes, scales;
   unsigned off[CHUNKS], scale_off[CHUNKS];
-  int k, first;                                                   // of the step that is asked for next, and of the first
+  CodeWalk walk;
 
   __device__ __forceinline__ void prepare(const T* base, const uint8_t* scale, long long stride, int row0, int rows, int k0, int k_end, int) {
     const long long blocks = stride / BLOCK8;
@@ -456,15 +457,15 @@ struct Converted : Tile<true, R, NW> {
       off[p] = r < rows ? (unsigned)(r * stride) + thread() % 4 * 16 : NO_ROW;
       scale_off[p] = r < rows ? (unsigned)(r * blocks) : NO_ROW;
     }
-    k = first = k0;
+    walk.start(k0);
 #pragma unroll
     for (int p = 0; p < CHUNKS; ++p) ask(p);
-    k += STEP;
+    walk.started(k_end);
   }
   __device__ __forceinline__ void ask(int p) {
-    // (behind the last step: the first again, which is not used)
-    q[p] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)off[p], k, 0));
-    byte[p] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_off[p], k / BLOCK8, 0);
+    // (the scalar part of an offset is outside the buffer's bounds check: walk.k itself stays in the row)
+    q[p] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)off[p], walk.k, 0));
+    byte[p] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_off[p], walk.k / BLOCK8, 0);
   }
   __device__ __forceinline__ void next_step() {}
   __device__ __forceinline__ void piece(int p, int, int left, unsigned char* lds, unsigned) {
@@ -482,7 +483,7 @@ struct Converted : Tile<true, R, NW> {
     *reinterpret_cast<u32x4*>(lds + r * 128 + ((c ^ S::swap_of(r)) * 16)) = lo;
     *reinterpret_cast<u32x4*>(lds + r * 128 + (((c + 1) ^ S::swap_of(r)) * 16)) = hi;
     ask(p);
-    if (p == CHUNKS - 1) k = left > 2 * STEP ? k + STEP : first;
+    if (p == CHUNKS - 1) walk.asked(left);
   }
 };
 
