@@ -139,3 +139,45 @@ def test_weights_and_rows_beyond_4_gib(rows):
     far[:, :n_in] = 3
     B.rms_norm(B.BF16, far.data_ptr(), stride, 0, 0, gain.data_ptr(), 0.0, 64, n_in, 0, 0, z.data_ptr(), n_in, 0, 0, inv.data_ptr())
     assert bool((z == 1).all()) and np.allclose(inv.cpu().numpy(), 1 / 3, rtol=1e-6)
+
+
+# Next to many whole tiles of 256, experts' last rows are taken in half the columns by two sets of waves, which share the sum: sums of one step (the second set has none), of two,
+# three and five, outputs that end eight or sixteen columns behind a tile, and rows that end anywhere in a half or a quarter of the height.
+ENDS = [([2580, 2404], 40, 3208), ([2580, 2404], 72, 3208), ([2580, 2404], 136, 3216), ([2561, 2432], 264, 3208), ([2624, 0, 2369], 128, 3208)]
+NO_EXPERT = 5
+
+
+def assert_ends_are_narrow(counts, rows, width):
+    """The rules of the launch, on the same counts: 256 x 256 tiles, and ends of at most a quarter of the whole tiles' number."""
+    assert (rows // 256 + len(counts)) * -(-width // 256) >= 256 and rows // len(counts) > 32
+    rest = [n % 256 for n in counts + [NO_EXPERT]]
+    whole = sum(n // 256 for n in counts + [NO_EXPERT]) + sum(r > 128 for r in rest)
+    half, low = sum(64 < r <= 128 for r in rest), sum(0 < r <= 64 for r in rest)
+    assert half > 0 and low > 0 and 4 * (half + low) <= whole
+
+
+@pytest.mark.parametrize("counts,short,wide", ENDS)
+def test_ends_in_half_the_columns(counts, short, wide):
+    offs, groups = offsets(counts), len(counts)
+    rows = offs[-1] + NO_EXPERT
+    assert_ends_are_narrow(counts, rows, wide)
+    rng = np.random.default_rng([short, wide])
+    a, w = (rng.integers(-2, 3, s).astype(np.float32) for s in ((rows, short), (groups, wide, short)))
+    want = U.round_to(R.linear(a, w, offs)[0].astype(np.float32), True)
+    assert np.array_equal(run("y", True, a, w, offs, groups, short, wide), want)
+    assert np.array_equal(run("dx", True, a, w.transpose(0, 2, 1).copy(), offs, groups, wide, short), want)
+    # what is not finite in the last expert's last row reaches that row alone
+    a[offs[-1] - 1, short - 1] = np.nan
+    for got in (run("y", True, a, w, offs, groups, short, wide), run("dx", True, a, w.transpose(0, 2, 1).copy(), offs, groups, wide, short)):
+        assert np.isnan(got[offs[-1] - 1]).all() and np.array_equal(np.delete(got, offs[-1] - 1, 0), np.delete(want, offs[-1] - 1, 0))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("counts,short,wide", ENDS)
+def test_ends_in_half_the_columns_in_eight_bits(counts, short, wide, bf16):
+    offs = offsets(counts)
+    assert_ends_are_narrow(counts, offs[-1] + NO_EXPERT, wide)
+    x8, xs, w8, ws = problem8(offs, short, wide, NO_EXPERT)
+    y, size = R.linear(R.decode(x8, xs), R.decode(w8, ws), offs)
+    got = run8(x8, xs, w8, ws, offs, short, wide, bf16)
+    assert np.all(np.abs(got - y) <= (R.padded(short) + 1) * R.U32 * size + (R.UBF * np.abs(y) if bf16 else 0))
