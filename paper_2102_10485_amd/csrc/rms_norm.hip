@@ -136,11 +136,39 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
   }
 }
 
+// A launch has fewer than 2^32 threads (the runtime takes more of them modulo 2^32, without an error): `go` is called for as many rows at a time, `waves` waves each, by their
+// first and their number.
+template <typename F>
+void by_launches(long long rows, int waves, F&& go) {
+  const long long most = (1ll << 31) / (64 * waves);
+  for (long long first = 0; first < rows; first += most) go(first, rows - first < most ? rows - first : most);
+}
+
+template <typename T>
+NormArgs rows_of(NormArgs a, long long first, long long rows) {
+  const long long wide = padded8(a.cols);
+  a.x = (const T*)a.x + first * a.x_stride;
+  if (a.residual) a.residual = (const T*)a.residual + first * a.residual_stride;
+  if (a.sum) a.sum = (T*)a.sum + first * a.sum_stride;
+  if (a.y) a.y = (T*)a.y + first * a.y_stride;
+  if (a.y8) a.y8 += first * wide, a.y8_scale += first * (wide / BLOCK8);
+  if (a.inv_rms) a.inv_rms += first;
+  a.rows = rows;
+  return a;
+}
+
+template <typename T, int WAVES, int CHUNKS, bool VEC, bool PAST>
+void launch_norm_as(const NormArgs& a, hipStream_t st) {
+  by_launches(a.rows, WAVES, [&](long long first, long long rows) {
+    hipLaunchKernelGGL((norm_kernel<T, WAVES, CHUNKS, VEC, PAST>), dim3((unsigned)(WAVES == 1 ? (rows + 3) / 4 : rows)), dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, st,
+                       rows_of<T>(a, first, rows));
+  });
+}
+
 template <typename T, bool VEC, bool PAST>
 void launch_norm(const NormArgs& a, hipStream_t st) {
   const long long cols = a.cols;
-  const unsigned rows = (unsigned)a.rows, by4 = (unsigned)((a.rows + 3) / 4);
-#define GAN_NORM(W, C) hipLaunchKernelGGL((norm_kernel<T, W, C, VEC, PAST>), dim3(W == 1 ? by4 : rows), dim3(W == 1 ? 256 : 64 * W), 0, st, a)
+#define GAN_NORM(W, C) launch_norm_as<T, W, C, VEC, PAST>(a, st)
   // Times on an MI355X.  Up to 1024 elements a wave per row has no barrier (bf16, 6400 x 1024: 13.5 us, four waves a row 15.6), but few rows
   // are done sooner by more waves (fp32, 1117 x 1000: 6.4 and 6.0).  Above, one chunk a lane is faster than more of them in fewer waves (bf16, 6400 x 2048: 22.8 us by four
   // waves, 28.7 by one; 4096 x 8192: 48.6 by sixteen, 52.9 by four).
@@ -151,7 +179,10 @@ void launch_norm(const NormArgs& a, hipStream_t st) {
   else if (cols <= 8192) GAN_NORM(16, 1);
   else if (cols <= 16384) GAN_NORM(16, 2);
   else if (cols <= 32768) GAN_NORM(16, 4);
-  else hipLaunchKernelGGL((norm_long_kernel<T, VEC>), dim3(rows), dim3(1024), 0, st, a);
+  else
+    by_launches(a.rows, 16, [&](long long first, long long rows) {
+      hipLaunchKernelGGL((norm_long_kernel<T, VEC>), dim3((unsigned)rows), dim3(1024), 0, st, rows_of<T>(a, first, rows));
+    });
 #undef GAN_NORM
 }
 
@@ -356,7 +387,16 @@ void launch_back(const NormBackArgs& a, hipStream_t st) {
   else {
     // (the gain's gradient first: dx may be the memory of dy)
     if (a.partial) hipLaunchKernelGGL(gain_long_kernel<T>, dim3((a.cols + 255) / 256, blocks), dim3(256), 0, st, a);
-    hipLaunchKernelGGL((norm_back_long_kernel<T, VEC>), dim3((unsigned)a.rows), dim3(1024), 0, st, a);
+    by_launches(a.rows, 16, [&](long long first, long long rows) {
+      NormBackArgs some = a;
+      some.dy = (const T*)a.dy + first * a.dy_stride;
+      some.sum = (const T*)a.sum + first * a.sum_stride;
+      if (a.dsum) some.dsum = (const T*)a.dsum + first * a.dsum_stride;
+      some.dx = (T*)a.dx + first * a.dx_stride;
+      some.inv_rms += first;
+      some.rows = rows;
+      hipLaunchKernelGGL((norm_back_long_kernel<T, VEC>), dim3((unsigned)rows), dim3(1024), 0, st, some);
+    });
   }
 #undef GAN_BACK
 }

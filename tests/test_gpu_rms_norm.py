@@ -227,3 +227,47 @@ def test_results_of_many_megabytes_are_those_of_each_row(cols, bf16):
 
     for one, many in zip(run(1), run(times)):
         assert bool((many.view(times, *one.shape) == one).all())
+
+
+@pytest.mark.parametrize("bits,cols", [(26, 8), (24, 1032), (22, 4104)])
+def test_more_rows_than_a_launch_has_threads_for(bits, cols):
+    """2^26 rows of a wave, 2^24 of four and 2^22 of sixteen are 2^32 threads, more than one launch can have.  The same 1021 rows again and again, y over x (34 GB of
+    the longer rows): each has the bits that a call on them alone gives; codes and scales of the shortest too."""
+    torch = U.torch_mod()
+    n = 1021
+    times = (1 << bits) // n + 2
+    x, _, gain = inputs(n, cols, True, 6)
+    g = torch.from_numpy(gain).cuda()
+
+    def run(times):
+        rows, wide, eight = n * times, R.padded(cols), cols < 128
+        t = torch.empty((times, n, cols), dtype=torch.bfloat16, device="cuda")
+        t[:] = torch.from_numpy(x).cuda().bfloat16()
+        inv = torch.zeros((times, n), device="cuda")
+        q, sc = (torch.full((times, n, k), 77, dtype=torch.uint8, device="cuda") if eight else None for k in (wide, wide // 128))
+        B.rms_norm(B.BF16, t.data_ptr(), cols, 0, 0, g.data_ptr(), EPS, rows, cols, 0, 0, t.data_ptr(), cols, q.data_ptr() if eight else 0,
+                   sc.data_ptr() if eight else 0, inv.data_ptr())
+        return [t, inv] + ([q, sc] if eight else [])
+
+    for one, many in zip(run(1), run(times)):
+        for k in range(0, times, 4096):
+            assert bool((many[k:k + 4096] == one).all())
+
+
+def test_gradient_of_more_rows_than_a_launch_has_threads_for():
+    """The gradient of 2^26 rows, its sums by column included: the same rows again and again, whole numbers of which the sums are exact."""
+    torch = U.torch_mod()
+    cols, rows = 8, (1 << 26) + 5
+    s = torch.full((rows, cols), 2.0, dtype=torch.bfloat16, device="cuda")
+    dy = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    dy[::4099, 3] = 1.0
+    inv, g, dg, n = torch.full((rows,), 0.5, device="cuda"), torch.ones(cols, device="cuda"), torch.zeros(cols, device="cuda"), B.rms_norm_backward_bytes(rows, cols)
+    work = torch.empty(n, dtype=torch.uint8, device="cuda")
+    B.rms_norm_backward(B.BF16, dy.data_ptr(), cols, s.data_ptr(), cols, g.data_ptr(), inv.data_ptr(), 0, 0, rows, cols, dy.data_ptr(), cols, dg.data_ptr(),
+                        work.data_ptr(), n)
+    want = np.zeros(cols)
+    want[3] = -(-rows // 4099)
+    assert np.array_equal(dg.cpu().numpy(), want)
+    # inv * (h - s * inv^2 * mean(h s)) = (h - 1/8) / 2 in the rows that have a gradient
+    row = torch.tensor([-0.0625] * 3 + [0.4375] + [-0.0625] * 4, device="cuda").bfloat16()
+    assert bool((dy[::4099] == row).all()) and int((dy != 0).sum()) == 8 * int(want[3])
