@@ -39,7 +39,11 @@ struct LinearArgs {
   int m, n, k;                                 // wgrad: m = outputs, n = inputs; else n, k (m: the expert's rows; wgrad: k)
   int parts;                                   // wgrad: an expert's rows are shared by this many blocks, whose results follow one another at `part` elements
   long long part;
+  unsigned first;                              // of the launch's tiles among the call's
 };
+
+// The block's number among all of the call's.
+__device__ __forceinline__ unsigned block_of(const LinearArgs& q) { return q.first + blockIdx.x; }
 
 // ---- fp32 ----
 //
@@ -179,10 +183,11 @@ __global__ __launch_bounds__(256, RT == 128 ? 2 : 4) void linear_fp32_kernel(Lin
   __shared__ __align__(16) unsigned char lds[2 * 3 * RT * RK * 2];
   unsigned char *la = lds, *lb = lds + 3 * RT * RK * 2;
 
-  const int n_tiles = (q.n + RT - 1) / RT, n0 = (int)(blockIdx.x % n_tiles) * RT;
+  const unsigned block = block_of(q);
+  const int n_tiles = (q.n + RT - 1) / RT, n0 = (int)(block % n_tiles) * RT;
   int group, m0, m_end, k_begin = 0, k_end = q.k, part = 0;
   if (KIND == WGRAD) {
-    const int m_tiles = (q.m + RT - 1) / RT, t = blockIdx.x / n_tiles, e = t / m_tiles;
+    const int m_tiles = (q.m + RT - 1) / RT, t = block / n_tiles, e = t / m_tiles;
     part = e % q.parts;
     group = e / q.parts;
     m0 = t % m_tiles * RT;
@@ -190,7 +195,7 @@ __global__ __launch_bounds__(256, RT == 128 ? 2 : 4) void linear_fp32_kernel(Lin
     group_rows(q.offs, q.groups, q.rows, group, k_begin, k_end);
     part_of(part, q.parts, k_begin, k_end);
   } else {
-    if (!find_tile(q.offs, q.groups, q.rows, RT, blockIdx.x / n_tiles, group, m0, m_end)) return;
+    if (!find_tile(q.offs, q.groups, q.rows, RT, block / n_tiles, group, m0, m_end)) return;
     if (group == q.groups) k_end = 0;                             // rows of no expert: zeros
   }
   const float* a = (const float*)q.a;
@@ -644,7 +649,7 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void linear_kernel(LinearA
   unsigned count[SORTS];
   count_tiles(q.offs, q.groups, q.rows, BM, count);
   const bool narrow = P::NARROW && 4 * (count[HALF] + count[LOW]) <= count[WHOLE] + count[HIGH];
-  const unsigned cols = (unsigned)(q.n + BN - 1) / BN, end_cols = narrow ? (unsigned)(q.n + BN / 2 - 1) / (BN / 2) : cols, xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
+  const unsigned cols = (unsigned)(q.n + BN - 1) / BN, end_cols = narrow ? (unsigned)(q.n + BN / 2 - 1) / (BN / 2) : cols, block = block_of(q), xcd = block & 7, i = block >> 3;
   const unsigned full = (count[WHOLE] + count[HIGH]) * cols, share = (full + 7) / 8;
   unsigned r, c, id = i < share ? xcd * share + i : (i - share) * 8 + xcd;
   int sort;
@@ -684,11 +689,12 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void linear_kernel(LinearA
 template <Form F, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, 2) void linear_wgrad_kernel(LinearArgs q) {
   extern __shared__ __align__(1024) unsigned char lds[];
-  const int n_tiles = (q.n + BN - 1) / BN, m_tiles = (q.m + BM - 1) / BM, t = blockIdx.x / n_tiles, e = t / m_tiles, group = e / q.parts, part = e % q.parts;
+  const unsigned block = block_of(q);
+  const int n_tiles = (q.n + BN - 1) / BN, m_tiles = (q.m + BM - 1) / BM, t = block / n_tiles, e = t / m_tiles, group = e / q.parts, part = e % q.parts;
   int begin, end;
   group_rows(q.offs, q.groups, q.rows, group, begin, end);
   part_of(part, q.parts, begin, end);
-  tile_product<F, WGRAD, BM, BN, WM, WN, Shapes<F, BM, BN, WM, WN, 1>::S, 1, float>(q, lds, group, part, t % m_tiles * BM, q.m, (int)(blockIdx.x % n_tiles) * BN, begin, end);
+  tile_product<F, WGRAD, BM, BN, WM, WN, Shapes<F, BM, BN, WM, WN, 1>::S, 1, float>(q, lds, group, part, t % m_tiles * BM, q.m, (int)(block % n_tiles) * BN, begin, end);
 }
 
 // dw = the parts, added in order
@@ -765,9 +771,10 @@ template <typename T, int TM, int JT, int U, int NW, bool ANY_ROWS, typename C>
 __global__ __launch_bounds__(64 * NW) void linear_few_kernel(LinearArgs q) {
   constexpr int EACH = Few<T>::EACH, DEEP = Few<T>::DEEP, ES = (int)sizeof(T);
   const int cols = (q.n + 16 * JT - 1) / (16 * JT);
-  const int column = (int)(blockIdx.x % cols), n0 = column * 16 * JT;
+  const unsigned block = block_of(q);
+  const int column = (int)(block % cols), n0 = column * 16 * JT;
   int group, m0, m_end;
-  if (!find_tile(q.offs, q.groups, q.rows, 16 * TM, blockIdx.x / cols, group, m0, m_end)) return;
+  if (!find_tile(q.offs, q.groups, q.rows, 16 * TM, block / cols, group, m0, m_end)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   floatx4 acc[TM * JT];
 #pragma unroll
@@ -871,9 +878,10 @@ template <typename T, int TM, int U, int NW, bool ANY_ROWS>
 __global__ __launch_bounds__(64 * NW) void linear_few_dgrad_kernel(LinearArgs q) {
   constexpr int EACH = Few<T>::EACH, DEEP = Few<T>::DEEP, ES = (int)sizeof(T), BN = 16 * EACH;
   const int cols = (q.n + BN - 1) / BN;
-  const int n0 = (int)(blockIdx.x % cols) * BN;
+  const unsigned block = block_of(q);
+  const int n0 = (int)(block % cols) * BN;
   int group, m0, m_end;
-  if (!find_tile(q.offs, q.groups, q.rows, 16 * TM, blockIdx.x / cols, group, m0, m_end)) return;
+  if (!find_tile(q.offs, q.groups, q.rows, 16 * TM, block / cols, group, m0, m_end)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   floatx4 acc[TM * EACH];
 #pragma unroll
@@ -954,13 +962,18 @@ __global__ __launch_bounds__(64 * NW) void linear_few_dgrad_kernel(LinearArgs q)
 
 constexpr long long MOST_BLOCKS = 0x7fffffff;
 
-gan_status launch(void (*kernel)(LinearArgs), long long blocks, int threads, int lds, const LinearArgs& q, hipStream_t st) {
+// A launch has fewer than 2^32 threads (the runtime takes more of them modulo 2^32, without an error): blocks beyond go to another, in eights, which keep their XCDs.
+gan_status launch(void (*kernel)(LinearArgs), long long blocks, int threads, int lds, LinearArgs q, hipStream_t st) {
   if (blocks > MOST_BLOCKS) return operator_fail(GAN_E_SHAPE, "more than 2^31 - 1 tiles");
   if (lds > 65536 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) {
     (void)hipGetLastError();
     return operator_fail(GAN_E_HIP, "the kernel's LDS could not be set");
   }
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, st, q);
+  const long long most = (1ll << 31) / threads;
+  for (long long first = 0; first < blocks; first += most) {
+    q.first = (unsigned)first;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(most, blocks - first)), dim3(threads), lds, st, q);
+  }
   return operator_launched();
 }
 
@@ -1078,7 +1091,7 @@ extern "C" gan_status gan_group_linear(int32_t precision, const void* x, int64_t
   if (x_stride < n_in || y_stride < n_out) return operator_fail(GAN_E_ARG, "x_stride is below n_in, or y_stride below n_out");
   if (rows == 0) return GAN_OK;
   const int e = precision == GAN_FP32 ? 4 : 2;
-  const LinearArgs q = {x, w, nullptr, nullptr, y, offs, x_stride, n_in, y_stride, (long long)n_in * n_out, 0, groups, (int)rows, 0, n_out, n_in, 1, 0};
+  const LinearArgs q = {x, w, nullptr, nullptr, y, offs, x_stride, n_in, y_stride, (long long)n_in * n_out, 0, groups, (int)rows, 0, n_out, n_in, 1, 0, 0};
   const hipStream_t st = (hipStream_t)hip_stream;
   const bool small = short_rows(x_stride, e) && short_rows(n_in, e), aligned = small && n_in % 8 == 0 && rows_aligned16(x, x_stride, e) && aligned16(w);
   const int few = few_rows(q, FORWARD, e);
@@ -1093,7 +1106,7 @@ extern "C" gan_status gan_group_linear_dgrad(int32_t precision, const void* dy, 
   if (dy_stride < n_out || dx_stride < n_in) return operator_fail(GAN_E_ARG, "dy_stride is below n_out, or dx_stride below n_in");
   if (rows == 0) return GAN_OK;
   const int e = precision == GAN_FP32 ? 4 : 2;
-  const LinearArgs q = {dy, w, nullptr, nullptr, dx, offs, dy_stride, n_in, dx_stride, (long long)n_in * n_out, 0, groups, (int)rows, 0, n_in, n_out, 1, 0};
+  const LinearArgs q = {dy, w, nullptr, nullptr, dx, offs, dy_stride, n_in, dx_stride, (long long)n_in * n_out, 0, groups, (int)rows, 0, n_in, n_out, 1, 0, 0};
   const hipStream_t st = (hipStream_t)hip_stream;
   const bool small = short_rows(dy_stride, e) && short_rows(n_in, e), aligned = small && n_out % 8 == 0 && n_in % 8 == 0 && rows_aligned16(dy, dy_stride, e) && aligned16(w);
   const int few = small && (long long)n_in * n_out * e < 1ll << 31 ? few_rows(q, DGRAD, e) : 0;
@@ -1117,7 +1130,7 @@ extern "C" gan_status gan_group_linear_wgrad(int32_t precision, const void* x, i
   if (groups == 0) return GAN_OK;
   const int e = precision == GAN_FP32 ? 4 : 2, parts = rows > 0 ? wgrad_parts(groups, rows, n_in, n_out) : 1;
   const long long n = (long long)groups * n_in * n_out;
-  const LinearArgs q = {dy, x, nullptr, nullptr, parts > 1 ? work : dw, offs, dy_stride, x_stride, n_in, 0, (long long)n_in * n_out, groups, (int)rows, n_out, n_in, 0, parts, n};
+  const LinearArgs q = {dy, x, nullptr, nullptr, parts > 1 ? work : dw, offs, dy_stride, x_stride, n_in, 0, (long long)n_in * n_out, groups, (int)rows, n_out, n_in, 0, parts, n, 0};
   const hipStream_t st = (hipStream_t)hip_stream;
   const bool aligned = short_rows(x_stride, e) && short_rows(dy_stride, e) && n_in % 8 == 0 && n_out % 8 == 0 && rows_aligned16(x, x_stride, e) && rows_aligned16(dy, dy_stride, e);
   const gan_status s = precision == GAN_FP32 ? launch_fp32(WGRAD, q, st) : aligned ? launch_large<ALIGNED, WGRAD, float>(q, st) : launch_large<ANY, WGRAD, float>(q, st);
@@ -1135,7 +1148,7 @@ extern "C" gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scal
   const long long k = padded8(n_in);
   if (!short_rows(k, 1)) return operator_fail(GAN_E_SHAPE, "more than 2^22 inputs in 8 bits");
   if (rows == 0) return GAN_OK;
-  const LinearArgs q = {x8, w8, x_scale, w_scale, y, offs, k, k, y_stride, k * n_out, 0, groups, (int)rows, 0, n_out, (int)k, 1, 0};
+  const LinearArgs q = {x8, w8, x_scale, w_scale, y, offs, k, k, y_stride, k * n_out, 0, groups, (int)rows, 0, n_out, (int)k, 1, 0, 0};
   const hipStream_t st = (hipStream_t)hip_stream;
   if (const int few = few_rows(q, FORWARD, 1))
     return y_precision == GAN_FP32 ? launch_few<uint8_t, false, float>(q, few, st) : launch_few<uint8_t, false, bf16_t>(q, few, st);

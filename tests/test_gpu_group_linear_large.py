@@ -181,3 +181,22 @@ def test_ends_in_half_the_columns_in_eight_bits(counts, short, wide, bf16):
     y, size = R.linear(R.decode(x8, xs), R.decode(w8, ws), offs)
     got = run8(x8, xs, w8, ws, offs, short, wide, bf16)
     assert np.all(np.abs(got - y) <= (R.padded(short) + 1) * R.U32 * size + (R.UBF * np.abs(y) if bf16 else 0))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_more_tiles_than_a_launch_has_threads_for(bf16):
+    """2050 experts of 2^20 outputs and one input: 2^24 tiles and more of 256 threads each.  Whole numbers; experts without rows get zeros."""
+    torch = U.torch_mod()
+    groups, n_out, kind = 2050, 1 << 20, torch.bfloat16 if bf16 else torch.float32
+    starts = np.zeros(groups + 1, np.int32)
+    starts[1:], starts[1025:], starts[2050:] = 2, 3, 5                # two rows of the first expert, one of the 1025th, two of the last
+    x = torch.tensor([[1.0], [2.0], [3.0], [1.0], [-1.0]], device="cuda").to(kind)
+    dy = torch.randint(-2, 3, (5, n_out), device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(kind)
+    dw = torch.full((groups, n_out), float("nan"), device="cuda")
+    nbytes = B.group_linear_wgrad_bytes(groups, 5, 1, n_out)
+    offs = torch.from_numpy(starts).cuda()
+    B.group_linear_wgrad(B.BF16 if bf16 else B.FP32, x.data_ptr(), 1, dy.data_ptr(), n_out, offs.data_ptr(), groups, 5, 1, n_out, dw.data_ptr(), 0, nbytes)
+    f = dy.float()
+    assert nbytes == 0 and torch.equal(dw[0], f[0] + 2 * f[1]) and torch.equal(dw[1024], 3 * f[2]) and torch.equal(dw[2049], f[3] - f[4])
+    for lo, hi in ((1, 1024), (1025, 2049)):
+        assert int(dw[lo:hi].count_nonzero()) == 0 and not bool(dw[lo:hi].isnan().any())
