@@ -136,12 +136,12 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
   }
 }
 
-// A launch has fewer than 2^32 threads (the runtime takes more of them modulo 2^32, without an error): `go` is called for as many rows at a time, `waves` waves each, by their
-// first and their number.
+// A launch has fewer than 2^32 threads (the runtime takes more of them modulo 2^32, without an error): `go` is called with the first of `count` shares of `waves` waves each,
+// and with how many of them a launch takes.
 template <typename F>
-void by_launches(long long rows, int waves, F&& go) {
+void by_launches(long long count, int waves, F&& go) {
   const long long most = (1ll << 31) / (64 * waves);
-  for (long long first = 0; first < rows; first += most) go(first, rows - first < most ? rows - first : most);
+  for (long long first = 0; first < count; first += most) go(first, count - first < most ? count - first : most);
 }
 
 template <typename T>
@@ -342,9 +342,9 @@ __global__ __launch_bounds__(256) void gain_long_kernel(NormBackArgs a) {
 }
 
 // dgain[c] = the blocks' partial sums, added in 32 chains that are joined in order; eight loads of a chain in flight
-__global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, float* dgain, int blocks, int cols) {
+__global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, float* dgain, int blocks, int cols, int first_col) {
   __shared__ float part[32][33];
-  const int c = threadIdx.x & 31, k = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+  const int c = threadIdx.x & 31, k = threadIdx.x >> 5, col = first_col + blockIdx.x * 32 + c;
   float d = 0.f;
   if (col < cols)
     for (int b = k; b < blocks; b += 256) {
@@ -495,7 +495,9 @@ extern "C" gan_status gan_rms_norm_backward(int32_t precision, const void* dy, i
     else go(bf16_t());
   }
   if (dgain)
-    hipLaunchKernelGGL(gain_sum_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, (const float*)work, dgain, rows > 0 ? back_blocks(rows, cols) : 0, cols);
+    by_launches((cols + 31) / 32, 16, [&](long long first, long long blocks) {
+      hipLaunchKernelGGL(gain_sum_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)work, dgain, rows > 0 ? back_blocks(rows, cols) : 0, cols, (int)first * 32);
+    });
   return operator_launched();
 }
 

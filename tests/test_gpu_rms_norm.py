@@ -271,3 +271,18 @@ def test_gradient_of_more_rows_than_a_launch_has_threads_for():
     # inv * (h - s * inv^2 * mean(h s)) = (h - 1/8) / 2 in the rows that have a gradient
     row = torch.tensor([-0.0625] * 3 + [0.4375] + [-0.0625] * 4, device="cuda").bfloat16()
     assert bool((dy[::4099] == row).all()) and int((dy != 0).sum()) == 8 * int(want[3])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_gain_of_more_columns_than_a_launch_has_threads_for(bf16):
+    """2^27 columns and some: 32 columns a block of 1024 threads are 2^32 threads and more.  Whole numbers: sums are exact."""
+    torch = U.torch_mod()
+    cols, kind = (1 << 27) + 40, torch.bfloat16 if bf16 else torch.float32
+    s, inv = torch.full((2, cols), 2.0, device="cuda").to(kind), torch.tensor([0.5, 0.25], device="cuda")
+    dy = (torch.arange(2 * cols, device="cuda") % 8).view(2, cols).to(kind)
+    gain, dx, dg = torch.zeros(cols, device="cuda"), torch.zeros((2, cols), device="cuda").to(kind), torch.full((cols,), float("nan"), device="cuda")
+    n = B.rms_norm_backward_bytes(2, cols)
+    work = torch.empty(n, dtype=torch.uint8, device="cuda")
+    B.rms_norm_backward(B.BF16 if bf16 else B.FP32, dy.data_ptr(), cols, s.data_ptr(), cols, gain.data_ptr(), inv.data_ptr(), 0, 0, 2, cols, dx.data_ptr(), cols,
+                        dg.data_ptr(), work.data_ptr(), n)
+    assert torch.equal(dg, dy[0].float() + 0.5 * dy[1].float()) and not bool(dx.any())
