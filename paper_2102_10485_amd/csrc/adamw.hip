@@ -215,7 +215,7 @@ extern "C" gan_status gan_adamw_step(gan_adamw* h, double lr, double beta1, doub
     return operator_fail(GAN_E_ARG, "a beta outside [0, 1), a negative eps or lr, or a step below 1");
   if (h->n_chunks == 0) return GAN_OK;
   StepArgs a;
-  a.tensors = h->tensors; a.chunks = h->chunks;
+  a.tensors = h->tensors;
   a.m = h->m; a.v = h->v; a.m_scale = h->m_scale; a.v_scale = h->v_scale;
   a.lr = (float)lr;
   a.b1 = (float)beta1; a.one_minus_b1 = (float)(1 - beta1);
@@ -225,13 +225,18 @@ extern "C" gan_status gan_adamw_step(gan_adamw* h, double lr, double beta1, doub
   a.step_size = (float)(lr / (1 - pow(beta1, (double)step)));
   a.key = seed + (unsigned)step * 0x9E3779B9u;
   const hipStream_t st = (hipStream_t)hip_stream;
-  const dim3 grid((unsigned)h->n_chunks), block(256);
-  if (h->bf16_grads) {
-    if (h->eight) hipLaunchKernelGGL((adamw_kernel<bf16_t, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((adamw_kernel<bf16_t, false>), grid, block, 0, st, a);
-  } else {
-    if (h->eight) hipLaunchKernelGGL((adamw_kernel<float, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((adamw_kernel<float, false>), grid, block, 0, st, a);
+  // a launch has fewer than 2^32 threads (the runtime takes more of them modulo 2^32, without an error): 2^23 chunks at a time
+  constexpr long long MOST = 1 << 23;
+  for (long long first = 0; first < h->n_chunks; first += MOST) {
+    a.chunks = h->chunks + first;
+    const dim3 grid((unsigned)(h->n_chunks - first < MOST ? h->n_chunks - first : MOST)), block(256);
+    if (h->bf16_grads) {
+      if (h->eight) hipLaunchKernelGGL((adamw_kernel<bf16_t, true>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((adamw_kernel<bf16_t, false>), grid, block, 0, st, a);
+    } else {
+      if (h->eight) hipLaunchKernelGGL((adamw_kernel<float, true>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((adamw_kernel<float, false>), grid, block, 0, st, a);
+    }
   }
   return operator_launched();
 }

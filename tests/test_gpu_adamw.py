@@ -159,3 +159,26 @@ def test_moments_beyond_2_to_the_32():
     assert np.array_equal(m[first:].cpu().numpy(), want[1]) and np.array_equal(v[first:].cpu().numpy(), want[2])
     assert np.array_equal(ms[first // 128:].cpu().numpy(), want[3]) and np.array_equal(vs[first // 128:].cpu().numpy(), want[4])
     assert float(p[-1]) < 0 and not bool(p[-2])                      # only the value that has a gradient moved
+
+
+def test_more_tensors_than_a_launch_has_threads_for():
+    """2^24 + 5 tensors of one value: a block of 256 threads each, 2^32 threads and more.  Bit for bit, as everywhere here."""
+    import ctypes
+    torch = U.torch_mod()
+    n = (1 << 24) + 5
+    rng = np.random.default_rng(4)
+    p, g = rng.normal(size=n).astype(np.float32), rng.normal(size=n).astype(np.float32)
+    tp, tg = torch.from_numpy(p).cuda(), torch.from_numpy(g).cuda()
+    m, v = (torch.zeros((n, 128), device="cuda") for _ in range(2))
+    at = np.arange(n, dtype=np.int64) * 4
+    sizes, pp, pg = np.ones(n, np.int64), at + tp.data_ptr(), at + tg.data_ptr()
+    as_pointers = lambda a: a.ctypes.data_as(ctypes.POINTER(ctypes.c_void_p))  # noqa: E731
+    lib, h = B.load_library(), ctypes.c_void_p()
+    B._operator(lib.gan_adamw_create(n, sizes.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)), as_pointers(pp), as_pointers(pg), B.FP32, None, None, 32, m.data_ptr(),
+                                     v.data_ptr(), None, None, ctypes.byref(h)))
+    B._operator(lib.gan_adamw_step(h, HYPER["lr"], HYPER["beta1"], HYPER["beta2"], HYPER["eps"], 1, 5, None))
+    B._operator(lib.gan_adamw_destroy(h))
+    want = R.adamw(p, g, np.zeros(n, np.float32), np.zeros(n, np.float32), None, None, 0.0, step=1, seed=5, eight=False, first=0, **HYPER)
+    assert np.array_equal(tp.cpu().numpy(), want[0])
+    assert np.array_equal(m[:, 0].cpu().numpy(), want[1]) and np.array_equal(v[:, 0].cpu().numpy(), want[2])
+    assert int(m.count_nonzero()) == np.count_nonzero(want[1])
