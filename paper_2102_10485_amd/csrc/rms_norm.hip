@@ -55,10 +55,11 @@ __device__ __forceinline__ void add_rounded(float (&v)[E], const T* residual, in
 template <typename T, bool VEC, bool PAST>
 __device__ __forceinline__ void write_chunk(const NormArgs& a, long long row, int col, const float (&s)[E], float inv) {
   float g[E], y[E];
-  load8<float, VEC>(a.gain + col, a.cols - col, g);
+  const int left = a.cols - col;
+  load8<float, VEC>(a.gain + col, left, g);
 #pragma unroll
-  for (int i = 0; i < E; ++i) y[i] = s[i] * inv * g[i];
-  if (a.y) store8<T, VEC, PAST>((T*)a.y + row * a.y_stride + col, a.cols - col, y);
+  for (int i = 0; i < E; ++i) y[i] = (VEC ? left > 0 : i < left) ? s[i] * inv * g[i] : 0.f;       // (behind the row inv may be NaN or infinite, and the codes are zero)
+  if (a.y) store8<T, VEC, PAST>((T*)a.y + row * a.y_stride + col, left, y);
   if (a.y8) {                                                     // the sixteen lanes of a block of 128 are here together, or none is
     const long long padded = padded8(a.cols);
     const int byte = scale_byte(y);

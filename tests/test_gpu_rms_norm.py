@@ -286,3 +286,20 @@ def test_gain_of_more_columns_than_a_launch_has_threads_for(bf16):
     B.rms_norm_backward(B.BF16 if bf16 else B.FP32, dy.data_ptr(), cols, s.data_ptr(), cols, gain.data_ptr(), inv.data_ptr(), 0, 0, 2, cols, dx.data_ptr(), cols,
                         dg.data_ptr(), work.data_ptr(), n)
     assert torch.equal(dg, dy[0].float() + 0.5 * dy[1].float()) and not bool(dx.any())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("cols", [1, 96, 129, 1000, 1032, 4104, 16392, 40001])
+def test_padding_is_zero_whatever_the_row_holds(cols, bf16):
+    """A row with a NaN, one with an infinity, and (eps 0) one of zeros, whose norm is 0/0: codes behind the last column are zero in all of them."""
+    torch = U.torch_mod()
+    x, _, gain = inputs(4, cols, bf16, 3)
+    x[0, cols // 2], x[1, 0], x[2] = np.nan, np.inf, 0
+    wide, g = R.padded(cols), torch.from_numpy(gain).cuda()
+    for pad, offset in ((0, 0), (3, 1)):
+        _, view, p = matrix(x, bf16, cols + pad, offset)
+        q, sc = (torch.full(s, 77, dtype=torch.uint8, device="cuda") for s in ((4, wide), (4, wide // 128)))
+        B.rms_norm(B.BF16 if bf16 else B.FP32, p, cols + pad, 0, 0, g.data_ptr(), 0.0, 4, cols, 0, 0, 0, 0, q.data_ptr(), sc.data_ptr(), 0)
+        q, sc = q.cpu().numpy(), sc.cpu().numpy()
+        assert not q[:, cols:].any()
+        assert np.all(q[[0, 2], :cols] & 0x7F == 0x7F) and q[1, 0] & 0x7F == 0x7F and np.all(np.isfinite(R.decode(q, sc)[3]))
