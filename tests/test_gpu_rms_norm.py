@@ -303,3 +303,21 @@ def test_padding_is_zero_whatever_the_row_holds(cols, bf16):
         q, sc = q.cpu().numpy(), sc.cpu().numpy()
         assert not q[:, cols:].any()
         assert np.all(q[[0, 2], :cols] & 0x7F == 0x7F) and q[1, 0] & 0x7F == 0x7F and np.all(np.isfinite(R.decode(q, sc)[3]))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("cols", [96, 1000, 4096, 16392])
+def test_backward_of_tiny_rows(cols, bf16):
+    """Without eps, rows of 1e-20 have inv_rms of 1e20, whose square is no fp32 number; their gradient is.  Bounds as in test_backward."""
+    torch = U.torch_mod()
+    s, _, gain = inputs(3, cols, bf16, 8)
+    s = U.round_to(s * np.float32(1e-20), bf16)
+    dy = U.round_to(np.random.default_rng(cols).normal(size=s.shape), bf16)
+    edx, edg, size, gsize = R.norm_backward(dy, s, gain, 0.0, None)
+    inv = torch.from_numpy((1 / np.sqrt((s.astype(np.float64) ** 2).mean(1))).astype(np.float32)).cuda()
+    ms, mdy, mdx = (matrix(a, bf16, cols) for a in (s, dy, np.zeros_like(s)))
+    g, dg, n = torch.from_numpy(gain).cuda(), torch.zeros(cols, device="cuda"), B.rms_norm_backward_bytes(3, cols)
+    work = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    B.rms_norm_backward(B.BF16 if bf16 else B.FP32, mdy[2], cols, ms[2], cols, g.data_ptr(), inv.data_ptr(), 0, 0, 3, cols, mdx[2], cols, dg.data_ptr(), work.data_ptr(), n)
+    assert np.all(np.abs(host(mdx[1]) - edx) <= 64 * R.U32 * size + (R.UBF * np.abs(edx) if bf16 else 0))
+    assert np.all(np.abs(dg.cpu().numpy() - edg) <= (3 + 4 + 64 + 4) * R.U32 * gsize)
