@@ -318,7 +318,8 @@ gan_status gan_op_dw4_to_dw3(gan_ctx* ctx, const float* dw4, float* dw3, int32_t
    type: GAN_FP32, or GAN_BF16_FP32MASTER for bf16 matrices; sums and statistics are fp32.
    Every call enqueues its kernels on hip_stream (a hipStream_t of the current device, 0 = the null stream) and returns
    without waiting; nothing is allocated or kept, so calls may be captured into a graph.  Every sum runs in an order
-   fixed by sizes and offsets: results are the same bit for bit from run to run.  Zero rows or zero groups are valid.
+   fixed by sizes and offsets: results are the same bit for bit from run to run.  Zero rows or zero groups are valid, and a matrix
+   without elements may be NULL.
    Refusals (GAN_E_ARG, GAN_E_SHAPE) come before anything is launched; gan_operator_last_error has the reason (text of the calling
    thread's last failed call, never NULL).
 

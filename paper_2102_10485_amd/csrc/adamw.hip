@@ -164,10 +164,12 @@ extern "C" gan_status gan_adamw_create(int32_t tensors, const int64_t* sizes, fl
                                        gan_adamw** out) {
   if (!out) return operator_fail(GAN_E_ARG, "out is NULL");
   *out = nullptr;
-  if (tensors < 1 || !sizes || !params || !grads || !m || !v) return operator_fail(GAN_E_ARG, "no tensors, or sizes, params, grads, m or v is NULL");
+  if (tensors < 1 || !sizes || !params || !grads) return operator_fail(GAN_E_ARG, "no tensors, or sizes, params or grads is NULL");
+  const bool any = gan_adamw_blocks(tensors, sizes) > 0;           // (tensors without values have no moments)
+  if (any && (!m || !v)) return operator_fail(GAN_E_ARG, "m or v is NULL");
   if (grad_precision != GAN_FP32 && grad_precision != GAN_BF16_FP32MASTER) return operator_fail(GAN_E_ARG, "unknown precision");
   if (state_bits != 32 && state_bits != 8) return operator_fail(GAN_E_ARG, "state_bits is neither 32 nor 8");
-  if ((state_bits == 8) != (m_scale != nullptr) || (state_bits == 8) != (v_scale != nullptr))
+  if (state_bits == 8 ? any && (!m_scale || !v_scale) : m_scale || v_scale)
     return operator_fail(GAN_E_ARG, "m_scale and v_scale go with state_bits 8");
   if (!aligned16(m) || !aligned16(v)) return operator_fail(GAN_E_ARG, "m or v is not 16-byte aligned");
   try {

@@ -1069,9 +1069,10 @@ int wgrad_parts(int groups, long long rows, int n_in, int n_out) {
   return (int)std::max(1ll, std::min({512 / std::max(1ll, blocks), each / 256, 64ll}));
 }
 
-gan_status check(int32_t precision, const void* x, const void* w, const int32_t* offs, int32_t groups, int64_t rows, int32_t n_in, int32_t n_out, const void* out) {
+// by_row: the two matrices that have `rows` rows; by_group: the one of `groups` matrices.  What has no elements may be NULL.
+gan_status check(int32_t precision, const void* by_row0, const void* by_row1, const void* by_group, const int32_t* offs, int32_t groups, int64_t rows, int32_t n_in, int32_t n_out) {
   if (precision != GAN_FP32 && precision != GAN_BF16_FP32MASTER) return operator_fail(GAN_E_ARG, "unknown precision");
-  if (!x || !w || !offs || !out) return operator_fail(GAN_E_ARG, "an operand is NULL");
+  if ((rows > 0 && (!by_row0 || !by_row1)) || (groups > 0 && !by_group) || !offs) return operator_fail(GAN_E_ARG, "an operand is NULL");
   if (groups < 0 || rows < 0 || n_in < 1 || n_out < 1) return operator_fail(GAN_E_ARG, "negative groups or rows, or no inputs or outputs");
   if (groups > 65535 || rows > 1 << 30 || n_in > 1 << 28 || n_out > 1 << 28) return operator_fail(GAN_E_SHAPE, "more than 65535 groups, 2^30 rows, or 2^28 inputs or outputs");
   return GAN_OK;
@@ -1087,7 +1088,7 @@ using namespace gan;
 
 extern "C" gan_status gan_group_linear(int32_t precision, const void* x, int64_t x_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows,
                                        int32_t n_in, int32_t n_out, void* y, int64_t y_stride, void* hip_stream) {
-  if (const gan_status s = check(precision, x, w, offs, groups, rows, n_in, n_out, y)) return s;
+  if (const gan_status s = check(precision, x, y, w, offs, groups, rows, n_in, n_out)) return s;
   if (x_stride < n_in || y_stride < n_out) return operator_fail(GAN_E_ARG, "x_stride is below n_in, or y_stride below n_out");
   if (rows == 0) return GAN_OK;
   const int e = precision == GAN_FP32 ? 4 : 2;
@@ -1102,7 +1103,7 @@ extern "C" gan_status gan_group_linear(int32_t precision, const void* x, int64_t
 
 extern "C" gan_status gan_group_linear_dgrad(int32_t precision, const void* dy, int64_t dy_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows,
                                              int32_t n_in, int32_t n_out, void* dx, int64_t dx_stride, void* hip_stream) {
-  if (const gan_status s = check(precision, dy, w, offs, groups, rows, n_in, n_out, dx)) return s;
+  if (const gan_status s = check(precision, dy, dx, w, offs, groups, rows, n_in, n_out)) return s;
   if (dy_stride < n_out || dx_stride < n_in) return operator_fail(GAN_E_ARG, "dy_stride is below n_out, or dx_stride below n_in");
   if (rows == 0) return GAN_OK;
   const int e = precision == GAN_FP32 ? 4 : 2;
@@ -1123,7 +1124,7 @@ extern "C" int64_t gan_group_linear_wgrad_bytes(int32_t groups, int64_t rows, in
 
 extern "C" gan_status gan_group_linear_wgrad(int32_t precision, const void* x, int64_t x_stride, const void* dy, int64_t dy_stride, const int32_t* offs,
                                              int32_t groups, int64_t rows, int32_t n_in, int32_t n_out, float* dw, void* work, int64_t work_bytes, void* hip_stream) {
-  if (const gan_status s = check(precision, x, dy, offs, groups, rows, n_in, n_out, dw)) return s;
+  if (const gan_status s = check(precision, x, dy, dw, offs, groups, rows, n_in, n_out)) return s;
   if (x_stride < n_in || dy_stride < n_out) return operator_fail(GAN_E_ARG, "x_stride is below n_in, or dy_stride below n_out");
   const int64_t need = gan_group_linear_wgrad_bytes(groups, rows, n_in, n_out);
   if (work_bytes < need || (need > 0 && !work) || !aligned16(work)) return operator_fail(GAN_E_ARG, "work is smaller than gan_group_linear_wgrad_bytes, or not 16-byte aligned");
@@ -1141,8 +1142,8 @@ extern "C" gan_status gan_group_linear_wgrad(int32_t precision, const void* x, i
 
 extern "C" gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scale, const uint8_t* w8, const uint8_t* w_scale, const int32_t* offs, int32_t groups,
                                         int64_t rows, int32_t n_in, int32_t n_out, int32_t y_precision, void* y, int64_t y_stride, void* hip_stream) {
-  if (const gan_status s = check(y_precision, x8, w8, offs, groups, rows, n_in, n_out, y)) return s;
-  if (!x_scale || !w_scale) return operator_fail(GAN_E_ARG, "x_scale or w_scale is NULL");
+  if (const gan_status s = check(y_precision, x8, y, w8, offs, groups, rows, n_in, n_out)) return s;
+  if ((rows > 0 && !x_scale) || (groups > 0 && !w_scale)) return operator_fail(GAN_E_ARG, "x_scale or w_scale is NULL");
   if (!aligned16(x8) || !aligned16(w8)) return operator_fail(GAN_E_ARG, "x8 or w8 is not 16-byte aligned");
   if (y_stride < n_out) return operator_fail(GAN_E_ARG, "y_stride is below n_out");
   const long long k = padded8(n_in);

@@ -442,7 +442,7 @@ extern "C" gan_status gan_rms_norm(int32_t precision, const void* x, int64_t x_s
                                    float eps, int64_t rows, int32_t cols, void* sum, int64_t sum_stride, void* y, int64_t y_stride, uint8_t* y8,
                                    uint8_t* y8_scale, float* inv_rms, void* hip_stream) {
   if (const gan_status s = check_sizes(precision, rows, cols)) return s;
-  if (!x || !gain) return operator_fail(GAN_E_ARG, "x or gain is NULL");
+  if ((rows > 0 && !x) || !gain) return operator_fail(GAN_E_ARG, "x or gain is NULL");
   if (!y8 != !y8_scale) return operator_fail(GAN_E_ARG, "y8 and y8_scale go together");
   if (!aligned16(y8)) return operator_fail(GAN_E_ARG, "y8 is not 16-byte aligned");
   if (!(eps >= 0.f)) return operator_fail(GAN_E_ARG, "eps is negative");
@@ -475,7 +475,7 @@ extern "C" gan_status gan_rms_norm_backward(int32_t precision, const void* dy, i
                                             const float* inv_rms, const void* dsum, int64_t dsum_stride, int64_t rows, int32_t cols, void* dx,
                                             int64_t dx_stride, float* dgain, void* work, int64_t work_bytes, void* hip_stream) {
   if (const gan_status s = check_sizes(precision, rows, cols)) return s;
-  if (!dy || !sum || !gain || !inv_rms || !dx) return operator_fail(GAN_E_ARG, "dy, sum, gain, inv_rms or dx is NULL");
+  if ((rows > 0 && (!dy || !sum || !inv_rms || !dx)) || !gain) return operator_fail(GAN_E_ARG, "dy, sum, gain, inv_rms or dx is NULL");
   for (const gan_status s : {check_matrix(dy, dy_stride, cols, "dy_stride is below cols"), check_matrix(sum, sum_stride, cols, "sum_stride is below cols"),
                              check_matrix(dsum, dsum_stride, cols, "dsum_stride is below cols"), check_matrix(dx, dx_stride, cols, "dx_stride is below cols")})
     if (s) return s;
@@ -505,7 +505,7 @@ extern "C" gan_status gan_rms_norm_backward(int32_t precision, const void* dy, i
 
 extern "C" gan_status gan_quantize8(int32_t precision, const void* x, int64_t x_stride, int64_t rows, int32_t cols, uint8_t* q, uint8_t* scale, void* hip_stream) {
   if (const gan_status s = check_sizes(precision, rows, cols)) return s;
-  if (!x || !q || !scale) return operator_fail(GAN_E_ARG, "x, q or scale is NULL");
+  if (rows > 0 && (!x || !q || !scale)) return operator_fail(GAN_E_ARG, "x, q or scale is NULL");
   if (!aligned16(q)) return operator_fail(GAN_E_ARG, "q is not 16-byte aligned");
   if (const gan_status s = check_matrix(x, x_stride, cols, "x_stride is below cols")) return s;
   if (rows == 0) return GAN_OK;
