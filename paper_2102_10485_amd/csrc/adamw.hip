@@ -229,6 +229,7 @@ extern "C" gan_status gan_adamw_step(gan_adamw* h, double lr, double beta1, doub
   const hipStream_t st = (hipStream_t)hip_stream;
   // a launch has fewer than 2^32 threads (the runtime takes more of them modulo 2^32, without an error): 2^23 chunks at a time
   constexpr long long MOST = 1 << 23;
+  operator_launches();
   for (long long first = 0; first < h->n_chunks; first += MOST) {
     a.chunks = h->chunks + first;
     const dim3 grid((unsigned)(h->n_chunks - first < MOST ? h->n_chunks - first : MOST)), block(256);

@@ -970,6 +970,7 @@ gan_status launch(void (*kernel)(LinearArgs), long long blocks, int threads, int
     return operator_fail(GAN_E_HIP, "the kernel's LDS could not be set");
   }
   const long long most = (1ll << 31) / threads;
+  operator_launches();
   for (long long first = 0; first < blocks; first += most) {
     q.first = (unsigned)first;
     hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(most, blocks - first)), dim3(threads), lds, st, q);

@@ -7,6 +7,7 @@
 namespace gan {
 
 gan_status operator_fail(gan_status s, const char* why);          // records the calling thread's text and returns s
+void operator_launches();                                         // before a launch: what an earlier HIP call of the caller's left behind is not its failure
 gan_status operator_launched();                                   // GAN_OK, or GAN_E_HIP with the runtime's text
 
 constexpr int BLOCK8 = 128;                                       // neighbours that share a scale

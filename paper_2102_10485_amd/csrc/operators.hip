@@ -11,6 +11,8 @@ gan_status operator_fail(gan_status s, const char* why) {
   return s;
 }
 
+void operator_launches() { (void)hipGetLastError(); }
+
 gan_status operator_launched() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? GAN_OK : operator_fail(GAN_E_HIP, hipGetErrorString(e));

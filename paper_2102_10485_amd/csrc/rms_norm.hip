@@ -450,6 +450,7 @@ extern "C" gan_status gan_rms_norm(int32_t precision, const void* x, int64_t x_s
                              check_matrix(sum, sum_stride, cols, "sum_stride is below cols"), check_matrix(y, y_stride, cols, "y_stride is below cols")})
     if (s) return s;
   if (rows == 0) return GAN_OK;
+  operator_launches();
   const int e = precision == GAN_FP32 ? 4 : 2;
   const bool vec = cols % E == 0 && rows_aligned16(x, x_stride, e) && (!residual || rows_aligned16(residual, residual_stride, e)) && aligned16(gain) &&
                    (!sum || rows_aligned16(sum, sum_stride, e)) && (!y || rows_aligned16(y, y_stride, e));
@@ -481,6 +482,7 @@ extern "C" gan_status gan_rms_norm_backward(int32_t precision, const void* dy, i
     if (s) return s;
   if (dgain && (work_bytes < gan_rms_norm_backward_bytes(rows, cols) || (!work && rows > 0) || !aligned16(work)))
     return operator_fail(GAN_E_ARG, "work is smaller than gan_rms_norm_backward_bytes, or not 16-byte aligned");
+  operator_launches();
   const hipStream_t st = (hipStream_t)hip_stream;
   const int e = precision == GAN_FP32 ? 4 : 2;
   if (rows > 0) {
@@ -509,6 +511,7 @@ extern "C" gan_status gan_quantize8(int32_t precision, const void* x, int64_t x_
   if (!aligned16(q)) return operator_fail(GAN_E_ARG, "q is not 16-byte aligned");
   if (const gan_status s = check_matrix(x, x_stride, cols, "x_stride is below cols")) return s;
   if (rows == 0) return GAN_OK;
+  operator_launches();
   const int e = precision == GAN_FP32 ? 4 : 2;
   const bool vec = cols % E == 0 && rows_aligned16(x, x_stride, e);
   const long long want = (rows * (padded8(cols) / E) + 255) / 256;
