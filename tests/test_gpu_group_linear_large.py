@@ -200,3 +200,49 @@ def test_more_tiles_than_a_launch_has_threads_for(bf16):
     assert nbytes == 0 and torch.equal(dw[0], f[0] + 2 * f[1]) and torch.equal(dw[1024], 3 * f[2]) and torch.equal(dw[2049], f[3] - f[4])
     for lo, hi in ((1, 1024), (1025, 2049)):
         assert int(dw[lo:hi].count_nonzero()) == 0 and not bool(dw[lo:hi].isnan().any())
+
+
+# (rows fall unevenly, so that experts end inside tiles; the sizes take tiles of 64 and of 128)
+FP32_TILES = [([40, 0, 130, 90], 200, 136), ([1500, 1201], 333, 2056)]
+
+
+@pytest.mark.parametrize("counts,n_in,n_out", FP32_TILES)
+def test_fp32_values_that_are_not_finite_leave_other_outputs_alone(counts, n_in, n_out):
+    """The outputs that a NaN or an infinity is not summed into have the bits that they have without it; the others are what fp32 arithmetic gives."""
+    offs, groups = offsets(counts), len(counts)
+    rows = offs[-1]
+    rng = np.random.default_rng([n_in, n_out, 4])
+    x, w, dy = (rng.normal(size=s).astype(np.float32) for s in ((rows, n_in), (groups, n_out, n_in), (rows, n_out)))
+    clean = [run(k, False, a, b, offs, groups, n_in, n_out) for k, a, b in (("y", x, w), ("dx", dy, w), ("dw", x, dy))]
+    x[5, 3], x[rows - 1, n_in - 1], dy[7, 2], dy[rows - 2, 0] = np.nan, np.inf, -np.inf, np.nan
+    x[20, 1], x[21, 1], dy[20, 4], dy[21, 4] = np.inf, -np.inf, 1.0, 1.0               # (NaN where both are summed)
+    with np.errstate(invalid="ignore"):
+        want = R.linear(x, w, offs)[0], R.linear(dy, w.transpose(0, 2, 1), offs)[0], R.linear_wgrad(x, dy, offs, groups)[0]
+    touched = np.zeros((rows, 1), bool), np.zeros((rows, 1), bool), np.zeros((groups, n_out, n_in), bool)
+    touched[0][[5, rows - 1, 20, 21]] = touched[1][[7, rows - 2, 20, 21]] = True
+    touched[2][0, :, [1, 3]] = touched[2][-1, :, n_in - 1] = touched[2][0, [2, 4]] = touched[2][-1, 0] = True
+    for kind, a, b, old, ref, at in zip(("y", "dx", "dw"), (x, dy, x), (w, w, dy), clean, want, touched):
+        got = run(kind, False, a, b, offs, groups, n_in, n_out)
+        assert np.array_equal(np.where(at, 0, got), np.where(at, 0, old)), kind
+        assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(np.isinf(got), np.isinf(ref)), kind
+        assert np.array_equal(np.signbit(got[np.isinf(ref)]), np.signbit(ref[np.isinf(ref)])), kind
+
+
+@pytest.mark.parametrize("counts,n_in,n_out", FP32_TILES)
+def test_fp32_values_out_of_the_parts_range(counts, n_in, n_out):
+    """Rows of 1e33 and weights of 1e-30 and less, sums of 1e25 and more: what three bf16 parts cannot hold is summed in fp32."""
+    offs, groups = offsets(counts), len(counts)
+    rows = offs[-1]
+    rng = np.random.default_rng([n_in, n_out, 5])
+    x, w, dy = (rng.normal(size=s).astype(np.float32) for s in ((rows, n_in), (groups, n_out, n_in), (rows, n_out)))
+    x[::3] *= np.float32(1e33)
+    dy[1::5] *= np.float32(3e34)
+    w[0] *= np.float32(1e-30)
+    w[-1] *= np.float32(1e-8)
+    y, size = R.linear(x, w, offs)
+    assert np.all(np.abs(run("y", False, x, w, offs, groups, n_in, n_out) - y) <= (n_in + 1) * R.U32 * size)
+    dx, size = R.linear(dy, w.transpose(0, 2, 1), offs)
+    assert np.all(np.abs(run("dx", False, dy, w, offs, groups, n_in, n_out) - dx) <= (n_out + 1) * R.U32 * size)
+    dy = (rng.normal(size=dy.shape) * 1e-30).astype(np.float32)
+    dw, size = R.linear_wgrad(x, dy, offs, groups)
+    assert np.all(np.abs(run("dw", False, x, dy, offs, groups, n_in, n_out) - dw) <= (rows + 1) * R.U32 * size)
