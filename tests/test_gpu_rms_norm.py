@@ -321,3 +321,28 @@ def test_backward_of_tiny_rows(cols, bf16):
     B.rms_norm_backward(B.BF16 if bf16 else B.FP32, mdy[2], cols, ms[2], cols, g.data_ptr(), inv.data_ptr(), 0, 0, 3, cols, mdx[2], cols, dg.data_ptr(), work.data_ptr(), n)
     assert np.all(np.abs(host(mdx[1]) - edx) <= 64 * R.U32 * size + (R.UBF * np.abs(edx) if bf16 else 0))
     assert np.all(np.abs(dg.cpu().numpy() - edg) <= (3 + 4 + 64 + 4) * R.U32 * gsize)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("rows,cols", [(5003, 264), (5003, 1000), (3001, 1536), (1501, 2500), (1501, 8192), (701, 16384), (201, 16400)])
+def test_backward_of_several_rows_a_block(rows, cols, bf16):
+    """More rows than all blocks have at a time, in every form of the kernel, and not a multiple of them.  A lane adds the terms of its rows in a chain, four waves are joined where a
+    row is a wave's, and the blocks' partial sums are added in 32 chains that are joined; a term has four roundings."""
+    torch = U.torch_mod()
+    for pad, offset, with_dsum in ((0, 0, True), (3, 1, False)):
+        rng = np.random.default_rng([rows, cols, pad, 2])
+        s, _, gain = inputs(rows, cols, bf16, 11)
+        dy, ds = (U.round_to(rng.normal(size=(rows, cols)), bf16) for _ in range(2))
+        st, n = cols + pad, B.rms_norm_backward_bytes(rows, cols)
+        blocks, at_a_time = n // (4 * cols), 4 if cols <= 1024 else 1
+        chain = -(-rows // (blocks * at_a_time))
+        assert chain > 1 and rows % (blocks * at_a_time)
+        ms, mdy, mds, mdx = (matrix(a, bf16, st, offset) for a in (s, dy, ds, np.zeros_like(s)))
+        inv = torch.from_numpy((1 / np.sqrt((s.astype(np.float64) ** 2).mean(1) + EPS)).astype(np.float32)).cuda()
+        g, dg = torch.from_numpy(gain).cuda(), torch.full((cols,), float("nan"), device="cuda")
+        work = torch.full((n // 4,), float("nan"), device="cuda")
+        B.rms_norm_backward(B.BF16 if bf16 else B.FP32, mdy[2], st, ms[2], st, g.data_ptr(), inv.data_ptr(), mds[2] if with_dsum else 0, st, rows, cols, mdx[2], st,
+                            dg.data_ptr(), work.data_ptr(), n)
+        edx, edg, size, gsize = R.norm_backward(dy, s, gain, EPS, ds if with_dsum else None)
+        assert np.all(np.abs(host(mdx[1]) - edx) <= 64 * R.U32 * size + (R.UBF * np.abs(edx) if bf16 else 0))
+        assert np.all(np.abs(dg.cpu().numpy() - edg) <= (4 + chain + 4 + -(-blocks // 32) + 32) * R.U32 * gsize)
