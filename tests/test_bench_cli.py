@@ -37,3 +37,24 @@ def test_single_pair_goes_with_the_train_row_only():
     # the option is parsed before any device work; an unknown value is an argparse error
     r = run("--single-pair", "both")
     assert r.returncode != 0 and "invalid choice" in r.stderr
+
+
+def test_stored_traffic_belongs_to_the_steps_sources(tmp_path):
+    """The digest that the stored counters belong to follows every file that the step is compiled from, and no other: operators beside it do not void them."""
+    import re
+    import shutil
+    sys.path.insert(0, ROOT)
+    import bench
+    csrc = os.path.join(ROOT, "paper_2102_10485_amd", "csrc")
+    files = [f for f in os.listdir(csrc) if f.endswith((".hip", ".h"))]
+    for f in files:
+        shutil.copy(os.path.join(csrc, f), tmp_path)
+    digest = bench.sources_digest(str(tmp_path))
+    assert digest == bench.sources_digest() and bench.OPERATOR_SOURCES < set(files)
+    for f in files:
+        text = (tmp_path / f).read_text()
+        (tmp_path / f).write_text(text + "\n")
+        assert (bench.sources_digest(str(tmp_path)) == digest) == (f in bench.OPERATOR_SOURCES), f
+        (tmp_path / f).write_text(text)
+        if f not in bench.OPERATOR_SOURCES:                           # the step's files include none of the operators'
+            assert not set(re.findall(r'#include "([^"]+)"', text)) & bench.OPERATOR_SOURCES, f
