@@ -355,6 +355,8 @@ gan_status gan_quantize8(int32_t precision, const void* x, int64_t x_stride, int
      gan_group_linear_wgrad dw[g] = sum of dy[i]^T x[i] over g's i  fp32 [groups][n_out][n_in], zero for an expert without rows
      gan_group_linear8      y[i] = w[g] x[i] of 8-bit matrices: x8 [rows][padded n_in], w8 [groups][n_out][padded n_in]; y in y_precision
    fp32 products are sums of products of three bf16 parts of every value, as in the training step (or of fp32 values, where experts have few rows).
+   8-bit products take an element as the bf16 number nearest to it, which it is but for blocks of the two lowest E, where it is rounded to a multiple of
+   2^-133, and elements from 2^128 on (E of 120 and more), which are infinite; products and sums are fp32.
    work: DEVICE, gan_group_linear_wgrad_bytes(...) (0: none is needed, and work may be NULL), 16-byte aligned.  At most 65535 groups. */
 gan_status gan_group_linear(int32_t precision, const void* x, int64_t x_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows,
                             int32_t n_in, int32_t n_out, void* y, int64_t y_stride, void* hip_stream);

@@ -226,3 +226,28 @@ def test_eight_bits_after_the_norm():
     # independent roundings of at most 2^-4 each (and 2^-10 of the block's scale near zero) on both sides
     err = np.linalg.norm(y.cpu().numpy() - want) / np.linalg.norm(want)
     assert err <= np.sqrt(2) * 2.0 ** -4
+
+
+@pytest.mark.parametrize("rows_of_codes", [True, False])
+def test_eight_bits_of_the_smallest_and_the_largest_blocks(rows_of_codes):
+    """Every finite code in blocks of the lowest and the highest exponents against single weights.  An element counts as the bf16 number nearest to it: a multiple of 2^-133 (off by half
+    of that at most, and not at all from E = -124 on), and infinite from 2^128 on; products with one weight are exact, up to what fp32 holds."""
+    codes = np.array([c for c in range(256) if c & 127 != 127], np.uint8)
+    n, exponents = len(codes), np.array([-126, -125, -124, -123, 117, 118, 119, 120, 121, 127])
+    x8 = np.zeros((n * len(exponents), 128), np.uint8)
+    x8[:, 5] = np.tile(codes, len(exponents))
+    xs = np.repeat(exponents + 127, n).astype(np.uint8)[:, None]
+    value = R.TABLE[x8[:, 5]] * 2.0 ** (xs[:, 0].astype(np.float64) - 127)
+    for e in (110, -20):                                             # of the weights 1, 1.125 ... 3.75 times 2^e
+        w8, ws = np.zeros((1, 16, 128), np.uint8), np.full((1, 16, 1), 127 + e, np.uint8)
+        w8[0, :, 5] = 0x38 + np.arange(16)
+        w = R.decode(w8[0], ws[0])[:, 5]
+        got = run8(x8, xs, w8, ws, [0, len(x8)], 128, 16, False) if rows_of_codes else run8(w8[0], ws[0], x8[None], xs[None], [0, 16], 128, len(x8), False).T
+        with np.errstate(over="ignore", invalid="ignore"):
+            want = np.where(np.abs(value) < 2.0 ** 128, value, np.inf * np.sign(value))[:, None] * w
+            want = np.where(np.abs(want) < 2.0 ** 128, want, np.inf * np.sign(want))
+        off = np.where(np.abs(value) < 2.0 ** -122, 2.0 ** -134, 0.0) * (value % 2.0 ** -133 != 0)
+        near = np.isfinite(want)
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~near], want[~near])
+        error = np.abs(got[near].astype(np.float64) - want[near])
+        assert np.all(error <= (off[:, None] * np.abs(w))[near] + (2.0 ** -149 if e < 0 else 0.0)), (e, error.max())
