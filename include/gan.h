@@ -347,9 +347,10 @@ gan_status gan_rms_norm_backward(int32_t precision, const void* dy, int64_t dy_s
 /* A matrix into 8 bits: weights once, or activations that no norm precedes. */
 gan_status gan_quantize8(int32_t precision, const void* x, int64_t x_stride, int64_t rows, int32_t cols, uint8_t* q, uint8_t* scale, void* hip_stream);
 
-/* Products grouped by label: rows offs[g] .. offs[g+1] - 1 are expert g's.  offs: DEVICE int32 [groups + 1], not decreasing, offs[0] = 0 (as
-   gan_get_routing reports them; an entry below the one before it or outside [0, rows] counts as that one or as the nearest inside);
-   rows from offs[groups] on belong to no expert: their results are zero.  w [groups][n_out][n_in] in the storage type.
+/* Products grouped by label: rows offs[g] .. offs[g+1] - 1 are expert g's.  offs: DEVICE int32 [groups + 1], not decreasing, offs[0] = 0
+   (an entry below the one before it or outside [0, rows] counts as that one or as the nearest inside).  The layout is that of gan_get_routing, which
+   reports HOST memory and the routing of a DC-CGAN context's last step: a caller sorts rows by label and copies the offsets to the device itself.  Rows from
+   offs[groups] on belong to no expert: their results are zero.  w [groups][n_out][n_in] in the storage type.
      gan_group_linear       y[i] = w[g] x[i]                       [rows][n_out]
      gan_group_linear_dgrad dx[i] = dy[i] w[g]                     [rows][n_in]
      gan_group_linear_wgrad dw[g] = sum of dy[i]^T x[i] over g's i  fp32 [groups][n_out][n_in], zero for an expert without rows

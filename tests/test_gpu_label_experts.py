@@ -84,3 +84,28 @@ def test_the_step_in_a_graph_and_on_another_stream():
             assert torch.equal(eager.g[k], graphed.g[k]) and torch.equal(eager.p[k], graphed.p[k]), k
     for a, b in zip(eager.moments + eager.scales, graphed.moments + graphed.scales):
         assert torch.equal(a, b)
+
+
+def test_rows_sorted_by_a_training_steps_routing():
+    """The routing that a DC-CGAN context reports, on the host, sorts other rows of the same batch for the products: its offsets are copied to the device as they are.  Whole numbers."""
+    from paper_2102_10485_amd import binding as B
+    from paper_2102_10485_amd import synth
+    torch = U.torch_mod()
+    labels, n, n_in, n_out = 9, 300, 72, 40
+    rng = np.random.default_rng(8)
+    lab = rng.integers(0, labels, n).astype(np.int32)
+    lab[lab == 4] = 5                                                 # a label without rows
+    spec = synth.SPECS["tiny0"]
+    gan = B.Gan(B.make_config(spec, labels, labels, n, B.BF16), torch.cuda.current_stream().cuda_stream)
+    z, image = rng.normal(size=(n, spec["z_dim"])), np.tanh(rng.normal(size=(n, spec["img_c"], spec["img_hw"], spec["img_hw"])))
+    dl, dz, dimage = torch.from_numpy(lab).cuda(), torch.from_numpy(z.astype(np.float32)).cuda(), torch.from_numpy(image.astype(np.float32)).cuda()
+    gan.train_step(dl.data_ptr(), dz.data_ptr(), dimage.data_ptr(), n)
+    perm, offs = gan.get_routing(n)
+    gan.close()
+    x, w = rng.integers(-2, 3, (n, n_in)).astype(np.float32), rng.integers(-2, 3, (labels, n_out, n_in)).astype(np.float32)
+    tx, tw, to = torch.from_numpy(x[perm]).cuda().bfloat16(), torch.from_numpy(w).cuda().bfloat16(), torch.from_numpy(offs).cuda()
+    y = torch.empty((n, n_out), dtype=torch.bfloat16, device="cuda")
+    B.group_linear(B.BF16, tx.data_ptr(), n_in, tw.data_ptr(), to.data_ptr(), labels, n, n_in, n_out, y.data_ptr(), n_out)
+    got = np.empty((n, n_out), np.float32)
+    got[perm] = y.float().cpu().numpy()
+    assert np.array_equal(got, U.round_to(np.einsum("ni,noi->no", x, w[lab]), True))
