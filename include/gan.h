@@ -317,7 +317,7 @@ gan_status gan_op_dw4_to_dw3(gan_ctx* ctx, const float* dw4, float* dw3, int32_t
    16 bytes run faster), up to 2^30 rows and 2^28 elements a row; offsets into tensors are 64-bit.  `precision` is the storage
    type: GAN_FP32, or GAN_BF16_FP32MASTER for bf16 matrices; sums and statistics are fp32.
    Every call enqueues its kernels on hip_stream (a hipStream_t of the current device, 0 = the null stream) and returns
-   without waiting; nothing is allocated or kept, so calls may be captured into a graph.  Every sum runs in an order
+   without waiting; nothing is allocated or kept, so calls may be captured into a graph (of gan_adamw_step see below).  Every sum runs in an order
    fixed by sizes and offsets: results are the same bit for bit from run to run.  Zero rows or zero groups are valid, and a matrix
    without elements may be NULL.
    Refusals (GAN_E_ARG, GAN_E_SHAPE) come before anything is launched; gan_operator_last_error has the reason (text of the calling
@@ -378,6 +378,8 @@ gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scale, const ui
                     8-bit format above, rounded up or down with the probability of the part cut off (a step changes a moment by less than
                     half a code, which rounding to nearest would undo for ever): by floor(|x| / ulp + u / 65536), u = bits 0 .. 15 (m) and 16 .. 31
                     (v) of a 32-bit mix of the element's index in these arrays, the step number and the seed.  What is not zero never becomes zero in v.
+   What gan_adamw_step is given (lr, betas, eps, step, seed) is part of its launch.  Captured into a graph, every replay is that step again, with the same
+   bias corrections, rate and rounding bits (which then are no chance); a program that replays graphs calls it beside them, once a step.
    A step, with t = step >= 1, every operation rounded to fp32 on its own:
      m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
      p = p (1 - lr decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps) */

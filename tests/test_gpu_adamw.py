@@ -182,3 +182,29 @@ def test_more_tensors_than_a_launch_has_threads_for():
     assert np.array_equal(tp.cpu().numpy(), want[0])
     assert np.array_equal(m[:, 0].cpu().numpy(), want[1]) and np.array_equal(v[:, 0].cpu().numpy(), want[2])
     assert int(m.count_nonzero()) == np.count_nonzero(want[1])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_captured_step_is_that_step_again(bits):
+    """What gan.h says of a graph: a replay repeats the step that was captured, its rates and its rounding bits, on the moments and gradients as they are then."""
+    torch = U.torch_mod()
+
+    def fresh():
+        b = Both([3000, 17], True, bits, seed=6)
+        for g in b.g:
+            g.copy_(torch.randn(g.shape, generator=torch.Generator().manual_seed(9)) * 1e-2)
+        return b
+
+    eager, graphed = fresh(), fresh()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.plan.step(1e-3, 0.9, 0.999, 1e-8, 7, 3, torch.cuda.current_stream().cuda_stream)
+    for k in range(3):
+        graph.replay()
+        eager.plan.step(1e-3, 0.9, 0.999, 1e-8, 7, 3, torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        pairs = list(zip(eager.p + eager.c, graphed.p + graphed.c)) + [(eager.m, graphed.m), (eager.v, graphed.v)]
+        if bits == 8:
+            pairs += [(eager.ms, graphed.ms), (eager.vs, graphed.vs)]
+        for a, b in pairs:
+            assert np.array_equal(a.float().cpu().numpy(), b.float().cpu().numpy(), equal_nan=True), k
