@@ -8,11 +8,12 @@
 // "k-major" below: the sum's index runs along memory (both operands of the forward product, dy of dgrad); the others have it as the row.
 // Which expert a tile of rows belongs to every wave finds itself from the offsets, so that a call is one launch.
 //
-// Times on an MI355X (its library's product of 8192^3: 1.34 PFLOP/s in bf16; a copy: 4.9 TB/s).  bf16 tiles: 8192^3 as one expert 1.26-1.37 PFLOP/s, forward, dgrad and wgrad, 1.35
-// from 8 bits: bound by the matrix pipe and the clock that its power leaves (its share of the cycles at eight experts of 2048 rows, 4096 -> 4096: 0.55; LDS
-// bank conflicts, all from the stores, 3 % of its cycles).  With drawn sizes of 2048 rows on average 478 us, where the experts' last tiles cost a tenth (equal experts: 437), and 456 from 8 bits; weight gradient 493-509, of which
-// 537 MB of fp32 results are 110.  A hundred experts of unequal sizes, 1024 -> 1024, cold weights: 57 us forward, 49 dgrad, 95 wgrad (4.7 TB/s): bound by the
-// weights' bytes.  Few rows: ten rows of a hundred experts 7 us (21 MB of weights), eight of eight experts in 8 bits 26 us (90 MB).
+// Times on an MI355X (its library's product of 8192^3: 1.36 PFLOP/s in bf16; a copy: 4.9 TB/s).  bf16 tiles: 8192^3 as one expert 1.24-1.35 PFLOP/s, forward, dgrad and wgrad, 1.33
+// from 8 bits: bound by the matrix pipe and the clock that its power leaves (its share of the cycles at eight experts of 2048 rows, 4096 -> 4096: 0.57, 0.54 from 8 bits).  Of the cycles
+// of LDS 3 % are bank conflicts, all from the stores of the results, and 29 % from 8 bits, where the converted operands are stored too.  With drawn sizes of 2048 rows on average
+// 480-500 us, where the experts' last tiles cost a tenth (equal experts: 454), and 447-472 from 8 bits (439); weight gradient 493-509, of which
+// 537 MB of fp32 results are 110.  A hundred experts of unequal sizes, 1024 -> 1024, cold weights: 57 us forward, 49 dgrad, 96 wgrad (4.7 TB/s): bound by the
+// weights' bytes.  Few rows: ten rows of a hundred experts 7 us (21 MB of weights), eight of eight experts in 8 bits 27-29 us (90 MB).
 #include "code_walk.h"
 #include "group_tiles.h"
 #include "lds_copy.h"
@@ -47,8 +48,8 @@ __device__ __forceinline__ unsigned block_of(const LinearArgs& q) { return q.fir
 
 // ---- fp32 ----
 //
-// Bound by the matrix pipe, which six bf16 products a value keep busy, and the vector instructions that split the operands: eight experts of 1024 rows, 2048 -> 2048, 445 us
-// forward, 433 dgrad, 379 wgrad = 154-181 TFLOP/s (the library's fp32 product: 133).
+// Bound by the matrix pipe, which six bf16 products a value keep busy, and the vector instructions that split the operands: eight experts of 1024 rows on average, 2048 -> 2048,
+// 459 us forward, 447 dgrad, 377 wgrad = 150-182 TFLOP/s (equal experts 388, 376, 373; the library's fp32 product: 133 TFLOP/s).
 // RT x RT tiles (128 or 64), 32 of the sum's index at a time: loaded into registers while the last ones are multiplied, then written to LDS as three planes of bf16
 // parts (split_mfma.h).  What has the sum's index as its row is kept that way and read with transposing LDS reads.
 constexpr int RK = 32;
@@ -139,7 +140,9 @@ __device__ __forceinline__ void part_of(int part, int parts, int& begin, int& en
 // own), so that its lanes store whole rows, 16 bytes each: 64 lanes with four columns each of sixteen rows would write 32 or 64 bytes of a row at a time (the weight
 // gradient of a hundred experts of 1024 x 1024: 173 us, 125 by rows).
 // PAST: past the caches.  A weight gradient's results are more than what they are made of and push it out of them (a hundred experts of 1024 x 1024: 124 us, 92 past
-// the caches; eight of 4096 x 4096: 527, 493; ten of 512 x 784: 11, 9.3).  A layer's outputs are read next, and stay.
+// the caches; eight of 4096 x 4096: 527, 493; ten of 512 x 784: 11, 9.3; followed by the AdamW step that reads them, 8-bit moments, a hundred of 1024 x 1024 447, 435, ten of 512 x 784
+// 29.2, 28.0, with 32-bit moments 33.1, 33.7).  The partial sums of a split gradient, which sum_parts_kernel reads next, go the same way, though they would be faster through the caches (both
+// launches, bf16, one expert of 16384 rows: 512 x 512 34, past them 38; 128 x 128 24, 33).  A layer's outputs are read next, and stay.
 template <typename C, bool PAST, int TM, int TN>
 __device__ __forceinline__ void store_rows(const floatx4 (&acc)[TM][TN], C* c, long long stride, unsigned char* lds, int m0, int m_end, int n0, int n_end) {
   constexpr int WIDE = TN * 16 * (int)sizeof(C), LANES = WIDE / 16, EACH = 16 / (int)sizeof(C);
@@ -635,7 +638,7 @@ constexpr int stages(Form f, int height, int width, int kib) {
 }
 // How a launch with tiles of BM x BN by WM x WN waves (SPLIT = 2: and as many again) takes experts' last rows: in half and a quarter of the height.  Next to many
 // 256 x 256 tiles, which have a CU for themselves, half the columns by two sets of four waves, twice the blocks of half the length, end a launch sooner (eight experts of
-// 2048 rows, 4096 -> 4096: 489 -> 478 us, in 8 bits 486 -> 456); where they are most of the launch, they read the weights less well (32 of 128, 2048 -> 2048: 79 -> 92).
+// 2048 rows, 4096 -> 4096: 489 -> 478 us, in 8 bits 486 -> 456, measured in turn); where they are most of the launch, they read the weights less well (32 of 128, 2048 -> 2048: 79 -> 92).
 template <Form F, int BM, int BN, int WM, int WN, int SPLIT>
 struct Shapes {
   static constexpr bool NARROW = BM == 256;
@@ -1062,6 +1065,8 @@ gan_status launch_few_dgrad(const LinearArgs& q, int sixteens, hipStream_t st) {
 // 640 -> 2176: 82, 62) and up to 32 in dgrad (a hundred of 24: 107, 121; 32 of 29, 640 <- 2176: 69, 91).  Beyond, where 64 x 64 tiles are few, forward: four of 100, 2048 -> 2048
 // (320 tiles): 64, 73; 32 of 25, 512 -> 512 (352): 16, 19.5; four of 175, 2048 -> 2048 (480): 94, 81; two of 1000, 1024 -> 1024 (530): 62, 44.  And where 128 x 128 tiles
 // are few in dgrad, whose columns this kernel reads more widely: ten of 111, 110 <- 6272: 47, 222; eight of 244, 1024 <- 2808 (184): 132, 153; ten of 640, 784 <- 512 (420): 71, 53.
+// This rule and the tiles' see the average number of rows, which the host knows, not the offsets: a batch that is all one expert's is taken like one of average experts (800 rows of
+// one of a hundred, 1024 -> 1024, bf16: 27 us forward, 15 dgrad; the same rows with that expert alone 14, 14; fp32 43, 25 and 34, 26).
 int few_rows(const LinearArgs& q, int kind, int esize) {
   const long long each = q.rows / most_groups(q);
   // short sums of many outputs give the waves little to share (128 experts of 3.5 rows, 256 -> 896: 32 us, 21 in tiles; fp32, eight of 128, 64 -> 896: 15.3, 5.6)
@@ -1078,12 +1083,20 @@ gan_status launch_fp32_as(int kind, const LinearArgs& q, hipStream_t st) {
   const long long blocks = kind == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, RT) : ceil_div(q.n, RT) * most_tiles(q.rows, q.groups, RT);
   return launch(kind == FORWARD ? linear_fp32_kernel<FORWARD, RT> : kind == DGRAD ? linear_fp32_kernel<DGRAD, RT> : linear_fp32_kernel<WGRAD, RT>, blocks, 256, 0, q, st);
 }
+// 128 x 128 tiles from 1024 of them on, four to a CU, in the weight gradient from 400; else 64 x 64.  us by 64, by 128.  Forward: four experts of 750 rows, 640 -> 640 (135 tiles of 128) 28, 45; 16 of
+// 128, 1024 -> 1024 (256) 52, 72; eight of 512, 2048 -> 2048 (640, an expert's last one mostly empty) 272, 288; ten of 112, 110 -> 6272 (882) 29, 33; one of 8192, 2048 -> 2048 (1040) 472, 370; 32 of 200,
+// 512 -> 2048 (1312) 130, 102; one of 16384, 1024 -> 4096 (4128) 922, 736.  It loses where fewer tiles are all whole (one of 4096, 2048 -> 2048, 528: 249, 199) and where more are not (a hundred of 64,
+// 1024 -> 1024, 1200: 169, 178).  Weight gradient: two of 512 x 784 (56) 19, 39; three of 1024 x 1024 (192) 29, 37; ten of 512 x 784 (280) 18, 20; 16 of 768 x 512 (384) 21.5, 19.8; ten of
+// 6272 x 110 (490) 26.7, 26.3; eight of 1024 x 1024 (512) 134, 107; one of 512 x 512 in 32 parts (512) 85, 69; a hundred of 512 x 512 (1600) 48, 46.
 gan_status launch_fp32(int kind, const LinearArgs& q, hipStream_t st) {
   const long long large = kind == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, 128) : tiles(q, 128, 128);
   return large >= (kind == WGRAD ? 400 : 1024) ? launch_fp32_as<128>(kind, q, st) : launch_fp32_as<64>(kind, q, st);
 }
 
-// Into how many parts the weight gradient takes an expert's rows: few tiles of long sums would leave most CUs idle.
+// Into how many parts the weight gradient takes an expert's rows: few tiles of long sums would leave most CUs idle.  As many as make two tiles of 128 a CU, of 256 rows at least, 64 at
+// most.  us, in one part and so: one expert of 16384 rows, 512 x 512 (32 parts), fp32 543, 77, bf16 150, 38; 128 x 128 (64) 441, 37 and 157, 33; one of 1000, 256 x 256 (3) 31, 16.5 and
+// 14.0, 11.6; four of 1000, 512 x 512 (3) 33, 26 and 15.6, 15.5; one of 4000, 2048 x 2048 (2) 248, 195, but in bf16, whose tiles of 256 are enough, 47, 57.  Half as many tiles: the first
+// 90 and 31; twice as many: 96 and 54.  Parts of 128 rows: 256 x 256 13.0 and 11.6, but 512 x 512 of 1000 rows 32 and 20.6; of 512 rows: 31 and 14, 33.5 and 15.6.
 int wgrad_parts(int groups, long long rows, int n_in, int n_out) {
   const long long blocks = wgrad_tiles(groups, n_out, n_in, 128), each = rows / std::max(1, groups);
   return (int)std::max(1ll, std::min({512 / std::max(1ll, blocks), each / 256, 64ll}));

@@ -2,9 +2,9 @@
 //
 //   sum = round(x + residual), inv = 1 / sqrt(mean(sum^2) + eps), y = sum * inv * gain
 //
-// Bound by memory: one pass over x and residual, six operations an element; bf16 on an MI355X: 16384 x 4096 into 8 bits 81 us (5.8 TB/s), 6400 x 2048 forward 21 us and
-// gradient 26 us from cold memory (5.1 and 4.1 TB/s; a plain copy 4.9), four rows of 1024 3.2 us.  A row is held in registers between the sum of its squares and
-// its output, by one wave (rows up to 2048 elements, where no barrier is needed), a block of four waves, or one of sixteen; rows beyond
+// Bound by memory: one pass over x and residual, six operations an element; bf16 on an MI355X: 16384 x 4096 into 8 bits 81-84 us (5.6-5.8 TB/s), 6400 x 2048 forward 21 us and
+// gradient 25 us from cold memory (5.1 and 4.1 TB/s; a plain copy 4.9), four rows of 1024 3.2 us.  A row is held in registers between the sum of its squares and
+// its output, by one wave (up to 512 elements, 1024 in many rows, where no barrier is needed), a block of four waves, or one of sixteen; rows beyond
 // 32768 elements (16384 in the gradient) are read a second time.
 #include "operators.h"
 
@@ -404,7 +404,9 @@ void launch_back(const NormBackArgs& a, hipStream_t st) {
 }
 
 // ---- 8 bits ----
-
+//
+// Bound by memory, a pass that reads a matrix and writes half or a quarter of its bytes: bf16, 16384 x 4096 44 us (4.6 TB/s), 32768 x 4096 74 (5.4), 6400 x 2048 9.3, fp32, 40960 x 4096 165 (5.1); up to a
+// million values the launch (3.8).  Sixteen lanes hold a block of 128, so that its scale is four exchanges between lanes.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void quantize8_kernel(const T* x, long long stride, long long rows, int cols, uint8_t* q, uint8_t* scale) {
   const long long wide = padded8(cols), chunks = rows * (wide / E);
