@@ -263,13 +263,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_back_kerne
       unpack<T>(now.s[c], s[c]);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        s[c][i] *= now.inv;                                       // (of size one, also where inv^2 is no fp32 number: rows of 1e-20 without eps)
-        dg[c][i] += h[c][i] * s[c][i];
+        dg[c][i] += h[c][i] * (s[c][i] * now.inv);
         h[c][i] *= g[i];
         dot += h[c][i] * s[c][i];
       }
     }
-    const float k = row_total<WAVES>(dot, scratch) / (float)a.cols;
+    const float k = now.inv * (now.inv * (row_total<WAVES>(dot, scratch) / (float)a.cols));     // (inv^2 alone may be no fp32 number: rows of 1e-20 without eps)
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
       const int col = (c * 64 * WAVES + lane) * E;
@@ -314,9 +313,9 @@ __global__ __launch_bounds__(1024) void norm_back_long_kernel(NormBackArgs a) {
     load8<T, VEC>(sum + col, a.cols - col, s);
     load8<float, VEC>(a.gain + col, a.cols - col, g);
 #pragma unroll
-    for (int i = 0; i < E; ++i) dot += h[i] * g[i] * (s[i] * inv);
+    for (int i = 0; i < E; ++i) dot += h[i] * g[i] * s[i];
   }
-  const float k = row_total<16>(dot, scratch) / (float)a.cols;
+  const float k = inv * (inv * (row_total<16>(dot, scratch) / (float)a.cols));
   for (int col = threadIdx.x * E; col < a.cols; col += 1024 * E) {
     load8<T, VEC>(dy + col, a.cols - col, h);
     load8<T, VEC>(sum + col, a.cols - col, s);
@@ -329,7 +328,7 @@ __global__ __launch_bounds__(1024) void norm_back_long_kernel(NormBackArgs a) {
       for (int i = 0; i < E; ++i) d[i] = 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < E; ++i) d[i] += inv * (h[i] * g[i] - s[i] * inv * k);
+    for (int i = 0; i < E; ++i) d[i] += inv * (h[i] * g[i] - s[i] * k);
     store8<T, VEC>((T*)a.dx + row * a.dx_stride + col, a.cols - col, d);
   }
 }
