@@ -358,7 +358,8 @@ gan_status gan_quantize8(int32_t precision, const void* x, int64_t x_stride, int
    fp32 products are sums of products of three bf16 parts of every value, as in the training step (or of fp32 values, where experts have few rows).
    8-bit products take an element as the bf16 number nearest to it, which it is but for blocks of the two lowest E, where it is rounded to a multiple of
    2^-133, and elements from 2^128 on (E of 120 and more), which are infinite; products and sums are fp32.
-   work: DEVICE, gan_group_linear_wgrad_bytes(...) (0: none is needed, and work may be NULL), 16-byte aligned.  At most 65535 groups. */
+   work: DEVICE, gan_group_linear_wgrad_bytes(...) (0: none is needed, and work may be NULL), 16-byte aligned.  At most 65535 groups (every block scans the
+   offsets: calls are made for hundreds of experts), 2^22 inputs in 8 bits, and 2^31 - 1 tiles of outputs (16 x 16 at the least); more are GAN_E_SHAPE. */
 gan_status gan_group_linear(int32_t precision, const void* x, int64_t x_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows,
                             int32_t n_in, int32_t n_out, void* y, int64_t y_stride, void* hip_stream);
 gan_status gan_group_linear_dgrad(int32_t precision, const void* dy, int64_t dy_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows,

@@ -96,3 +96,10 @@ def test_chance_rounding_is_fair():
         total += R.decode(R.chance_codes(x, s, u & 0xFFFF, False), s[:, None])
     ulp = np.maximum(np.exp2(np.floor(np.log2(x / np.exp2(s - 127.0)[:, None]))), 2.0 ** -6) / 8 * np.exp2(s - 127.0)[:, None]
     assert np.all(np.abs(total[:, 1:].mean(1) / n - x[:, 1]) <= 5 * 0.5 * ulp[:, 1] / np.sqrt(127 * n))
+
+
+def test_eight_bits_of_too_many_inputs():
+    """2^22 inputs are the most in 8 bits, padded to 128 or not; what is refused for its sizes is refused without rows too."""
+    for n_in, rows in (((1 << 22) + 1, 10), ((1 << 22) + 128, 0), (1 << 28, 10)):
+        refused(lambda: B.group_linear8(P, P, P, P, P, 4, rows, n_in, 64, B.BF16, P, 64), B.GAN_E_SHAPE, "2^22")
+    B.group_linear8(P, P, P, P, P, 4, 0, 1 << 22, 64, B.BF16, P, 64)
