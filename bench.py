@@ -40,7 +40,8 @@ MEASURED_TRAFFIC = {
 
 
 # the operators for label experts, of which the step compiles and launches nothing
-OPERATOR_SOURCES = {"adamw.hip", "code_walk.h", "group_linear.hip", "group_tiles.h", "operators.h", "operators.hip", "rms_norm.hip"}
+OPERATOR_SOURCES = {"activation.h", "adamw.hip", "code_walk.h", "dropout.hip", "expert_rows.hip", "group_act.hip", "group_linear.hip", "group_linear_act.hip", "group_product.h",
+                    "group_tiles.h", "operators.h", "operators.hip", "rms_norm.hip", "route.hip", "row_chunks.h"}
 
 
 def sources_digest(root=None):

@@ -311,7 +311,8 @@ gan_status gan_op_dw4_to_dw3(gan_ctx* ctx, const float* dw4, float* dw3, int32_t
 
 /* ---- operators for label experts that are not DC-CGANs ------------------------------------------------------------
    Rows of many labels stand in one matrix, one label's behind the other's, and every label has weights of its own
-   (an expert): the root-mean-square norm, the products grouped by label, and the optimiser step over all tensors.
+   (an expert): the root-mean-square norm, the products grouped by label, with an epilogue or without, the router that chooses experts, rows sorted by label, handed out and put
+   together again, dropout, and the optimiser step over all tensors.
    None needs a context.  All matrices are row-major and DEVICE; a stride is the number of elements from one row to the
    next, at least the row's length.  Any length, stride and alignment of the element's own size is taken (multiples of
    16 bytes run faster), up to 2^30 rows and 2^28 elements a row; offsets into tensors are 64-bit.  `precision` is the storage
@@ -369,6 +370,75 @@ gan_status gan_group_linear_wgrad(int32_t precision, const void* x, int64_t x_st
                                   int64_t rows, int32_t n_in, int32_t n_out, float* dw, void* work, int64_t work_bytes, void* hip_stream);
 gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scale, const uint8_t* w8, const uint8_t* w_scale, const int32_t* offs, int32_t groups,
                              int64_t rows, int32_t n_in, int32_t n_out, int32_t y_precision, void* y, int64_t y_stride, void* hip_stream);
+
+/* Products grouped by label with an epilogue.  act: gan_act; bias: fp32 [groups][n_out], or NULL (none).
+     gan_group_linear_act        z[i] = w[g] x[i] + bias[g];  y[i] = act(z[i]) + residual[i]     [rows][n_out]; z is stored where it is not NULL, residual NULL: none.
+                                 y is formed from z before its rounding, and rounded once.
+     gan_group_linear8_act       the same y of 8-bit matrices (as gan_group_linear8); residual in y_precision
+     gan_group_linear_dgrad_act  dx[i] = (dy[i] w[g] + other[i]) act'(z[i])    [rows][n_in]: the gradient of the sums z whose activation was x, from the gradient dy of this
+                                 layer's sums and that which reaches x by other ways (NULL: none).  GAN_ACT_NONE: z is not read, and dx is that of x.
+     gan_group_act_backward      dz = dy act'(z)  [rows][cols], dbias[g] = sum of dz (before its rounding) over g's rows  fp32 [groups][cols], zero for an expert without
+                                 rows; dz or dbias may be NULL.  GAN_ACT_NONE: z is not read.  work: DEVICE, gan_group_act_backward_bytes(...), 16-byte aligned (dbias NULL: none).
+   Rows of no expert: all their results are zero.  y may be the memory of residual, dx that of other or z, dz that of dy or z, if the strides are the same; z and y are two
+   matrices.  The activations at infinity are their limits; act' of GAN_ACT_RELU is 0 at zero. */
+typedef enum { GAN_ACT_NONE = 0, GAN_ACT_RELU = 1, GAN_ACT_GELU = 2 /* z times the normal distribution's Phi(z) */, GAN_ACT_SILU = 3 /* z / (1 + exp(-z)) */ } gan_act;
+gan_status gan_group_linear_act(int32_t precision, const void* x, int64_t x_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows, int32_t n_in,
+                                int32_t n_out, const float* bias, int32_t act, const void* residual, int64_t residual_stride, void* z, int64_t z_stride, void* y,
+                                int64_t y_stride, void* hip_stream);
+gan_status gan_group_linear8_act(const uint8_t* x8, const uint8_t* x_scale, const uint8_t* w8, const uint8_t* w_scale, const int32_t* offs, int32_t groups, int64_t rows,
+                                 int32_t n_in, int32_t n_out, const float* bias, int32_t act, const void* residual, int64_t residual_stride, int32_t y_precision, void* y,
+                                 int64_t y_stride, void* hip_stream);
+gan_status gan_group_linear_dgrad_act(int32_t precision, const void* dy, int64_t dy_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows, int32_t n_in,
+                                      int32_t n_out, const void* other, int64_t other_stride, int32_t act, const void* z, int64_t z_stride, void* dx, int64_t dx_stride,
+                                      void* hip_stream);
+int64_t gan_group_act_backward_bytes(int32_t groups, int64_t rows, int32_t cols);
+gan_status gan_group_act_backward(int32_t precision, const void* dy, int64_t dy_stride, int32_t act, const void* z, int64_t z_stride, const int32_t* offs, int32_t groups,
+                                  int64_t rows, int32_t cols, void* dz, int64_t dz_stride, float* dbias, void* work, int64_t work_bytes, void* hip_stream);
+
+/* Rows that choose their experts.  logits [rows][experts] in the storage type.  An expert whose logit is -infinity or NaN is not there for the row; p are the probabilities of
+   those that are, exp(l - max) / sum of the same (all NaN in a row with a NaN or +infinity).  expert int32 [rows][k]: the k largest, the largest first, the lowest
+   index among equals (-0 and 0 are), -1 where fewer are there; weight fp32 [rows][k] (or NULL): their p, normalize = 1: divided by the sum over the row's choices; 0 behind them.
+   counts int32 [experts + 1] (or NULL; then mean and balance are NULL too): how many rows chose each expert, and how many rows have an expert at all; mean fp32 [experts] (or NULL): the
+   mean of p over these rows (0 without any); balance fp32 [1] (or NULL): experts * sum over e of counts[e] / sum(counts) * mean[e], 1 where all experts get the same.
+   A row of padding is one without an expert, all its logits -infinity.
+   At most 4096 experts, 16 choices, 2^30 choices in all.  work: DEVICE, gan_route_bytes(rows, experts), 16-byte aligned (counts NULL: none). */
+int64_t gan_route_bytes(int64_t rows, int32_t experts);
+gan_status gan_route(int32_t precision, const void* logits, int64_t logits_stride, int64_t rows, int32_t experts, int32_t k, int32_t normalize, int32_t* expert, float* weight,
+                     int32_t* counts, float* mean, float* balance, void* work, int64_t work_bytes, void* hip_stream);
+/* Its gradient, from the same logits, k and normalize, the expert and counts that gan_route left, dweight fp32 [rows][k] (NULL: none; what stands beside a choice of no expert is
+   not used) and balance_grad, the factor of balance in the loss (counts NULL: none): dlogits [rows][experts], which may be the memory of logits, if the strides are
+   the same.  The counts are constants, as choices have no gradient; the logits of experts that are not there have gradient 0. */
+gan_status gan_route_backward(int32_t precision, const void* logits, int64_t logits_stride, int64_t rows, int32_t experts, int32_t k, int32_t normalize, const int32_t* expert,
+                              const float* dweight, const int32_t* counts, float balance_grad, void* dlogits, int64_t dlogits_stride, void* hip_stream);
+
+/* Labels sorted on the device: what gan_route chose (n = rows * k, an entry for every choice), or the labels of a batch (n = rows, k = 1 below).  labels: DEVICE int32 [n]; what is
+   outside [0, groups) is of no expert and goes behind all others.  offs int32 [groups + 1]: where each group begins, as the grouped products take it; order int32 [n] (or NULL): the
+   entry at each place, those of a group in their order; place int32 [n] (or NULL): the place of each entry.  At most 4096 groups, 2^30 labels.
+   work: DEVICE, gan_sort_by_label_bytes(n, groups) (0: none is needed), 16-byte aligned. */
+int64_t gan_sort_by_label_bytes(int64_t n, int32_t groups);
+gan_status gan_sort_by_label(const int32_t* labels, int64_t n, int32_t groups, int32_t* offs, int32_t* order, int32_t* place, void* work, int64_t work_bytes, void* hip_stream);
+/* Rows handed out to their places, and put together again.  place int32 [rows][k] and offs as gan_sort_by_label leaves them for rows * k entries (a place outside
+   [0, rows * k) is skipped, one from offs[groups] on is of no expert); matrices of rows * k rows stand in the places' order.
+     gan_gather_rows            out[place[i][s]] = x[i]; rows of no expert are zero
+     gan_combine_rows           y[i] = residual[i] + sum over s of weight[i][s] out[place[i][s]], without those of no expert; residual NULL: none; weight NULL: all 1,
+                                which is gan_gather_rows' gradient.  y may be the memory of residual, if the strides are the same.
+     gan_combine_rows_backward  dout[place[i][s]] = weight[i][s] dy[i] (zero for rows of no expert), dweight[i][s] = the sum of dy[i] * out[place[i][s]] over the
+                                columns, 0 for choices of no expert; either may be NULL.  dout may be the memory of out, if the strides are the same.  (residual's gradient is dy.) */
+gan_status gan_gather_rows(int32_t precision, const void* x, int64_t x_stride, const int32_t* place, const int32_t* offs, int32_t groups, int32_t k, int64_t rows,
+                           int32_t cols, void* out, int64_t out_stride, void* hip_stream);
+gan_status gan_combine_rows(int32_t precision, const void* out, int64_t out_stride, const int32_t* place, const float* weight, const int32_t* offs, int32_t groups, int32_t k,
+                            const void* residual, int64_t residual_stride, int64_t rows, int32_t cols, void* y, int64_t y_stride, void* hip_stream);
+gan_status gan_combine_rows_backward(int32_t precision, const void* dy, int64_t dy_stride, const void* out, int64_t out_stride, const int32_t* place, const float* weight,
+                                     const int32_t* offs, int32_t groups, int32_t k, int64_t rows, int32_t cols, void* dout, int64_t dout_stride, float* dweight,
+                                     void* hip_stream);
+
+/* Dropout: y = residual + keep * x / (1 - q), q = p to the nearest multiple of 2^-16 (p in [0, 1), and q below 1); residual NULL: none.  The gradient is the same call on dy without a
+   residual.  The mask is never stored: columns 8c .. 8c + 7 of row r are kept by the eight 16-bit numbers of Philox-4x32-10 with counter (n low, n high, site, step), n = r *
+   ceil(cols / 8) + c, and key (seed low, seed high), the lower half of a word first, each kept where its number is at least 65536 q.  What is dropped is 0 whatever x was.
+   site tells the places of a network apart, step its iterations; step_device (DEVICE uint32, or NULL) is added to step when the call runs, so that a captured call
+   has another mask at every replay.  y may be the memory of x or residual, if the strides are the same. */
+gan_status gan_dropout(int32_t precision, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, int64_t rows, int32_t cols, double p, uint64_t seed,
+                       uint32_t site, uint32_t step, const uint32_t* step_device, void* y, int64_t y_stride, void* hip_stream);
 
 /* AdamW over many tensors in one launch.  The handle holds where they are (HOST arrays of DEVICE pointers, read by gan_adamw_create) and nothing that
    a step changes: params[t] fp32 [sizes[t]], grads[t] in grad_precision, copies[t] (copies or an entry may be NULL) a bf16 copy that every step writes,

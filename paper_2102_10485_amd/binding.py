@@ -11,6 +11,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 MAX_LAYERS = 8
 FP32, BF16 = 0, 1
 FAMILY_STRIDED, FAMILY_PAPER = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 
 GAN_OK, GAN_E_ARG, GAN_E_SHAPE, GAN_E_OOM, GAN_E_HIP, GAN_E_LABEL, GAN_E_STATE = 0, -1, -2, -3, -4, -5, -6
 
@@ -108,6 +109,20 @@ def load_library():
     L.gan_group_linear_wgrad_bytes.argtypes, L.gan_group_linear_wgrad_bytes.restype = [i32, i64, i32, i32], i64
     L.gan_group_linear_wgrad.argtypes = [i32, _VP, i64, _VP, i64, _VP, i32, i64, i32, i32, _VP, _VP, i64, _VP]
     L.gan_group_linear8.argtypes = [_VP, _VP, _VP, _VP, _VP, i32, i64, i32, i32, i32, _VP, i64, _VP]
+    L.gan_group_linear_act.argtypes = [i32, _VP, i64, _VP, _VP, i32, i64, i32, i32, _VP, i32, _VP, i64, _VP, i64, _VP, i64, _VP]
+    L.gan_group_linear8_act.argtypes = [_VP, _VP, _VP, _VP, _VP, i32, i64, i32, i32, _VP, i32, _VP, i64, i32, _VP, i64, _VP]
+    L.gan_group_linear_dgrad_act.argtypes = [i32, _VP, i64, _VP, _VP, i32, i64, i32, i32, _VP, i64, i32, _VP, i64, _VP, i64, _VP]
+    L.gan_group_act_backward_bytes.argtypes, L.gan_group_act_backward_bytes.restype = [i32, i64, i32], i64
+    L.gan_group_act_backward.argtypes = [i32, _VP, i64, i32, _VP, i64, _VP, i32, i64, i32, _VP, i64, _VP, _VP, i64, _VP]
+    L.gan_route_bytes.argtypes, L.gan_route_bytes.restype = [i64, i32], i64
+    L.gan_route.argtypes = [i32, _VP, i64, i64, i32, i32, i32, _VP, _VP, _VP, _VP, _VP, _VP, i64, _VP]
+    L.gan_route_backward.argtypes = [i32, _VP, i64, i64, i32, i32, i32, _VP, _VP, _VP, C.c_float, _VP, i64, _VP]
+    L.gan_sort_by_label_bytes.argtypes, L.gan_sort_by_label_bytes.restype = [i64, i32], i64
+    L.gan_sort_by_label.argtypes = [_VP, i64, i32, _VP, _VP, _VP, _VP, i64, _VP]
+    L.gan_gather_rows.argtypes = [i32, _VP, i64, _VP, _VP, i32, i32, i64, i32, _VP, i64, _VP]
+    L.gan_combine_rows.argtypes = [i32, _VP, i64, _VP, _VP, _VP, i32, i32, _VP, i64, i64, i32, _VP, i64, _VP]
+    L.gan_combine_rows_backward.argtypes = [i32, _VP, i64, _VP, i64, _VP, _VP, _VP, i32, i32, i64, i32, _VP, i64, _VP, _VP]
+    L.gan_dropout.argtypes = [i32, _VP, i64, _VP, i64, i64, i32, dbl, C.c_uint64, C.c_uint32, C.c_uint32, _VP, _VP, i64, _VP]
     L.gan_adamw_blocks.argtypes, L.gan_adamw_blocks.restype = [i32, _I64P], i64
     L.gan_adamw_create.argtypes = [i32, _I64P, C.POINTER(_VP), C.POINTER(_VP), i32, C.POINTER(_VP), _FP, i32, _VP, _VP, _VP, _VP, C.POINTER(_VP)]
     L.gan_adamw_step.argtypes = [_VP, dbl, dbl, dbl, dbl, i64, C.c_uint32, _VP]
@@ -159,6 +174,66 @@ def group_linear_wgrad(precision, x, x_stride, dy, dy_stride, offs, groups, rows
 
 def group_linear8(x8, x_scale, w8, w_scale, offs, groups, rows, n_in, n_out, y_precision, y, y_stride, stream=0):
     _operator(load_library().gan_group_linear8(x8, x_scale, w8, w_scale, offs, groups, rows, n_in, n_out, y_precision, y, y_stride, stream))
+
+
+def group_linear_act(precision, x, x_stride, w, offs, groups, rows, n_in, n_out, bias, act, residual, residual_stride, z, z_stride, y, y_stride, stream=0):
+    _operator(load_library().gan_group_linear_act(precision, x, x_stride, w, offs, groups, rows, n_in, n_out, bias, act, residual, residual_stride, z, z_stride, y, y_stride,
+                                                  stream))
+
+
+def group_linear8_act(x8, x_scale, w8, w_scale, offs, groups, rows, n_in, n_out, bias, act, residual, residual_stride, y_precision, y, y_stride, stream=0):
+    _operator(load_library().gan_group_linear8_act(x8, x_scale, w8, w_scale, offs, groups, rows, n_in, n_out, bias, act, residual, residual_stride, y_precision, y, y_stride,
+                                                   stream))
+
+
+def group_linear_dgrad_act(precision, dy, dy_stride, w, offs, groups, rows, n_in, n_out, other, other_stride, act, z, z_stride, dx, dx_stride, stream=0):
+    _operator(load_library().gan_group_linear_dgrad_act(precision, dy, dy_stride, w, offs, groups, rows, n_in, n_out, other, other_stride, act, z, z_stride, dx, dx_stride,
+                                                        stream))
+
+
+def group_act_backward_bytes(groups, rows, cols):
+    return load_library().gan_group_act_backward_bytes(groups, rows, cols)
+
+
+def group_act_backward(precision, dy, dy_stride, act, z, z_stride, offs, groups, rows, cols, dz, dz_stride, dbias, work, work_bytes, stream=0):
+    _operator(load_library().gan_group_act_backward(precision, dy, dy_stride, act, z, z_stride, offs, groups, rows, cols, dz, dz_stride, dbias, work, work_bytes, stream))
+
+
+def route_bytes(rows, experts):
+    return load_library().gan_route_bytes(rows, experts)
+
+
+def route(precision, logits, logits_stride, rows, experts, k, normalize, expert, weight, counts, mean, balance, work, work_bytes, stream=0):
+    _operator(load_library().gan_route(precision, logits, logits_stride, rows, experts, k, int(normalize), expert, weight, counts, mean, balance, work, work_bytes, stream))
+
+
+def route_backward(precision, logits, logits_stride, rows, experts, k, normalize, expert, dweight, counts, balance_grad, dlogits, dlogits_stride, stream=0):
+    _operator(load_library().gan_route_backward(precision, logits, logits_stride, rows, experts, k, int(normalize), expert, dweight, counts, balance_grad, dlogits,
+                                                dlogits_stride, stream))
+
+
+def sort_by_label_bytes(n, groups):
+    return load_library().gan_sort_by_label_bytes(n, groups)
+
+
+def sort_by_label(labels, n, groups, offs, order, place, work, work_bytes, stream=0):
+    _operator(load_library().gan_sort_by_label(labels, n, groups, offs, order, place, work, work_bytes, stream))
+
+
+def gather_rows(precision, x, x_stride, place, offs, groups, k, rows, cols, out, out_stride, stream=0):
+    _operator(load_library().gan_gather_rows(precision, x, x_stride, place, offs, groups, k, rows, cols, out, out_stride, stream))
+
+
+def combine_rows(precision, out, out_stride, place, weight, offs, groups, k, residual, residual_stride, rows, cols, y, y_stride, stream=0):
+    _operator(load_library().gan_combine_rows(precision, out, out_stride, place, weight, offs, groups, k, residual, residual_stride, rows, cols, y, y_stride, stream))
+
+
+def combine_rows_backward(precision, dy, dy_stride, out, out_stride, place, weight, offs, groups, k, rows, cols, dout, dout_stride, dweight, stream=0):
+    _operator(load_library().gan_combine_rows_backward(precision, dy, dy_stride, out, out_stride, place, weight, offs, groups, k, rows, cols, dout, dout_stride, dweight, stream))
+
+
+def dropout(precision, x, x_stride, residual, residual_stride, rows, cols, p, seed, site, step, step_device, y, y_stride, stream=0):
+    _operator(load_library().gan_dropout(precision, x, x_stride, residual, residual_stride, rows, cols, p, seed, site, step, step_device, y, y_stride, stream))
 
 
 def adamw_blocks(sizes):

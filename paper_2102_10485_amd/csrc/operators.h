@@ -10,6 +10,11 @@ gan_status operator_fail(gan_status s, const char* why);          // records the
 void operator_launches();                                         // before a launch: what an earlier HIP call of the caller's left behind is not its failure
 gan_status operator_launched();                                   // GAN_OK, or GAN_E_HIP with the runtime's text
 
+constexpr long long MOST_ROWS = 1 << 30;
+constexpr int MOST_COLS = 1 << 28;
+gan_status check_sizes(int32_t precision, long long rows, int cols);
+gan_status check_matrix(const void* p, long long stride, int cols, const char* why);
+
 constexpr int BLOCK8 = 128;                                       // neighbours that share a scale
 __host__ __device__ inline long long padded8(long long cols) { return (cols + BLOCK8 - 1) / BLOCK8 * BLOCK8; }
 

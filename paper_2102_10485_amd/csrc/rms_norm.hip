@@ -420,20 +420,6 @@ __global__ __launch_bounds__(256) void quantize8_kernel(const T* x, long long st
   }
 }
 
-constexpr long long MOST_ROWS = 1 << 30;
-constexpr int MOST_COLS = 1 << 28;
-
-bool precision_known(int32_t p) { return p == GAN_FP32 || p == GAN_BF16_FP32MASTER; }
-gan_status check_matrix(const void* p, long long stride, int cols, const char* why) {
-  return p && stride < cols ? operator_fail(GAN_E_ARG, why) : GAN_OK;
-}
-gan_status check_sizes(int32_t precision, long long rows, int cols) {
-  if (!precision_known(precision)) return operator_fail(GAN_E_ARG, "unknown precision");
-  if (rows < 0 || cols < 1) return operator_fail(GAN_E_ARG, "negative rows or no columns");
-  if (rows > MOST_ROWS || cols > MOST_COLS) return operator_fail(GAN_E_SHAPE, "more than 2^30 rows or 2^28 columns");
-  return GAN_OK;
-}
-
 }  // namespace
 }  // namespace gan
 

@@ -1,0 +1,196 @@
+"""Rows sorted by label, handed out and put together (GPU): every way the sort goes, labels of none, odd widths and strides, rows far apart; and the gradients.
+
+Bounds: a sum of k products and the residual in fp32 is off by at most k + 1 roundings of the terms' sum; a row's product by one for each of 8 chunks' elements in a lane's chain and log2(256) + 2
+more, at most cols / 256 + 20 in all; and one rounding of the storage type."""
+import numpy as np
+import pytest
+
+from paper_2102_10485_amd import binding as B
+from tests import experts_ref as E
+from tests import gpu_util as U
+from tests import operators_ref as R
+from tests.test_gpu_rms_norm import host, matrix
+
+pytestmark = pytest.mark.gpu
+
+
+def sort(labels, groups, order=True, place=True):
+    torch = U.torch_mod()
+    n = labels.size
+    t = torch.from_numpy(np.ascontiguousarray(labels, np.int32).ravel()).cuda()
+    offs, o, p = (torch.full((s + 4,), -77, dtype=torch.int32, device="cuda") for s in (groups + 1, n, n))
+    size = B.sort_by_label_bytes(n, groups)
+    work = torch.full((max(size, 16),), 255, dtype=torch.uint8, device="cuda")
+    B.sort_by_label(t.data_ptr() if n else 0, n, groups, offs.data_ptr(), o.data_ptr() if order else 0, p.data_ptr() if place else 0, work.data_ptr(), size)
+    torch.cuda.synchronize()
+    for v, used in ((offs, groups + 1), (o, n if order else 0), (p, n if place else 0)):
+        assert bool((v[used:] == -77).all())
+    return offs[:groups + 1], o[:n], p[:n]
+
+
+@pytest.mark.parametrize("n,groups", [(0, 5), (1, 1), (7, 0), (100, 3), (64, 64), (2048, 100), (2048, 512), (2000, 513), (2048, 2048), (1500, 2049), (2048, 4096), (2049, 7), (5000, 257),
+                                      (70001, 8), (9000, 2048), (30000, 4096), (600000, 256), (3000, 0)])
+def test_sort(n, groups):
+    for kind in ("drawn", "one", "none", "back"):
+        rng = np.random.default_rng([n, groups])
+        labels = rng.integers(-2, groups + 2, n) if kind == "drawn" else np.full(n, max(0, groups - 1)) if kind == "one" else np.full(n, -1) if kind == "none" else np.arange(n)[::-1] % (groups + 1)
+        if kind == "drawn" and n > 10:
+            labels[3], labels[5] = 2 ** 31 - 1, -2 ** 31
+        offs, order, place = (t.cpu().numpy() for t in sort(labels, groups))
+        for got, want in zip((offs, order, place), E.sort_by_label(labels, groups)):
+            assert np.array_equal(got, want), kind
+    sort(labels, groups, order=False)
+    sort(labels, groups, place=False)
+
+
+# rows, cols, k, groups
+SHAPES = [(1, 1, 1, 1), (5, 7, 2, 3), (30, 64, 3, 4), (17, 1000, 1, 10), (9, 1032, 5, 4), (40, 513, 8, 6), (3, 8200, 2, 2), (2, 40001, 9, 3), (300, 24, 4, 100), (6, 2048, 16, 40)]
+
+
+def problem(rows, cols, k, groups, bf16, seed=0):
+    rng = np.random.default_rng([rows, cols, k, seed])
+    m = lambda *s: U.round_to(rng.normal(size=s), bf16)  # noqa: E731
+    labels = rng.integers(-1, groups, (rows, k))
+    return labels, m(rows, cols), m(rows * k, cols), m(rows, cols), m(rows, cols), rng.random((rows, k)).astype(np.float32)
+
+
+def unwritten(m, offset, rows, stride, cols):
+    rest = m[0].clone()
+    rest[offset:offset + rows * stride].view(rows, stride)[:, :cols] = float("nan")
+    assert bool(rest.isnan().all())
+    return host(m[1])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("rows,cols,k,groups", SHAPES)
+def test_rows(rows, cols, k, groups, bf16):
+    torch = U.torch_mod()
+    prec, out_round = B.BF16 if bf16 else B.FP32, R.UBF if bf16 else 0
+    for pad, offset, weighted, in_place in ((0, 0, True, False), (8, 8, False, True), (3, 1, True, True)):
+        labels, x, out, res, dy, w = problem(rows, cols, k, groups, bf16, pad)
+        st, n = cols + pad, rows * k
+        offs, _, place = sort(labels, groups)
+        routed, at = int(offs[groups]), place.view(rows, k).cpu().numpy()
+        tw = torch.from_numpy(w).cuda()
+        pw, w = (tw.data_ptr(), w) if weighted else (0, None)
+        mx, mo, mr, md = (matrix(v, bf16, st, offset) for v in (x, out, res, dy))
+        mxs = matrix(np.full((n, cols), 7.0), bf16, st, offset)
+        B.gather_rows(prec, mx[2], st, place.data_ptr(), offs.data_ptr(), groups, k, rows, cols, mxs[2], st)
+        torch.cuda.synchronize()
+        assert np.array_equal(unwritten(mxs, offset, n, st, cols), E.gather(x, at, routed))
+        my = mr if in_place else matrix(np.zeros_like(x), bf16, st, offset)
+        use = pad != 8
+        B.combine_rows(prec, mo[2], st, place.data_ptr(), pw, offs.data_ptr(), groups, k, mr[2] if use or in_place else 0, st, rows, cols, my[2], st)
+        torch.cuda.synchronize()
+        want, size = E.combine(out, at, w, routed, res)
+        assert np.all(np.abs(unwritten(my, offset, rows, st, cols) - want) <= (k + 1) * R.U32 * size + out_round * np.abs(want))
+        # gradients
+        mdo = mo if in_place else matrix(np.full((n, cols), 7.0), bf16, st, offset)
+        dw = torch.full((n + 4,), float("nan"), device="cuda")
+        B.combine_rows_backward(prec, md[2], st, mo[2], st, place.data_ptr(), pw, offs.data_ptr(), groups, k, rows, cols, mdo[2], st, dw.data_ptr())
+        torch.cuda.synchronize()
+        want, dot, size = E.combine_backward(dy, out, at, w, routed)
+        assert np.all(np.abs(unwritten(mdo, offset, n, st, cols) - want) <= (R.U32 + out_round) * np.abs(want))
+        assert np.all(np.abs(dw[:n].view(rows, k).cpu().numpy() - dot) <= (cols / 256 + 20) * R.U32 * size) and bool(dw[n:].isnan().all())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_parts_of_the_gradient_alone(bf16):
+    torch = U.torch_mod()
+    rows, cols, k, groups = 20, 72, 2, 3
+    prec = B.BF16 if bf16 else B.FP32
+    labels, x, out, res, dy, w = problem(rows, cols, k, groups, bf16)
+    offs, _, place = sort(labels, groups)
+    tw, mo, md, mdo = torch.from_numpy(w).cuda(), matrix(out, bf16, cols), matrix(dy, bf16, cols), matrix(np.zeros_like(out), bf16, cols)
+    dw = torch.zeros((rows, k), device="cuda")
+    for a, b in ((mdo[2], 0), (0, dw.data_ptr()), (0, 0)):
+        B.combine_rows_backward(prec, md[2], cols, mo[2], cols, place.data_ptr(), tw.data_ptr(), offs.data_ptr(), groups, k, rows, cols, a, cols, b)
+    torch.cuda.synchronize()
+    want, dot, size = E.combine_backward(dy, out, place.view(rows, k).cpu().numpy(), w, int(offs[groups]))
+    assert np.all(np.abs(host(mdo[1]) - want) <= (R.U32 + (R.UBF if bf16 else 0)) * np.abs(want)) and np.all(np.abs(dw.cpu().numpy() - dot) <= 40 * R.U32 * size)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("cols", [64, 50, 2056])
+def test_places_and_offsets_that_are_none(cols, bf16):
+    """Places outside [0, rows * k) are skipped, offsets outside count as the nearest inside; rows of no expert are read nowhere, whatever they hold."""
+    torch = U.torch_mod()
+    rows, k = 6, 2
+    prec = B.BF16 if bf16 else B.FP32
+    rng = np.random.default_rng(2)
+    place = rng.permutation(rows * k).reshape(rows, k).astype(np.int32)
+    place[1, 0], place[2, 1], place[3, 1], place[4, 0] = -1, 12, 2 ** 31 - 1, -2 ** 31
+    x = rng.integers(-3, 4, (rows, cols)).astype(np.float32)
+    out = rng.integers(-3, 4, (rows * k, cols)).astype(np.float32)
+    tp = torch.from_numpy(place).cuda()
+    for last, routed in ((9, 9), (-4, 0), (1 << 30, 12)):
+        offs = torch.tensor([0, 5, last], dtype=torch.int32, device="cuda")
+        good = (place >= 0) & (place < routed)
+        hold = out.copy()
+        hold[routed:] = np.nan
+        mx, mo, ms, my, md, mdo = (matrix(v, bf16, cols) for v in (x, hold, np.full((rows * k, cols), 5.0), np.zeros((rows, cols)), x, np.full((rows * k, cols), 5.0)))
+        dw = torch.full((rows, k), 9.0, device="cuda")
+        B.gather_rows(prec, mx[2], cols, tp.data_ptr(), offs.data_ptr(), 2, k, rows, cols, ms[2], cols)
+        B.combine_rows(prec, mo[2], cols, tp.data_ptr(), 0, offs.data_ptr(), 2, k, 0, 0, rows, cols, my[2], cols)
+        B.combine_rows_backward(prec, md[2], cols, mo[2], cols, tp.data_ptr(), 0, offs.data_ptr(), 2, k, rows, cols, mdo[2], cols, dw.data_ptr())
+        torch.cuda.synchronize()
+        xs, dot = np.full((rows * k, cols), 5.0), np.zeros((rows, k))
+        y = np.zeros((rows, cols))
+        for i in range(rows):
+            for s in range(k):
+                if 0 <= place[i, s] < rows * k:
+                    xs[place[i, s]] = x[i] if good[i, s] else 0
+                if good[i, s]:
+                    y[i] += out[place[i, s]]
+                    dot[i, s] = (x[i] * out[place[i, s]]).sum()
+        assert np.array_equal(host(ms[1]), xs) and np.array_equal(host(my[1]), y) and np.array_equal(host(mdo[1]), xs) and np.array_equal(dw.cpu().numpy(), dot)
+
+
+def test_many_rows():
+    """More rows than a wave's block has at a time, whole numbers: exact."""
+    torch = U.torch_mod()
+    rows, cols, k, groups = 5000, 40, 2, 9
+    rng = np.random.default_rng(4)
+    labels = rng.integers(-1, groups, (rows, k))
+    offs, order, place = sort(labels, groups)
+    at, routed = place.view(rows, k).cpu().numpy(), int(offs[groups])
+    x, out = rng.integers(-3, 4, (rows, cols)).astype(np.float32), rng.integers(-3, 4, (rows * k, cols)).astype(np.float32)
+    w = rng.integers(0, 3, (rows, k)).astype(np.float32)
+    tx, to, tw = torch.from_numpy(x).cuda(), torch.from_numpy(out).cuda(), torch.from_numpy(w).cuda()
+    xs, y, dout, dw = torch.empty_like(to), torch.empty_like(tx), torch.empty_like(to), torch.empty_like(tw)
+    p, o = place.data_ptr(), offs.data_ptr()
+    B.gather_rows(B.FP32, tx.data_ptr(), cols, p, o, groups, k, rows, cols, xs.data_ptr(), cols)
+    B.combine_rows(B.FP32, to.data_ptr(), cols, p, tw.data_ptr(), o, groups, k, tx.data_ptr(), cols, rows, cols, y.data_ptr(), cols)
+    B.combine_rows_backward(B.FP32, tx.data_ptr(), cols, to.data_ptr(), cols, p, tw.data_ptr(), o, groups, k, rows, cols, dout.data_ptr(), cols, dw.data_ptr())
+    torch.cuda.synchronize()
+    want = E.combine_backward(x, out, at, w, routed)
+    for got, ref in ((xs, E.gather(x, at, routed)), (y, E.combine(out, at, w, routed, x)[0]), (dout, want[0]), (dw, want[1])):
+        assert np.array_equal(got.cpu().numpy(), ref)
+
+
+def test_rows_far_apart():
+    """Rows 2^31 elements apart (bf16: 4 GiB): three of x, six places."""
+    torch = U.torch_mod()
+    rows, k, cols, stride = 3, 2, 72, (1 << 31) + 8
+    a, b = (torch.zeros(n * stride + cols, dtype=torch.bfloat16, device="cuda") for n in (rows - 1, rows * k - 1))
+    place = torch.tensor([[5, 0], [1, 3], [4, 2]], dtype=torch.int32, device="cuda")
+    offs, dw = torch.tensor([0, 6], dtype=torch.int32, device="cuda"), torch.zeros((rows, k), device="cuda")
+    for r in range(rows):
+        a[r * stride:r * stride + cols] = r + 1
+    B.gather_rows(B.BF16, a.data_ptr(), stride, place.data_ptr(), offs.data_ptr(), 1, k, rows, cols, b.data_ptr(), stride)
+    torch.cuda.synchronize()
+    assert [float(b[p * stride + cols - 1]) for p in range(6)] == [1, 2, 3, 2, 3, 1]
+    B.combine_rows_backward(B.BF16, a.data_ptr(), stride, b.data_ptr(), stride, place.data_ptr(), 0, offs.data_ptr(), 1, k, rows, cols, b.data_ptr(), stride, dw.data_ptr())
+    B.combine_rows(B.BF16, b.data_ptr(), stride, place.data_ptr(), 0, offs.data_ptr(), 1, k, a.data_ptr(), stride, rows, cols, a.data_ptr(), stride)
+    torch.cuda.synchronize()
+    assert [float(a[r * stride + cols - 1]) for r in range(rows)] == [3, 6, 9]
+    assert np.array_equal(dw.cpu().numpy(), np.array([[1, 1], [4, 4], [9, 9]]) * 72.0)
+
+
+def test_no_rows():
+    torch = U.torch_mod()
+    offs = torch.zeros(4, dtype=torch.int32, device="cuda")
+    B.gather_rows(B.BF16, 0, 64, 0, offs.data_ptr(), 3, 2, 0, 64, 0, 64)
+    B.combine_rows(B.BF16, 0, 64, 0, 0, offs.data_ptr(), 3, 2, 0, 64, 0, 64, 0, 64)
+    B.combine_rows_backward(B.BF16, 0, 64, 0, 64, 0, 0, offs.data_ptr(), 3, 2, 0, 64, 0, 64, 0)
+    torch.cuda.synchronize()
