@@ -401,7 +401,7 @@ gan_status gan_group_act_backward(int32_t precision, const void* dy, int64_t dy_
    counts int32 [experts + 1] (or NULL; then mean and balance are NULL too): how many rows chose each expert, and how many rows have an expert at all; mean fp32 [experts] (or NULL): the
    mean of p over these rows (0 without any); balance fp32 [1] (or NULL): experts * sum over e of counts[e] / sum(counts) * mean[e], 1 where all experts get the same.
    A row of padding is one without an expert, all its logits -infinity.
-   At most 4096 experts, 16 choices, 2^30 choices in all.  work: DEVICE, gan_route_bytes(rows, experts), 16-byte aligned (counts NULL: none). */
+   At most 4096 experts, 16 choices, 2^30 choices in all.  work: DEVICE, gan_route_bytes(rows, experts) (0: none is needed), 16-byte aligned (counts NULL: none). */
 int64_t gan_route_bytes(int64_t rows, int32_t experts);
 gan_status gan_route(int32_t precision, const void* logits, int64_t logits_stride, int64_t rows, int32_t experts, int32_t k, int32_t normalize, int32_t* expert, float* weight,
                      int32_t* counts, float* mean, float* balance, void* work, int64_t work_bytes, void* hip_stream);

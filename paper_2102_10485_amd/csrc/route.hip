@@ -23,68 +23,136 @@ struct RouteArgs {
   const void* logits;
   int* expert;
   float* weight;
-  float* sums;                                                    // [blocks][experts]: of the probabilities, or NULL
-  int* counts;                                                    // [blocks][experts + 1]: choices of each expert, and rows that have one
+  int* counts;                                                    // the results, or NULL (then mean and balance are too)
+  float *mean, *balance;
+  int* ticket;                                                    // what several blocks leave: see Work
+  float* sums;
+  int* parts;
   long long stride, rows;
   int experts, k, normalize;
 };
 
-// Numbers as whole numbers of the same order; 0: not there.  -0 counts as 0.
-__device__ __forceinline__ unsigned key_of(float v) {
-  const unsigned u = __float_as_uint(v + 0.f);
-  return v > -INFINITY ? (u >> 31 ? ~u : u | 0x80000000u) : 0u;
-}
-__device__ __forceinline__ float value_of(unsigned key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
+constexpr float LOG2E = 1.44269504088896341f;
 
-template <int L>
-__device__ __forceinline__ unsigned most_of(unsigned v) {
-#pragma unroll
-  for (int d = 1; d < L; d *= 2) v = max(v, (unsigned)__shfl_xor((int)v, d));
+// ---- a row among L lanes ----
+
+// Joins the values of L neighbouring lanes; all of them get the result.  Within sixteen lanes the other operand comes by the instruction's own lane exchange (DPP): neighbours,
+// pairs, the mirrored eight, the mirrored sixteen.
+template <int CONTROL>
+__device__ __forceinline__ unsigned from_lane(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, 0xf, 0xf, true); }
+template <int L, typename F>
+__device__ __forceinline__ unsigned join(unsigned v, F&& f) {
+  if constexpr (L >= 2) v = f(v, from_lane<0xB1>(v));
+  if constexpr (L >= 4) v = f(v, from_lane<0x4E>(v));
+  if constexpr (L >= 8) v = f(v, from_lane<0x141>(v));
+  if constexpr (L >= 16) v = f(v, from_lane<0x140>(v));
+  if constexpr (L >= 32) v = f(v, (unsigned)__shfl_xor((int)v, 16));
+  if constexpr (L >= 64) v = f(v, (unsigned)__shfl_xor((int)v, 32));
   return v;
 }
 template <int L>
-__device__ __forceinline__ unsigned least_of(unsigned v) {
-#pragma unroll
-  for (int d = 1; d < L; d *= 2) v = min(v, (unsigned)__shfl_xor((int)v, d));
-  return v;
-}
+__device__ __forceinline__ unsigned most_of(unsigned v) { return join<L>(v, [](unsigned a, unsigned b) { return max(a, b); }); }
+template <int L>
+__device__ __forceinline__ unsigned least_of(unsigned v) { return join<L>(v, [](unsigned a, unsigned b) { return min(a, b); }); }
 template <int L>
 __device__ __forceinline__ float sum_of(float v) {
-#pragma unroll
-  for (int d = 1; d < L; d *= 2) v += __shfl_xor(v, d);
-  return v;
+  return __uint_as_float(join<L>(__float_as_uint(v), [](unsigned a, unsigned b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 
 // the expert of a lane's c-th logit
 template <int L>
 __device__ __forceinline__ int expert_of(int c) { return (c / 8 * L + (int)(threadIdx.x % L)) * 8 + c % 8; }
 
-// A row's keys; true where one of its logits is NaN.
+// Numbers as whole numbers of the same order; 0: not there.  -0 counts as 0.  A bf16 number leaves room for its expert below it, so that keys are all different and
+// equal numbers come in the experts' order.
+template <typename T>
+__device__ __forceinline__ unsigned key_of(float v, int expert) {
+  const unsigned u = __float_as_uint(v + 0.f), key = u >> 31 ? ~u : u | 0x80000000u;
+  return v > -INFINITY ? sizeof(T) == 4 ? key : (key & 0xffff0000u) | (0xffffu - expert) : 0u;
+}
+template <typename T>
+__device__ __forceinline__ float value_of(unsigned key) {
+  const unsigned u = key >> 31 ? key & 0x7fffffffu : ~key;
+  return __uint_as_float(sizeof(T) == 4 ? u : u & 0xffff0000u);
+}
+
+// A row's logits (-infinity behind its end) and keys.
 template <typename T, int L, int C>
-__device__ __forceinline__ bool load_keys(const T* row, int experts, bool in, unsigned (&key)[C]) {
-  bool bad = false;
+__device__ __forceinline__ void load_row(const T* row, int experts, float (&v)[C], unsigned (&key)[C]) {
 #pragma unroll
   for (int j = 0; j < C / 8; ++j) {
-    const int e = expert_of<L>(j * 8);
-    float v[8];
-    load8<T, false>(row + e, in ? experts - e : 0, v);
+    const int e = expert_of<L>(j * 8), left = experts - e;
+    float w[8];
+    load8<T, false>(row + e, left, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const bool is = in && e + i < experts;
-      key[j * 8 + i] = is ? key_of(v[i]) : 0u;
-      bad |= is && v[i] != v[i];
+      v[j * 8 + i] = i < left ? w[i] : -INFINITY;
+      key[j * 8 + i] = key_of<T>(v[j * 8 + i], e + i);
     }
   }
-  return bad;
 }
+template <int C>
+__device__ __forceinline__ unsigned most(const unsigned (&key)[C]) {
+  unsigned m = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) m = max(m, key[c]);
+  return m;
+}
+// v = exp(v - top); their sum over the row (NaN and +infinity make it NaN)
+template <int L, int C>
+__device__ __forceinline__ float powers(float (&v)[C], float top) {
+  float s = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    v[c] = __builtin_amdgcn_exp2f((v[c] - top) * LOG2E);
+    s += v[c];
+  }
+  return sum_of<L>(s);
+}
+
+// The row's next choice: its key (0: none) and expert.  `last` is the choice before it.
+template <typename T, int L, int C>
+__device__ __forceinline__ unsigned next_choice(unsigned (&key)[C], unsigned last, int& expert) {
+  if constexpr (sizeof(T) == 2) {
+    // The largest key below the last: less the last, modulo 2^32, keys below it are above all others.
+    unsigned m = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) m = max(m, key[c] - last);
+    m = most_of<L>(m) + last;
+    expert = m ? (int)(0xffffu - (m & 0xffffu)) : -1;
+    return m;
+  } else {
+    // (the key does not tell equal numbers apart: the lowest expert among them is found, and taken out)
+    const unsigned m = most_of<L>(most(key));
+    int mine = -1;
+#pragma unroll
+    for (int c = C - 1; c >= 0; --c) mine = key[c] == m ? c : mine;
+    const unsigned at = mine >= 0 ? (unsigned)((mine / 8 * L + (int)(threadIdx.x % L)) * 8 + mine % 8) : 0xffffffffu, first = least_of<L>(at);
+    mine = at == first ? mine : -1;
+#pragma unroll
+    for (int c = 0; c < C; ++c) key[c] = c == mine ? 0u : key[c];
+    expert = m ? (int)first : -1;
+    return m;
+  }
+}
+
+// ---- counts, means, balance ----
+
+constexpr int SUM_EXPERTS = 32;                                   // of a block of route_sum_kernel
+
+// The workspace of several blocks: a ticket for those of route_sum_kernel, their shares of the loss, and every block's sums and counts.
+struct Work {
+  static constexpr long long LOSS = 16, SUMS = LOSS + MOST_EXPERTS / SUM_EXPERTS * 16;
+  static long long bytes(int blocks, int experts) { return SUMS + (long long)blocks * (2 * experts + 1) * 4; }
+};
 
 template <typename T, int L, int C, bool STATS>
 __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
   constexpr int R = 256 / L;                                      // rows of a block at a time
   extern __shared__ __align__(16) unsigned char lds[];
-  int* ids = (int*)lds;
-  float* weights = (float*)lds + R * a.k;
-  int* hist = (int*)lds + 2 * R * a.k;
+  int* ids = (int*)lds;                                           // (where a row has fewer lanes than it may have choices)
+  float* weights = (float*)lds + (L < MOST_CHOICES ? R * a.k : 0);
+  int* hist = (int*)(weights + (L < MOST_CHOICES ? R * a.k : 0));
   float* wide = (float*)hist + (a.experts + 1);
   float total[C];
   if constexpr (STATS) {
@@ -97,54 +165,59 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
   for (long long first = (long long)blockIdx.x * R; first < a.rows; first += (long long)gridDim.x * R) {
     const long long row = first + at;
     const bool in = row < a.rows;
+    float v[C];
     unsigned key[C];
-    const bool bad = load_keys<T, L, C>((const T*)a.logits + (in ? row : 0) * a.stride, a.experts, in, key);
-    unsigned best = 0;
-#pragma unroll
-    for (int c = 0; c < C; ++c) best = max(best, key[c]);
-    best = most_of<L>(best);
-    const float top = value_of(best);
-    float s = 0.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) s += key[c] ? expf(value_of(key[c]) - top) : 0.f;
-    s = sum_of<L>(s);
-    if (most_of<L>(bad)) s = NAN;
-    const float inv = 1.f / s;
+    load_row<T, L, C>((const T*)a.logits + (in ? row : 0) * a.stride, in ? a.experts : 0, v, key);
+    const unsigned best = most_of<L>(most(key));
+    const float top = value_of<T>(best), inv = 1.f / powers<L>(v, top);
     if constexpr (STATS) {
       if (best) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) total[c] += key[c] ? expf(value_of(key[c]) - top) * inv : 0.f;
+        for (int c = 0; c < C; ++c) total[c] += key[c] ? v[c] * inv : 0.f;
         if (lane == 0) atomicAdd(&hist[a.experts], 1);
       }
     }
-    float of_all = 0.f;
+    float of_all = 0.f, my_p = 0.f;
+    int my_id = -1;
+    unsigned m = 0;
     for (int j = 0; j < a.k; ++j) {
-      unsigned m = 0, index = 0xffffffffu;
-#pragma unroll
-      for (int c = 0; c < C; ++c) m = max(m, key[c]);
-      m = most_of<L>(m);
-#pragma unroll
-      for (int c = 0; c < C; ++c) index = min(index, key[c] == m ? (unsigned)expert_of<L>(c) : 0xffffffffu);
-      index = least_of<L>(index);
-#pragma unroll
-      for (int c = 0; c < C; ++c) key[c] = (unsigned)expert_of<L>(c) == index ? 0u : key[c];
-      const float p = m ? expf(value_of(m) - top) * inv : 0.f;
+      int id;
+      if (j == 0 && sizeof(T) == 2) {
+        m = best;
+        id = m ? (int)(0xffffu - (m & 0xffffu)) : -1;
+      } else if (j == 0 || m) {                                   // (behind the last expert that is there all are none)
+        m = next_choice<T, L, C>(key, m, id);
+      } else {
+        id = -1;
+      }
+      const float p = m ? __builtin_amdgcn_exp2f((value_of<T>(m) - top) * LOG2E) * inv : 0.f;
       of_all += p;
-      if (lane == 0) {
-        ids[at * a.k + j] = m ? (int)index : -1;
+      if constexpr (L >= MOST_CHOICES) {
+        my_id = lane == j ? id : my_id;
+        my_p = lane == j ? p : my_p;
+      } else if (lane == 0) {
+        ids[at * a.k + j] = id;
         weights[at * a.k + j] = p;
-        if (STATS && m) atomicAdd(&hist[index], 1);
+        if (STATS && m) atomicAdd(&hist[id], 1);
       }
     }
-    if (a.normalize && lane == 0 && best)
-      for (int j = 0; j < a.k; ++j) weights[at * a.k + j] /= of_all;
-    __syncthreads();
-    const int n = (int)(a.rows - first < R ? a.rows - first : R) * a.k;
-    for (int i = threadIdx.x; i < n; i += 256) {
-      a.expert[first * a.k + i] = ids[i];
-      if (a.weight) a.weight[first * a.k + i] = weights[i];
+    if constexpr (L >= MOST_CHOICES) {
+      if (in && lane < a.k) {
+        if (STATS && my_id >= 0) atomicAdd(&hist[my_id], 1);
+        a.expert[row * a.k + lane] = my_id;
+        if (a.weight) a.weight[row * a.k + lane] = a.normalize && my_id >= 0 ? my_p / of_all : my_p;
+      }
+    } else {
+      if (a.normalize && lane == 0 && best)
+        for (int j = 0; j < a.k; ++j) weights[at * a.k + j] /= of_all;
+      __syncthreads();
+      const int n = (int)(a.rows - first < R ? a.rows - first : R) * a.k;
+      for (int i = threadIdx.x; i < n; i += 256) {
+        a.expert[first * a.k + i] = ids[i];
+        if (a.weight) a.weight[first * a.k + i] = weights[i];
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
   if constexpr (STATS) {
     // the rows of a wave first, then the four waves in order
@@ -152,6 +225,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int d = L; d < 64; d *= 2) total[c] += __shfl_xor(total[c], d);
+    __syncthreads();
     for (int w = 0; w < 4; ++w) {
       if ((int)(threadIdx.x >> 6) == w && (threadIdx.x & 63) < L)
 #pragma unroll
@@ -161,63 +235,120 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
         }
       __syncthreads();
     }
-    for (int e = threadIdx.x; e < a.experts; e += 256) a.sums[(long long)blockIdx.x * a.experts + e] = wide[e];
-    for (int e = threadIdx.x; e <= a.experts; e += 256) a.counts[(long long)blockIdx.x * (a.experts + 1) + e] = hist[e];
+    if (gridDim.x > 1) {
+      if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
+      for (int e = threadIdx.x; e < a.experts; e += 256) a.sums[(long long)blockIdx.x * a.experts + e] = wide[e];
+      for (int e = threadIdx.x; e <= a.experts; e += 256) a.parts[(long long)blockIdx.x * (a.experts + 1) + e] = hist[e];
+      return;
+    }
+    // the only block
+    __shared__ double loss[4];
+    __shared__ int all[4];
+    const int counted = hist[a.experts];
+    double mine = 0;
+    int chosen = 0;
+    for (int e = threadIdx.x; e <= a.experts; e += 256) {
+      a.counts[e] = hist[e];
+      if (e == a.experts) break;
+      const double p = (double)wide[e] / (counted > 0 ? counted : 1);
+      if (a.mean) a.mean[e] = (float)p;
+      mine += hist[e] * p;
+      chosen += hist[e];
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      mine += __shfl_xor(mine, d);
+      chosen += __shfl_xor(chosen, d);
+    }
+    if ((threadIdx.x & 63) == 0) {
+      loss[threadIdx.x >> 6] = mine;
+      all[threadIdx.x >> 6] = chosen;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && a.balance) {
+      const long long n = (long long)all[0] + all[1] + all[2] + all[3];
+      *a.balance = (float)(n > 0 ? (loss[0] + loss[1] + loss[2] + loss[3]) * a.experts / (double)n : 0.0);
+    }
   }
 }
 
-// counts, means and the balance loss from the blocks' sums
-__global__ __launch_bounds__(1024) void route_sum_kernel(const float* sums, const int* parts, int blocks, int experts, int* counts, float* mean, float* balance) {
+// Counts, means and the balance loss from the blocks' sums: a block for 32 experts, whose shares of the loss the last one adds up in order.
+__global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, double* loss, int blocks) {
   __shared__ int n[32][33];
   __shared__ double d[32][33];
-  __shared__ int rows;
-  const int c = threadIdx.x & 31, s = threadIdx.x >> 5;
+  __shared__ int rows, last;
+  const int c = threadIdx.x & 31, s = threadIdx.x >> 5, wave = threadIdx.x >> 6, e = blockIdx.x * SUM_EXPERTS + c;
   int counted = 0;
-  for (int b = threadIdx.x; b < blocks; b += 1024) counted += parts[(long long)b * (experts + 1) + experts];
-  n[s][c] = counted;
+  for (int b = threadIdx.x; b < blocks; b += 1024) counted += a.parts[(long long)b * (a.experts + 1) + a.experts];
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) counted += __shfl_xor(counted, x);
+  if ((threadIdx.x & 63) == 0) n[0][wave] = counted;
   __syncthreads();
   if (threadIdx.x == 0) {
     int t = 0;
-    for (int i = 0; i < 1024; ++i) t += n[i >> 5][i & 31];
+    for (int w = 0; w < 16; ++w) t += n[0][w];
     rows = t;
-    counts[experts] = t;
+    if (blockIdx.x == 0) a.counts[a.experts] = t;
   }
   __syncthreads();
-  double loss = 0;
-  long long all = 0;
-  for (int e0 = 0; e0 < experts; e0 += 32) {
-    const int e = e0 + c;
-    int t = 0;
-    double p = 0;
-    if (e < experts)
-      for (int b = s; b < blocks; b += 32) {
-        t += parts[(long long)b * (experts + 1) + e];
-        p += sums[(long long)b * experts + e];
+  int t = 0;
+  double p = 0;
+  if (e < a.experts)
+    for (int b = s; b < blocks; b += 256) {
+      int m[8];
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool in = b + 32 * i < blocks;
+        m[i] = in ? a.parts[(long long)(b + 32 * i) * (a.experts + 1) + e] : 0;
+        f[i] = in ? a.sums[(long long)(b + 32 * i) * a.experts + e] : 0.f;
       }
-    __syncthreads();
-    n[s][c] = t;
-    d[s][c] = p;
-    __syncthreads();
-    if (s == 0 && e < experts) {
-      for (int i = 1; i < 32; ++i) t += n[i][c], p += d[i][c];
-      p /= rows > 0 ? rows : 1;
-      counts[e] = t;
-      if (mean) mean[e] = (float)p;
-      loss += t * p;
-      all += t;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t += m[i], p += f[i];
     }
-  }
+  n[s][c] = t;
+  d[s][c] = p;
   __syncthreads();
   if (s == 0) {
-    d[0][c] = loss;
-    d[1][c] = (double)all;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0 && balance) {
-    for (int i = 1; i < 32; ++i) loss += d[0][i], all += (long long)d[1][i];
-    *balance = (float)(all > 0 ? loss * experts / (double)all : 0);
+    if (e < a.experts) {
+#pragma unroll
+      for (int i = 1; i < 32; ++i) t += n[i][c], p += d[i][c];
+      p /= rows > 0 ? rows : 1;
+      a.counts[e] = t;
+      if (a.mean) a.mean[e] = (float)p;
+    }
+    double share = t * p, all = t;
+#pragma unroll
+    for (int x = 1; x < 32; x *= 2) {
+      share += __shfl_xor(share, x);
+      all += __shfl_xor(all, x);
+    }
+    if (c == 0) {
+      __hip_atomic_store(&loss[2 * blockIdx.x], share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&loss[2 * blockIdx.x + 1], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+      if (last && a.balance) {
+        share = all = 0;
+        for (int b = 0; b < (int)gridDim.x; ++b) {
+          share += __hip_atomic_load(&loss[2 * b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          all += __hip_atomic_load(&loss[2 * b + 1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        *a.balance = (float)(all > 0 ? share * a.experts / all : 0);
+      }
+    }
   }
 }
+
+// without rows
+__global__ void route_none_kernel(int experts, int* counts, float* mean, float* balance) {
+  for (int e = threadIdx.x; e <= experts; e += 256) {
+    counts[e] = 0;
+    if (mean && e < experts) mean[e] = 0.f;
+  }
+  if (balance && threadIdx.x == 0) *balance = 0.f;
+}
+
+// ---- gradient ----
 
 struct RouteBackArgs {
   const void* logits;
@@ -229,10 +360,17 @@ struct RouteBackArgs {
   float balance_grad;
 };
 
+// dl_e = p_e (share_e - D) + extra_e, share_e = c counts_e.  extra is zero but for the choices, which are a lane's each: p_e g_e (then their sum is in D), or that of the softmax over
+// the choices, w_e (g_e - sum_j w_j g_j) with w_e = p_e / the choices' p.  They reach the lanes that hold their logits through a row of LDS.
 template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
-  constexpr int R = 256 / L;
+  constexpr int R = 256 / L, EACH = L < MOST_CHOICES ? MOST_CHOICES / L : 1;      // choices of a lane
+  __shared__ __align__(16) float rows_extra[R][L * C];
   __shared__ int part[4];
+  const int at = threadIdx.x / L, lane = threadIdx.x % L;
+  float* extra = rows_extra[at];
+#pragma unroll
+  for (int c = 0; c < C; ++c) extra[expert_of<L>(c)] = 0.f;
   float share[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) share[c] = 0.f;
@@ -252,97 +390,94 @@ __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
       share[c] = e < a.experts ? coefficient * (float)a.counts[e] : 0.f;
     }
   }
-  const int at = threadIdx.x / L;
+  __syncthreads();
   for (long long first = (long long)blockIdx.x * R; first < a.rows; first += (long long)gridDim.x * R) {
     const long long row = first + at;
     const bool in = row < a.rows;
-    unsigned key[C];
-    const bool bad = load_keys<T, L, C>((const T*)a.logits + (in ? row : 0) * a.stride, a.experts, in, key);
-    float g[C], p[C];
-    unsigned chosen[(C + 31) / 32] = {};
+    const T* logits = (const T*)a.logits + (in ? row : 0) * a.stride;
+    int id[EACH];
+    float g[EACH], l[EACH];
 #pragma unroll
-    for (int c = 0; c < C; ++c) g[c] = 0.f;
-    if (a.dweight && in)
-      for (int j = 0; j < a.k; ++j) {
-        const int e = a.expert[row * a.k + j];
-        const float dw = a.dweight[row * a.k + j];
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (expert_of<L>(c) == e) {
-            g[c] += dw;
-            chosen[c / 32] |= 1u << c % 32;
-          }
-      }
-    unsigned best = 0;
-#pragma unroll
-    for (int c = 0; c < C; ++c) best = max(best, key[c]);
-    best = most_of<L>(best);
-    const float top = value_of(best);
-    float s = 0.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      p[c] = key[c] ? expf(value_of(key[c]) - top) : 0.f;
-      s += p[c];
+    for (int i = 0; i < EACH; ++i) {
+      const int j = lane + i * L;
+      const bool is = a.dweight && in && j < a.k;
+      id[i] = is ? a.expert[row * a.k + j] : -1;
+      g[i] = is ? a.dweight[row * a.k + j] : 0.f;
+      if ((unsigned)id[i] >= (unsigned)a.experts) id[i] = -1;
+      l[i] = id[i] >= 0 ? to_float(logits[id[i]]) : 0.f;
     }
-    s = sum_of<L>(s);
-    if (most_of<L>(bad)) s = NAN;
-    const float inv = 1.f / s;
+    float v[C];
+    unsigned key[C];
+    load_row<T, L, C>(logits, in ? a.experts : 0, v, key);
+    const float top = value_of<T>(most_of<L>(most(key))), inv = 1.f / powers<L>(v, top);
     float mean = 0.f, of_chosen = 0.f, of_weights = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      p[c] = key[c] ? p[c] * inv : 0.f;
-      const bool is = chosen[c / 32] >> c % 32 & 1;
-      if (a.normalize) {
-        of_chosen += is ? p[c] : 0.f;
-        of_weights += is ? p[c] * g[c] : 0.f;
-        mean += p[c] * share[c];
-      } else {
-        mean += p[c] * (share[c] + g[c]);
-      }
-    }
-    mean = sum_of<L>(mean);
-    float over = 0.f, mean_weights = 0.f;
-    if (a.normalize) {
-      of_chosen = sum_of<L>(of_chosen);
-      of_weights = sum_of<L>(of_weights);
-      over = 1.f / of_chosen;
-      mean_weights = of_weights * over;
+      v[c] = key[c] ? v[c] * inv : 0.f;
+      mean += v[c] * share[c];
     }
 #pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      l[i] = id[i] >= 0 && l[i] > -INFINITY ? __builtin_amdgcn_exp2f((l[i] - top) * LOG2E) * inv : 0.f;      // its p
+      of_chosen += l[i];
+      of_weights += id[i] >= 0 ? l[i] * g[i] : 0.f;
+    }
+    mean = sum_of<L>(mean);
+    of_weights = sum_of<L>(of_weights);
+    if (a.normalize) {
+      const float over = 1.f / sum_of<L>(of_chosen);
+#pragma unroll
+      for (int i = 0; i < EACH; ++i)
+        if (id[i] >= 0) extra[id[i]] = l[i] * over * (g[i] - of_weights * over);
+    } else {
+      mean += of_weights;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i)
+        if (id[i] >= 0) extra[id[i]] = l[i] * g[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
     for (int j = 0; j < C / 8; ++j) {
+      const int e = expert_of<L>(j * 8);
       float d[8];
+      const float4 x = *reinterpret_cast<const float4*>(extra + e), y = *reinterpret_cast<const float4*>(extra + e + 4);
+      const float more[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int c = j * 8 + i;
-        const bool is = chosen[c / 32] >> c % 32 & 1;
-        if (a.normalize) d[i] = p[c] * (share[c] - mean) + (is && key[c] ? p[c] * over * (g[c] - mean_weights) : 0.f);
-        else d[i] = p[c] * (share[c] + g[c] - mean);
-        if (!key[c]) d[i] = 0.f;
+        d[i] = key[c] ? v[c] * (share[c] - mean) + more[i] : 0.f;
       }
-      const int e = expert_of<L>(j * 8);
       store8<T, false>((T*)a.dlogits + (in ? row : 0) * a.dstride + e, in ? a.experts - e : 0, d);
     }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+      if (id[i] >= 0) extra[id[i]] = 0.f;
   }
 }
 
-// lanes of a row
-int lanes_of(int experts) { return experts <= 8 ? 1 : experts <= 32 ? 4 : experts <= 128 ? 16 : 64; }
-long long tiles_of(long long rows, int experts) {
-  const int r = 256 / lanes_of(experts);
-  return (rows + r - 1) / r;
-}
-// Blocks that leave sums of their rows behind.
-int stat_blocks(long long rows, int experts) { return (int)std::min(tiles_of(rows, experts), 512ll); }
-
+// Lanes of a row and logits of a lane.
 template <typename F>
 void with_lanes(int experts, F&& go) {
-  if (experts <= 8) go(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
-  else if (experts <= 32) go(std::integral_constant<int, 4>(), std::integral_constant<int, 8>());
-  else if (experts <= 128) go(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
-  else if (experts <= 512) go(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
+  typedef std::integral_constant<int, 8> Eight;
+  if (experts <= 8) go(std::integral_constant<int, 1>(), Eight());
+  else if (experts <= 32) go(std::integral_constant<int, 4>(), Eight());
+  else if (experts <= 128) go(std::integral_constant<int, 16>(), Eight());
+  else if (experts <= 256) go(std::integral_constant<int, 16>(), std::integral_constant<int, 16>());
+  else if (experts <= 512) go(std::integral_constant<int, 16>(), std::integral_constant<int, 32>());
   else if (experts <= 1024) go(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
   else go(std::integral_constant<int, 64>(), std::integral_constant<int, 64>());
 }
+long long tiles_of(long long rows, int experts) {
+  const int r = 256 / (experts <= 8 ? 1 : experts <= 32 ? 4 : experts <= 512 ? 16 : 64);
+  return (rows + r - 1) / r;
+}
+// Blocks that leave sums of their rows behind.
+int stat_blocks(long long rows, int experts) { return (int)std::min(tiles_of(rows, experts), 1024ll); }
 
 gan_status check_route(int32_t precision, int64_t rows, int32_t experts, int32_t k, int64_t stride) {
   if (const gan_status s = check_sizes(precision, rows, experts)) return s;
@@ -360,7 +495,8 @@ using namespace gan;
 
 extern "C" int64_t gan_route_bytes(int64_t rows, int32_t experts) {
   if (rows < 1 || experts < 1 || rows > MOST_ROWS || experts > MOST_EXPERTS) return 0;
-  return (int64_t)stat_blocks(rows, experts) * (2 * experts + 1) * 4;
+  const int blocks = stat_blocks(rows, experts);
+  return blocks > 1 ? Work::bytes(blocks, experts) : 0;
 }
 
 extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t logits_stride, int64_t rows, int32_t experts, int32_t k, int32_t normalize, int32_t* expert,
@@ -373,25 +509,28 @@ extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t l
   if (rows == 0 && !counts) return GAN_OK;
   operator_launches();
   const hipStream_t st = (hipStream_t)hip_stream;
-  const int blocks = rows > 0 ? stat_blocks(rows, experts) : 0;
-  float* sums = (float*)work;
-  int* parts = (int*)work + (long long)blocks * experts;
-  if (rows > 0) {
-    const RouteArgs a = {logits, expert, weight, sums, parts, logits_stride, rows, experts, k, normalize};
-    with_lanes(experts, [&](auto l, auto c) {
-      constexpr int L = decltype(l)::value, C = decltype(c)::value;
-      const unsigned lds = (2 * (256 / L) * k + (counts ? 2 * experts + 1 : 0)) * 4;
-      const dim3 grid(counts ? (unsigned)blocks : (unsigned)std::min(tiles_of(rows, experts), 1ll << 20));
-      const auto go = [&](auto t) {
-        typedef decltype(t) T;
-        if (counts) hipLaunchKernelGGL((route_kernel<T, L, C, true>), grid, dim3(256), lds, st, a);
-        else hipLaunchKernelGGL((route_kernel<T, L, C, false>), grid, dim3(256), lds, st, a);
-      };
-      if (precision == GAN_FP32) go(float());
-      else go(bf16_t());
-    });
+  if (rows == 0) {
+    hipLaunchKernelGGL(route_none_kernel, dim3(1), dim3(256), 0, st, experts, counts, mean, balance);
+    return operator_launched();
   }
-  if (counts) hipLaunchKernelGGL(route_sum_kernel, dim3(1), dim3(1024), 0, st, sums, parts, blocks, experts, counts, mean, balance);
+  const int blocks = stat_blocks(rows, experts);
+  uint8_t* const w = (uint8_t*)work;
+  float* const sums = (float*)(w + Work::SUMS);
+  const RouteArgs a = {logits, expert, weight, counts, mean, balance, (int*)w, sums, (int*)(sums + (long long)blocks * experts), logits_stride, rows, experts, k, normalize};
+  with_lanes(experts, [&](auto l, auto c) {
+    constexpr int L = decltype(l)::value, C = decltype(c)::value;
+    const unsigned lds = ((L < MOST_CHOICES ? 2 * (256 / L) * k : 0) + (counts ? 2 * experts + 1 : 0)) * 4;
+    const dim3 grid(counts ? (unsigned)blocks : (unsigned)std::min(tiles_of(rows, experts), 1ll << 20));
+    const auto go = [&](auto t) {
+      typedef decltype(t) T;
+      if (counts) hipLaunchKernelGGL((route_kernel<T, L, C, true>), grid, dim3(256), lds, st, a);
+      else hipLaunchKernelGGL((route_kernel<T, L, C, false>), grid, dim3(256), lds, st, a);
+    };
+    if (precision == GAN_FP32) go(float());
+    else go(bf16_t());
+  });
+  if (counts && blocks > 1)
+    hipLaunchKernelGGL(route_sum_kernel, dim3((experts + SUM_EXPERTS - 1) / SUM_EXPERTS), dim3(1024), 0, st, a, (double*)(w + Work::LOSS), blocks);
   return operator_launched();
 }
 

@@ -57,14 +57,14 @@ def test_route():
               work_bytes=B.route_bytes(10, 64))
     each(B.route, ok, [(dict(precision=2), ARG, "precision"), (dict(logits=0), ARG, "NULL"), (dict(expert=0), ARG, "NULL"), (dict(k=0), ARG, "k is"), (dict(k=65), ARG, "k is"),
                        (dict(logits_stride=63), ARG, "stride"), (dict(rows=-1), ARG, "negative"), (dict(experts=0), ARG, "columns"), (dict(counts=0), ARG, "counts"),
-                       (dict(work=0), ARG, "work"), (dict(work_bytes=0), ARG, "work"), (dict(work=P + 8), ARG, "work"), (dict(k=17), SHAPE, "16 choices"),
+                       (dict(work=0, rows=500), ARG, "work"), (dict(work_bytes=0, rows=500), ARG, "work"), (dict(work=P + 8), ARG, "work"), (dict(k=17), SHAPE, "16 choices"),
                        (dict(experts=4097, logits_stride=4097), SHAPE, "4096"), (dict(rows=1 << 30), SHAPE, "2^30")])
     B.route(**{**ok, "rows": 0, "counts": 0, "mean": 0, "balance": 0})
     ok = dict(precision=B.BF16, logits=P, logits_stride=64, rows=10, experts=64, k=2, normalize=1, expert=P, dweight=P, counts=P, balance_grad=0.1, dlogits=P, dlogits_stride=64)
     each(B.route_backward, ok, [(dict(logits=0), ARG, "NULL"), (dict(dlogits=0), ARG, "NULL"), (dict(expert=0), ARG, "NULL"), (dict(dlogits_stride=63), ARG, "stride"),
                                 (dict(logits_stride=1), ARG, "stride"), (dict(k=65), ARG, "k is")])
     B.route_backward(**{**ok, "rows": 0})
-    assert B.route_bytes(0, 5) == 0 and B.route_bytes(1, 5) == 44 and B.route_bytes(5, 5000) == 0
+    assert B.route_bytes(0, 5) == 0 and B.route_bytes(1, 5) == 0 and B.route_bytes(5000, 5) > 0 and B.route_bytes(5, 5000) == 0
 
 
 def test_rows():
