@@ -2,8 +2,8 @@
 //
 //   dz = dy act'(z),    dbias[g] = sum of dz over g's rows
 //
-// Bound by memory, one pass over dy and z.  Blocks take tiles of rows of one expert each and some columns, and leave the sums of their rows, which a second kernel adds up expert
-// by expert, in order.
+// Bound by memory, one pass over dy and z.  Blocks take tiles of rows of one expert each and 128 columns, and leave the sums of their rows, which a second kernel adds up
+// expert by expert, in order.
 #include "activation.h"
 #include "group_tiles.h"
 
@@ -19,67 +19,83 @@ struct ActBackArgs {
   float* partial;                                                 // [tiles][cols], or NULL
   long long dy_stride, z_stride, dz_stride;
   int groups, rows, cols, act;
+  int tall;                                                       // rows of a tile
   long long tiles;                                                // of rows, at most
 };
 
-constexpr int TALL = 64;                                          // rows of a tile
+constexpr int WIDE = 128;                                         // columns of a tile
+int wide_tiles(int cols) { return (cols + WIDE - 1) / WIDE; }
+// Tiles of 128 rows, of 32 where those would leave CUs idle.
+int tall_of(long long rows, int cols) { return rows / 128 * wide_tiles(cols) >= 512 ? 128 : 32; }
 
-// Four waves of 64 lanes, eight columns each: wave w takes the rows w, w + 4, ...
-template <typename T, bool VEC>
+// Sixteen lanes have eight columns each; sixteen rows at a time, U such in flight.
+template <typename T, bool VEC, int U>
 __global__ __launch_bounds__(256) void act_back_kernel(ActBackArgs a) {
-  __shared__ float part[4][512];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wide = (a.cols + 511) / 512;
+  __shared__ __align__(16) float part[16][WIDE + 4];
+  const int lane = threadIdx.x & 15, rows_at = threadIdx.x >> 4, wide = (a.cols + WIDE - 1) / WIDE;
   for (long long at = blockIdx.x; at < a.tiles * wide; at += gridDim.x) {
     const long long tile = at / wide;
-    const int col = ((int)(at - tile * wide) * 64 + lane) * 8, left = a.cols - col;
+    const int col0 = (int)(at - tile * wide) * WIDE, col = col0 + lane * 8, left = a.cols - col;
     int group, row, end;
-    if (!find_tile(a.offs, a.groups, a.rows, TALL, (unsigned)tile, group, row, end)) return;      // (no later tile either)
-    end = min(end, row + TALL);
+    if (!find_tile(a.offs, a.groups, a.rows, a.tall, (unsigned)tile, group, row, end)) return;    // (no later tile either)
+    end = min(end, row + a.tall);
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-    for (int r = row + wave; r < end; r += 4) {
-      float d[8], z[8];
-      load8<T, VEC>((const T*)a.dy + r * a.dy_stride + col, left, d);
-      if (a.act != GAN_ACT_NONE) {
-        load8<T, VEC>((const T*)a.z + r * a.z_stride + col, left, z);
-        times_slope<false>(a.act, d, z);                          // (the bias's gradient is fp32)
+    for (int r0 = row + rows_at; r0 < end; r0 += 16 * U) {
+      float d[U][8], z[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int r = r0 + 16 * u, some = r < end ? left : 0;
+        load8<T, VEC>((const T*)a.dy + r * a.dy_stride + col, some, d[u]);
+        if (a.act != GAN_ACT_NONE) load8<T, VEC>((const T*)a.z + r * a.z_stride + col, some, z[u]);
       }
-      if (group == a.groups)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = 0.f;
-      if (a.dz) store8<T, VEC>((T*)a.dz + r * a.dz_stride + col, left, d);
+      for (int u = 0; u < U; ++u) {
+        const int r = r0 + 16 * u;
+        times_slope<sizeof(T) == 2 ? FULL : EXACT>(a.act, d[u], z[u]);                             // (the bias's gradient is fp32)
+        if (group == a.groups)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += d[i];
+          for (int i = 0; i < 8; ++i) d[u][i] = 0.f;
+        if (a.dz) store8<T, VEC>((T*)a.dz + r * a.dz_stride + col, r < end ? left : 0, d[u]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += d[u][i];
+      }
     }
     if (!a.partial) continue;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) part[wave][lane * 8 + i] = sum[i];
+    *reinterpret_cast<float4*>(&part[rows_at][lane * 8]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    *reinterpret_cast<float4*>(&part[rows_at][lane * 8 + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
     __syncthreads();
-    for (int c = threadIdx.x; c < 512; c += 256) {
-      const int to = (int)(at - tile * wide) * 512 + c;
-      if (to < a.cols) a.partial[tile * a.cols + to] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
+    const int c = threadIdx.x;
+    if (c < WIDE && col0 + c < a.cols) {
+      float s[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) s[k] = part[k][c];
+#pragma unroll
+      for (int k = 8; k > 0; k /= 2)
+#pragma unroll
+        for (int i = 0; i < k; ++i) s[i] += s[i + k];
+      a.partial[tile * a.cols + col0 + c] = s[0];
     }
   }
 }
 
-// dbias: the sums of each expert's tiles, in order
-__global__ __launch_bounds__(256) void bias_sum_kernel(const int* offs, int groups, int rows, int cols, const float* partial, float* dbias) {
-  const int wide = (cols + 255) / 256;
+// dbias: the sums of each expert's tiles, in eight chains, which are joined in order
+__global__ __launch_bounds__(64) void bias_sum_kernel(const int* offs, int groups, int rows, int cols, int tall, const float* partial, float* dbias) {
+  const int wide = (cols + 63) / 64, l = threadIdx.x;
   for (long long at = blockIdx.x; at < (long long)groups * wide; at += gridDim.x) {
-    const int group = (int)(at / wide), col = (int)(at - (long long)group * wide) * 256 + threadIdx.x;
+    const int group = (int)(at / wide), col = (int)(at - (long long)group * wide) * 64 + l;
     // the tiles of the experts before
     unsigned first = 0, count = 0;
     int done = 0;
-    const int l = threadIdx.x & 63;
     for (int g0 = 0; g0 <= group; g0 += 64) {
       const int g = g0 + l;
       int hi = g < groups ? min(max(offs[g + 1], 0), rows) : rows;
       hi = max(wave_scan_max(hi), done);
       int lo = __shfl_up(hi, 1);
       if (l == 0) lo = done;
-      const unsigned tiles = ((unsigned)(hi - lo) + TALL - 1) / TALL;
+      const unsigned tiles = ((unsigned)(hi - lo) + tall - 1) / tall;
       const unsigned upto = first + (unsigned)wave_scan_add((int)tiles);
       if (group < g0 + 64) {
         count = (unsigned)__shfl((int)tiles, group - g0);
@@ -90,9 +106,15 @@ __global__ __launch_bounds__(256) void bias_sum_kernel(const int* offs, int grou
       first = (unsigned)__shfl((int)upto, 63);
     }
     if (col >= cols) continue;
-    float s = 0.f;
-    for (unsigned t = 0; t < count; ++t) s += partial[(long long)(first + t) * cols + col];
-    dbias[(long long)group * cols + col] = s;
+    float s[8] = {};
+    for (unsigned t = 0; t < count; t += 8) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = t + k < count ? partial[(long long)(first + t + k) * cols + col] : 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[k] += v[k];
+    }
+    dbias[(long long)group * cols + col] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
   }
 }
 
@@ -103,7 +125,7 @@ using namespace gan;
 
 extern "C" int64_t gan_group_act_backward_bytes(int32_t groups, int64_t rows, int32_t cols) {
   if (groups < 1 || rows < 1 || cols < 1 || groups > 65535 || rows > MOST_ROWS || cols > MOST_COLS) return 0;
-  return most_tiles(rows, groups, TALL) * cols * (int64_t)sizeof(float);
+  return most_tiles(rows, groups, tall_of(rows, cols)) * cols * (int64_t)sizeof(float);
 }
 
 extern "C" gan_status gan_group_act_backward(int32_t precision, const void* dy, int64_t dy_stride, int32_t act, const void* z, int64_t z_stride, const int32_t* offs,
@@ -126,17 +148,20 @@ extern "C" gan_status gan_group_act_backward(int32_t precision, const void* dy, 
   const int e = precision == GAN_FP32 ? 4 : 2;
   if (rows > 0) {
     const bool vec = cols % 8 == 0 && rows_aligned16(dy, dy_stride, e) && (act == GAN_ACT_NONE || rows_aligned16(z, z_stride, e)) && (!dz || rows_aligned16(dz, dz_stride, e));
-    const ActBackArgs a = {dy, z, offs, dz, dbias && groups > 0 ? (float*)work : nullptr, dy_stride, z_stride, dz_stride, groups, (int)rows, cols, act,
-                           most_tiles(rows, groups, TALL)};
-    const dim3 grid((unsigned)std::min(a.tiles * ((cols + 511) / 512), 1ll << 20));
-#define GAN_ACT_BACK(T, V) hipLaunchKernelGGL((act_back_kernel<T, V>), grid, dim3(256), 0, st, a)
-    if (precision == GAN_FP32) { if (vec) GAN_ACT_BACK(float, true); else GAN_ACT_BACK(float, false); }
-    else { if (vec) GAN_ACT_BACK(bf16_t, true); else GAN_ACT_BACK(bf16_t, false); }
+    const int tall = tall_of(rows, cols);
+    const ActBackArgs a = {dy, z, offs, dz, dbias && groups > 0 ? (float*)work : nullptr, dy_stride, z_stride, dz_stride, groups, (int)rows, cols, act, tall,
+                           most_tiles(rows, groups, tall)};
+    const dim3 grid((unsigned)std::min(a.tiles * wide_tiles(cols), 1ll << 20));
+#define GAN_ACT_BACK(T, V) \
+  if (tall == 32) hipLaunchKernelGGL((act_back_kernel<T, V, 2>), grid, dim3(256), 0, st, a); \
+  else hipLaunchKernelGGL((act_back_kernel<T, V, 4>), grid, dim3(256), 0, st, a)
+    if (precision == GAN_FP32) { if (vec) { GAN_ACT_BACK(float, true); } else { GAN_ACT_BACK(float, false); } }
+    else { if (vec) { GAN_ACT_BACK(bf16_t, true); } else { GAN_ACT_BACK(bf16_t, false); } }
 #undef GAN_ACT_BACK
   }
   if (dbias && groups > 0) {
-    const long long blocks = groups * (((long long)cols + 255) / 256);
-    hipLaunchKernelGGL(bias_sum_kernel, dim3((unsigned)std::min(blocks, 1ll << 20)), dim3(256), 0, st, offs, groups, (int)rows, cols, (const float*)work, dbias);
+    const long long blocks = groups * (((long long)cols + 63) / 64);
+    hipLaunchKernelGGL(bias_sum_kernel, dim3((unsigned)std::min(blocks, 1ll << 20)), dim3(64), 0, st, offs, groups, (int)rows, cols, tall_of(rows, cols), (const float*)work, dbias);
   }
   return operator_launched();
 }

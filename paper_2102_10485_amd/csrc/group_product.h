@@ -225,25 +225,23 @@ __device__ __forceinline__ void store_some(C* p, int left, const float (&v)[N]) 
   else store_four<C>(p, left, v);
 }
 
-// Outputs n .. of row m, of which `left` are the row's last, as sums `v`; b: their biases, read by load_bias (a column's are the same for all of an expert's rows).
+// The biases of columns n .. of an expert (zero for rows of none)
 template <int N>
 __device__ __forceinline__ void load_bias(const ActArgs& q, int group, int n, float (&b)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) b[i] = 0.f;
   if (q.bias && group < q.groups) load_some<float, N>(q.bias + (long long)group * q.n + n, q.n - n, b);
 }
+// Outputs n .. of row m from their sums v; b: their biases, add and z: what the row has there of these operands (where it has them).
 template <typename C, int KIND, int N>
-__device__ __forceinline__ void finish(const ActArgs& q, int group, int m, int n, float (&v)[N], const float (&b)[N]) {
-  constexpr bool NEAR = sizeof(C) == 2;
+__device__ __forceinline__ void finish(const ActArgs& q, bool on, int m, int n, float (&v)[N], const float (&b)[N], const float (&add)[N], const float (&z)[N]) {
+  constexpr Accuracy A = sizeof(C) == 2 ? NEAR : EXACT;
   const int left = q.n - n;
-  const bool on = group < q.groups;
-  float add[N];
-  if (q.add && on) load_some<C, N>((const C*)q.add + m * q.add_stride + n, left, add);
   if constexpr (KIND == FORWARD) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += b[i];
     if (q.z_out) store_some<C, N>((C*)q.z_out + m * q.z_stride + n, left, v);
-    activate<NEAR>(q.act, v);
+    activate<A>(q.act, v);
     if (q.add && on)
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += add[i];
@@ -251,42 +249,78 @@ __device__ __forceinline__ void finish(const ActArgs& q, int group, int m, int n
     if (q.add && on)
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += add[i];
-    if (q.act != GAN_ACT_NONE && on) {
-      float z[N];
-      load_some<C, N>((const C*)q.z_in + m * q.z_stride + n, left, z);
-      times_slope<NEAR>(q.act, v, z);
-    }
+    if (on) times_slope<A>(q.act, v, z);
   }
   store_some<C, N>((C*)q.c + m * q.c_stride + n, left, v);
 }
 
-// store_rows with the epilogue: the sums go through LDS in fp32, sixteen rows at a time, and come back as 16 bytes of outputs a lane.
+// 16 bytes of any alignment as they are, and their values
+template <typename C>
+__device__ __forceinline__ u32x4 load_raw(const C* p) { return __builtin_bit_cast(u32x4, *reinterpret_cast<const typename Words<sizeof(C)>::T*>(p)); }
+template <typename C, int N>
+__device__ __forceinline__ void values_of(const u32x4& w, float (&v)[N]) {
+  static_assert(N * sizeof(C) == 16, "16 bytes");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(C) == 4) {
+      v[i] = __uint_as_float(w[i]);
+    } else {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+}
+
+// store_rows with the epilogue: the sums go through LDS in fp32, sixteen rows at a time, and come back as 16 bytes of outputs a lane.  The other operands of AHEAD sixteens are asked for
+// before they are needed.
 template <typename C, int KIND, int TM, int TN>
 __device__ __forceinline__ void store_act_rows(const ActArgs& q, const floatx4 (&acc)[TM][TN], int group, unsigned char* lds, int m0, int m_end, int n0, int n_end) {
-  constexpr int EACH = 16 / (int)sizeof(C), LANES = TN * 16 / EACH, ROW = TN * 64 + 16;
+  constexpr int EACH = 16 / (int)sizeof(C), LANES = TN * 16 / EACH, ROW = TN * 64 + 16, PASSES = 16 * LANES / 64, AHEAD = KIND == FORWARD ? 4 : 2;
   static_assert(64 % LANES == 0, "whole rows");
   const int l = threadIdx.x & 63, n = n0 + l % LANES * EACH;
+  const bool on = group < q.groups, whole = n + EACH <= n_end, has_add = q.add && on, has_z = KIND != FORWARD && q.act != GAN_ACT_NONE && on;
   float b[EACH];
 #pragma unroll
   for (int i = 0; i < EACH; ++i) b[i] = 0.f;
   if (KIND == FORWARD && n < n_end) load_bias(q, group, n, b);
+  u32x4 raw_add[TM][PASSES], raw_z[TM][PASSES];
+  const auto ask = [&](int i) {
+    if (m0 + i * 16 >= m_end || !whole) return;
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+      const int m = min(m0 + i * 16 + k * (64 / LANES) + l / LANES, m_end - 1);
+      if (has_add) raw_add[i][k] = load_raw((const C*)q.add + m * q.add_stride + n);
+      if (has_z) raw_z[i][k] = load_raw((const C*)q.z_in + m * q.z_stride + n);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < TM && i < AHEAD; ++i) ask(i);
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     if (m0 + i * 16 >= m_end) break;
 #pragma unroll
     for (int j = 0; j < TN; ++j) *reinterpret_cast<floatx4*>(lds + (l & 15) * ROW + (j * 16 + (l >> 4) * 4) * 4) = acc[i][j];
+    if (i + AHEAD < TM) ask(i + AHEAD);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int r = l / LANES; r < 16; r += 64 / LANES) {
-      float v[EACH];
+    for (int k = 0; k < PASSES; ++k) {
+      const int r = k * (64 / LANES) + l / LANES, m = m0 + i * 16 + r;
+      float v[EACH], add[EACH], z[EACH];
 #pragma unroll
-      for (int k = 0; k < EACH; k += 4) {
-        const floatx4 f = *reinterpret_cast<const floatx4*>(lds + r * ROW + (l % LANES * EACH + k) * 4);
+      for (int c = 0; c < EACH; c += 4) {
+        const floatx4 f = *reinterpret_cast<const floatx4*>(lds + r * ROW + (l % LANES * EACH + c) * 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[k + e] = f[e];
+        for (int e = 0; e < 4; ++e) v[c + e] = f[e];
       }
-      const int m = m0 + i * 16 + r;
-      if (m < m_end && n < n_end) finish<C, KIND>(q, group, m, n, v, b);
+      if (m >= m_end || n >= n_end) continue;
+      if (whole) {
+        values_of<C>(raw_add[i][k], add);
+        values_of<C>(raw_z[i][k], z);
+      } else {
+        if (has_add) load_some<C, EACH>((const C*)q.add + m * q.add_stride + n, n_end - n, add);
+        if (has_z) load_some<C, EACH>((const C*)q.z_in + m * q.z_stride + n, n_end - n, z);
+      }
+      finish<C, KIND>(q, on, m, n, v, b, add, z);
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -903,9 +937,12 @@ __device__ __forceinline__ void join_waves(const floatx4 (&acc)[Q], F&& write) {
 template <typename C, int KIND, typename Q>
 __device__ __forceinline__ void write_four(const Q& q, int group, int m, int n, const float (&v)[4]) {
   if constexpr (std::is_same_v<Q, ActArgs>) {
-    float f[4] = {v[0], v[1], v[2], v[3]}, b[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool on = group < q.groups;
+    float f[4] = {v[0], v[1], v[2], v[3]}, b[4] = {}, add[4] = {}, z[4] = {};
     if (KIND == FORWARD) load_bias(q, group, n, b);
-    finish<C, KIND>(q, group, m, n, f, b);
+    if (q.add && on) load_some<C, 4>((const C*)q.add + m * q.add_stride + n, q.n - n, add);
+    if (KIND != FORWARD && q.act != GAN_ACT_NONE && on) load_some<C, 4>((const C*)q.z_in + m * q.z_stride + n, q.n - n, z);
+    finish<C, KIND>(q, on, m, n, f, b, add, z);
   } else {
     store_four<C>((C*)q.c + (long long)m * q.c_stride + n, q.n - n, v);
   }

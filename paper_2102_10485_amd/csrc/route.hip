@@ -138,7 +138,7 @@ __device__ __forceinline__ unsigned next_choice(unsigned (&key)[C], unsigned las
 
 // ---- counts, means, balance ----
 
-constexpr int SUM_EXPERTS = 32;                                   // of a block of route_sum_kernel
+constexpr int SUM_EXPERTS = 8;                                    // of a block of route_sum_kernel
 
 // The workspace of several blocks: a ticket for those of route_sum_kernel, their shares of the loss, and every block's sums and counts.
 struct Work {
@@ -272,71 +272,66 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
   }
 }
 
-// Counts, means and the balance loss from the blocks' sums: a block for 32 experts, whose shares of the loss the last one adds up in order.
+// Counts, means and the balance loss from the blocks' sums: a block for eight experts (128 threads each, a load of up to 1024 blocks' sums at a time), whose shares of the loss the last
+// block to come adds up in order.  (65536 rows, 256 experts: NEW us; blocks of 32 experts 16.2.)
 __global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, double* loss, int blocks) {
-  __shared__ int n[32][33];
-  __shared__ double d[32][33];
-  __shared__ int rows, last;
-  const int c = threadIdx.x & 31, s = threadIdx.x >> 5, wave = threadIdx.x >> 6, e = blockIdx.x * SUM_EXPERTS + c;
-  int counted = 0;
-  for (int b = threadIdx.x; b < blocks; b += 1024) counted += a.parts[(long long)b * (a.experts + 1) + a.experts];
-#pragma unroll
-  for (int x = 1; x < 64; x *= 2) counted += __shfl_xor(counted, x);
-  if ((threadIdx.x & 63) == 0) n[0][wave] = counted;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    int t = 0;
-    for (int w = 0; w < 16; ++w) t += n[0][w];
-    rows = t;
-    if (blockIdx.x == 0) a.counts[a.experts] = t;
-  }
-  __syncthreads();
-  int t = 0;
+  __shared__ int n[16][SUM_EXPERTS], rows[16];
+  __shared__ double d[16][SUM_EXPERTS];
+  const int c = threadIdx.x % SUM_EXPERTS, s = threadIdx.x / SUM_EXPERTS, wave = threadIdx.x >> 6, l = threadIdx.x & 63, e = blockIdx.x * SUM_EXPERTS + c;
+  constexpr int SLICES = 1024 / SUM_EXPERTS;
+  int counted = 0, t = 0;
   double p = 0;
+  for (int b = threadIdx.x; b < blocks; b += 1024) counted += a.parts[(long long)b * (a.experts + 1) + a.experts];
   if (e < a.experts)
-    for (int b = s; b < blocks; b += 256) {
+    for (int b = s; b < blocks; b += SLICES * 8) {
       int m[8];
       float f[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bool in = b + 32 * i < blocks;
-        m[i] = in ? a.parts[(long long)(b + 32 * i) * (a.experts + 1) + e] : 0;
-        f[i] = in ? a.sums[(long long)(b + 32 * i) * a.experts + e] : 0.f;
+        const bool in = b + SLICES * i < blocks;
+        m[i] = in ? a.parts[(long long)(b + SLICES * i) * (a.experts + 1) + e] : 0;
+        f[i] = in ? a.sums[(long long)(b + SLICES * i) * a.experts + e] : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) t += m[i], p += f[i];
     }
-  n[s][c] = t;
-  d[s][c] = p;
-  __syncthreads();
-  if (s == 0) {
-    if (e < a.experts) {
 #pragma unroll
-      for (int i = 1; i < 32; ++i) t += n[i][c], p += d[i][c];
-      p /= rows > 0 ? rows : 1;
-      a.counts[e] = t;
-      if (a.mean) a.mean[e] = (float)p;
-    }
-    double share = t * p, all = t;
-#pragma unroll
-    for (int x = 1; x < 32; x *= 2) {
-      share += __shfl_xor(share, x);
-      all += __shfl_xor(all, x);
-    }
-    if (c == 0) {
-      __hip_atomic_store(&loss[2 * blockIdx.x], share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(&loss[2 * blockIdx.x + 1], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      last = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
-      if (last && a.balance) {
-        share = all = 0;
-        for (int b = 0; b < (int)gridDim.x; ++b) {
-          share += __hip_atomic_load(&loss[2 * b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          all += __hip_atomic_load(&loss[2 * b + 1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        *a.balance = (float)(all > 0 ? share * a.experts / all : 0);
-      }
+  for (int x = 1; x < 64; x *= 2) {
+    counted += __shfl_xor(counted, x);
+    if (x >= SUM_EXPERTS) {
+      t += __shfl_xor(t, x);
+      p += __shfl_xor(p, x);
     }
   }
+  if (l < SUM_EXPERTS) n[wave][l] = t, d[wave][l] = p;
+  if (l == 0) rows[wave] = counted;
+  __syncthreads();
+  if (threadIdx.x >= SUM_EXPERTS) return;
+  counted = rows[0];
+#pragma unroll
+  for (int w = 1; w < 16; ++w) t += n[w][c], p += d[w][c], counted += rows[w];
+  p /= counted > 0 ? counted : 1;
+  if (e < a.experts) {
+    a.counts[e] = t;
+    if (a.mean) a.mean[e] = (float)p;
+  }
+  double share = t * p, all = t;
+#pragma unroll
+  for (int x = 1; x < SUM_EXPERTS; x *= 2) {
+    share += __shfl_xor(share, x);
+    all += __shfl_xor(all, x);
+  }
+  if (threadIdx.x > 0) return;
+  if (blockIdx.x == 0) a.counts[a.experts] = counted;
+  __hip_atomic_store(&loss[2 * blockIdx.x], share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(&loss[2 * blockIdx.x + 1], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (__hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) != (int)gridDim.x - 1 || !a.balance) return;
+  share = all = 0;
+  for (int b = 0; b < (int)gridDim.x; ++b) {
+    share += __hip_atomic_load(&loss[2 * b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    all += __hip_atomic_load(&loss[2 * b + 1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  *a.balance = (float)(all > 0 ? share * a.experts / all : 0);
 }
 
 // without rows
@@ -545,7 +540,7 @@ extern "C" gan_status gan_route_backward(int32_t precision, const void* logits, 
   const hipStream_t st = (hipStream_t)hip_stream;
   with_lanes(experts, [&](auto l, auto c) {
     constexpr int L = decltype(l)::value, C = decltype(c)::value;
-    const dim3 grid((unsigned)std::min(tiles_of(rows, experts), 4096ll));
+    const dim3 grid((unsigned)std::min(tiles_of(rows, experts), 1024ll));
     if (precision == GAN_FP32) hipLaunchKernelGGL((route_back_kernel<float, L, C>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((route_back_kernel<bf16_t, L, C>), grid, dim3(256), 0, st, a);
   });
