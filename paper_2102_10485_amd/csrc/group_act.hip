@@ -23,16 +23,18 @@ struct ActBackArgs {
   long long tiles;                                                // of rows, at most
 };
 
-constexpr int WIDE = 128;                                         // columns of a tile
+// Tiles of 128 rows and 128 columns, of 32 rows where those would leave CUs idle.  A wave then reads 256 bytes of each of four rows at a time, and the blocks that run together whole rows
+// (bf16, 16384 x 4096 of eight experts with both launches: 83 us = 4.9 TB/s; 1 KiB of a row by a wave 95; results through the caches 87; operands converted as they arrive, two waves a SIMD 157;
+// ten experts' 1117 rows of 512 in fp32 7.9).
+constexpr int LANES = 16, WIDE = LANES * 8, AT = 256 / LANES;     // lanes of a row, columns of a tile, its rows at a time
 int wide_tiles(int cols) { return (cols + WIDE - 1) / WIDE; }
-// Tiles of 128 rows, of 32 where those would leave CUs idle.
 int tall_of(long long rows, int cols) { return rows / 128 * wide_tiles(cols) >= 512 ? 128 : 32; }
 
-// Sixteen lanes have eight columns each; sixteen rows at a time, U such in flight.
-template <typename T, bool VEC, int U>
-__global__ __launch_bounds__(256) void act_back_kernel(ActBackArgs a) {
-  __shared__ __align__(16) float part[16][WIDE + 4];
-  const int lane = threadIdx.x & 15, rows_at = threadIdx.x >> 4, wide = (a.cols + WIDE - 1) / WIDE;
+// A lane has eight columns of every sixteenth row, U of them in flight.
+template <typename T, bool VEC, bool PAST, int U>
+__global__ __launch_bounds__(256, 4) void act_back_kernel(ActBackArgs a) {
+  __shared__ __align__(16) float part[AT][WIDE + 4];
+  const int lane = threadIdx.x % LANES, rows_at = threadIdx.x / LANES, wide = (a.cols + WIDE - 1) / WIDE;
   for (long long at = blockIdx.x; at < a.tiles * wide; at += gridDim.x) {
     const long long tile = at / wide;
     const int col0 = (int)(at - tile * wide) * WIDE, col = col0 + lane * 8, left = a.cols - col;
@@ -42,24 +44,27 @@ __global__ __launch_bounds__(256) void act_back_kernel(ActBackArgs a) {
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-    for (int r0 = row + rows_at; r0 < end; r0 += 16 * U) {
-      float d[U][8], z[U][8];
+    for (int r0 = row + rows_at; r0 < end; r0 += AT * U) {
+      Raw8<T> raw_d[U], raw_z[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int r = r0 + 16 * u, some = r < end ? left : 0;
-        load8<T, VEC>((const T*)a.dy + r * a.dy_stride + col, some, d[u]);
-        if (a.act != GAN_ACT_NONE) load8<T, VEC>((const T*)a.z + r * a.z_stride + col, some, z[u]);
+        const int r = r0 + AT * u, some = r < end ? left : 0;
+        raw_d[u].template load<VEC>((const T*)a.dy + r * a.dy_stride + col, some);
+        if (a.act != GAN_ACT_NONE) raw_z[u].template load<VEC>((const T*)a.z + r * a.z_stride + col, some);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int r = r0 + 16 * u;
-        times_slope<sizeof(T) == 2 ? FULL : EXACT>(a.act, d[u], z[u]);                             // (the bias's gradient is fp32)
+        const int r = r0 + AT * u;
+        float d[8], z[8];
+        raw_d[u].values(d);
+        raw_z[u].values(z);
+        times_slope<sizeof(T) == 2 ? FULL : EXACT>(a.act, d, z);                                   // (the bias's gradient is fp32)
         if (group == a.groups)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[u][i] = 0.f;
-        if (a.dz) store8<T, VEC>((T*)a.dz + r * a.dz_stride + col, r < end ? left : 0, d[u]);
+          for (int i = 0; i < 8; ++i) d[i] = 0.f;
+        if (a.dz) store8<T, VEC, PAST>((T*)a.dz + r * a.dz_stride + col, r < end ? left : 0, d);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += d[u][i];
+        for (int i = 0; i < 8; ++i) sum[i] += d[i];
       }
     }
     if (!a.partial) continue;
@@ -67,16 +72,15 @@ __global__ __launch_bounds__(256) void act_back_kernel(ActBackArgs a) {
     *reinterpret_cast<float4*>(&part[rows_at][lane * 8]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
     *reinterpret_cast<float4*>(&part[rows_at][lane * 8 + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
     __syncthreads();
-    const int c = threadIdx.x;
-    if (c < WIDE && col0 + c < a.cols) {
-      float s[16];
+    for (int c = threadIdx.x; c < WIDE; c += 256) {
+      float s[AT];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) s[k] = part[k][c];
+      for (int k = 0; k < AT; ++k) s[k] = part[k][c];
 #pragma unroll
-      for (int k = 8; k > 0; k /= 2)
+      for (int k = AT / 2; k > 0; k /= 2)
 #pragma unroll
         for (int i = 0; i < k; ++i) s[i] += s[i + k];
-      a.partial[tile * a.cols + col0 + c] = s[0];
+      if (col0 + c < a.cols) a.partial[tile * a.cols + col0 + c] = s[0];
     }
   }
 }
@@ -152,9 +156,11 @@ extern "C" gan_status gan_group_act_backward(int32_t precision, const void* dy, 
     const ActBackArgs a = {dy, z, offs, dz, dbias && groups > 0 ? (float*)work : nullptr, dy_stride, z_stride, dz_stride, groups, (int)rows, cols, act, tall,
                            most_tiles(rows, groups, tall)};
     const dim3 grid((unsigned)std::min(a.tiles * wide_tiles(cols), 1ll << 20));
+    const bool past = rows * cols * e > PAST_CACHES;
 #define GAN_ACT_BACK(T, V) \
-  if (tall == 32) hipLaunchKernelGGL((act_back_kernel<T, V, 2>), grid, dim3(256), 0, st, a); \
-  else hipLaunchKernelGGL((act_back_kernel<T, V, 4>), grid, dim3(256), 0, st, a)
+  if (tall == 32) hipLaunchKernelGGL((act_back_kernel<T, V, false, 2>), grid, dim3(256), 0, st, a); \
+  else if (V && past) hipLaunchKernelGGL((act_back_kernel<T, V, V, 4>), grid, dim3(256), 0, st, a); \
+  else hipLaunchKernelGGL((act_back_kernel<T, V, false, 4>), grid, dim3(256), 0, st, a)
     if (precision == GAN_FP32) { if (vec) { GAN_ACT_BACK(float, true); } else { GAN_ACT_BACK(float, false); } }
     else { if (vec) { GAN_ACT_BACK(bf16_t, true); } else { GAN_ACT_BACK(bf16_t, false); } }
 #undef GAN_ACT_BACK

@@ -219,10 +219,15 @@ __device__ __forceinline__ void load_some(const T* p, int left, float (&v)[N]) {
     }
   }
 }
-template <typename C, int N>
+template <typename C, int N, bool PAST>
 __device__ __forceinline__ void store_some(C* p, int left, const float (&v)[N]) {
-  if constexpr (N == 8) store8<C, false>(p, left, v);
-  else store_four<C>(p, left, v);
+  if constexpr (N == 8) {
+    store8<C, false, PAST>(p, left, v);
+  } else if (PAST && sizeof(C) == 4 && left >= 4) {
+    __builtin_nontemporal_store(Words<4>::T{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, reinterpret_cast<Words<4>::T*>(p));
+  } else {
+    store_four<C>(p, left, v);
+  }
 }
 
 // The biases of columns n .. of an expert (zero for rows of none)
@@ -233,14 +238,14 @@ __device__ __forceinline__ void load_bias(const ActArgs& q, int group, int n, fl
   if (q.bias && group < q.groups) load_some<float, N>(q.bias + (long long)group * q.n + n, q.n - n, b);
 }
 // Outputs n .. of row m from their sums v; b: their biases, add and z: what the row has there of these operands (where it has them).
-template <typename C, int KIND, int N>
+template <typename C, int KIND, bool PAST, int N>
 __device__ __forceinline__ void finish(const ActArgs& q, bool on, int m, int n, float (&v)[N], const float (&b)[N], const float (&add)[N], const float (&z)[N]) {
   constexpr Accuracy A = sizeof(C) == 2 ? NEAR : EXACT;
   const int left = q.n - n;
   if constexpr (KIND == FORWARD) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += b[i];
-    if (q.z_out) store_some<C, N>((C*)q.z_out + m * q.z_stride + n, left, v);
+    if (q.z_out) store_some<C, N, PAST>((C*)q.z_out + m * q.z_stride + n, left, v);
     activate<A>(q.act, v);
     if (q.add && on)
 #pragma unroll
@@ -251,7 +256,7 @@ __device__ __forceinline__ void finish(const ActArgs& q, bool on, int m, int n, 
       for (int i = 0; i < N; ++i) v[i] += add[i];
     if (on) times_slope<A>(q.act, v, z);
   }
-  store_some<C, N>((C*)q.c + m * q.c_stride + n, left, v);
+  store_some<C, N, PAST>((C*)q.c + m * q.c_stride + n, left, v);
 }
 
 // 16 bytes of any alignment as they are, and their values
@@ -272,7 +277,9 @@ __device__ __forceinline__ void values_of(const u32x4& w, float (&v)[N]) {
 }
 
 // store_rows with the epilogue: the sums go through LDS in fp32, sixteen rows at a time, and come back as 16 bytes of outputs a lane.  The other operands of AHEAD sixteens are asked for
-// before they are needed.
+// before they are needed, and results go past the caches, which the weights need: bf16, us on an MI355X, eight experts 4096 -> 4096 over 16384 rows with bias, GELU, residual and stored
+// sums: 539 (through the caches 558; asked for when needed 585), with its reader, a second product, 1021 (1055); a hundred 1024 -> 1024 over 6400: 55 (59) and 114 (127).  Without an epilogue
+// the first takes 468: the bias and GELU's 21 instructions an element are 25 of the rest, the residual and the stored sums 45.
 template <typename C, int KIND, int TM, int TN>
 __device__ __forceinline__ void store_act_rows(const ActArgs& q, const floatx4 (&acc)[TM][TN], int group, unsigned char* lds, int m0, int m_end, int n0, int n_end) {
   constexpr int EACH = 16 / (int)sizeof(C), LANES = TN * 16 / EACH, ROW = TN * 64 + 16, PASSES = 16 * LANES / 64, AHEAD = KIND == FORWARD ? 4 : 2;
@@ -320,7 +327,7 @@ __device__ __forceinline__ void store_act_rows(const ActArgs& q, const floatx4 (
         if (has_add) load_some<C, EACH>((const C*)q.add + m * q.add_stride + n, n_end - n, add);
         if (has_z) load_some<C, EACH>((const C*)q.z_in + m * q.z_stride + n, n_end - n, z);
       }
-      finish<C, KIND>(q, on, m, n, v, b, add, z);
+      finish<C, KIND, true>(q, on, m, n, v, b, add, z);
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -942,7 +949,7 @@ __device__ __forceinline__ void write_four(const Q& q, int group, int m, int n, 
     if (KIND == FORWARD) load_bias(q, group, n, b);
     if (q.add && on) load_some<C, 4>((const C*)q.add + m * q.add_stride + n, q.n - n, add);
     if (KIND != FORWARD && q.act != GAN_ACT_NONE && on) load_some<C, 4>((const C*)q.z_in + m * q.z_stride + n, q.n - n, z);
-    finish<C, KIND>(q, on, m, n, f, b, add, z);
+    finish<C, KIND, false>(q, on, m, n, f, b, add, z);
   } else {
     store_four<C>((C*)q.c + (long long)m * q.c_stride + n, q.n - n, v);
   }

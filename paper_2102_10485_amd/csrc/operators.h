@@ -10,6 +10,7 @@ gan_status operator_fail(gan_status s, const char* why);          // records the
 void operator_launches();                                         // before a launch: what an earlier HIP call of the caller's left behind is not its failure
 gan_status operator_launched();                                   // GAN_OK, or GAN_E_HIP with the runtime's text
 
+constexpr long long PAST_CACHES = 64 << 20;                      // bytes of a result that its reader would not find in the caches
 constexpr long long MOST_ROWS = 1 << 30;
 constexpr int MOST_COLS = 1 << 28;
 gan_status check_sizes(int32_t precision, long long rows, int cols);
@@ -62,6 +63,55 @@ __device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
     }
   }
 }
+
+// Eight neighbours as they lie in memory, to be had in flight in few registers: read as load8 does, values later.
+template <typename T>
+struct Raw8 {
+  unsigned w[2 * sizeof(T)];
+  template <bool VEC>
+  __device__ __forceinline__ void load(const T* p, int left) {
+    typedef typename Words<VEC ? 16 : sizeof(T)>::T words;
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) w[i] = 0;
+    if (VEC ? left > 0 : left >= 8) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const words v = reinterpret_cast<const words*>(p)[i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
+      }
+    } else if (!VEC) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) w[i] = i < left ? __float_as_uint(p[i]) : 0u;
+        else w[i / 2] |= (i < left ? (unsigned)p[i].v : 0u) << 16 * (i % 2);
+      }
+    }
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      v[i] = sizeof(T) == 4 ? __uint_as_float(w[i % (2 * sizeof(T))]) : __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+  template <bool VEC, bool PAST = false>
+  __device__ __forceinline__ void store(T* p, int left) const {
+    typedef typename Words<VEC ? 16 : sizeof(T)>::T words;
+    if (VEC ? left > 0 : left >= 8) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const words v = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+        if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<words*>(p) + i);
+        else reinterpret_cast<words*>(p)[i] = v;
+      }
+    } else if (!VEC) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) { if (i < left) p[i] = __uint_as_float(w[i]); }
+        else { if (i < left) p[i].v = (unsigned short)(w[i / 2] >> 16 * (i % 2)); }
+      }
+    }
+  }
+};
 
 // PAST: past the caches
 template <typename T, int ALIGN, bool PAST>

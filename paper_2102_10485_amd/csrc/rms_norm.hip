@@ -39,10 +39,9 @@ struct NormArgs {
   float eps;
 };
 
-// Results of more bytes than this go past the caches, which would not hold them all for their reader (bf16 with the sum, us through the caches and past them:
+// Results of more bytes than PAST_CACHES go past the caches, which would not hold them all for their reader (bf16 with the sum, us through the caches and past them:
 // 16384 x 4096 94.6, 76.2, into 8 bits 86.7, 70.3; 65536 x 512 48.5, 39.5; 12000 x 2048 37.5, 34.3; a norm and two products of four experts on 16384 x 4096
 // 950, 942; the gradient of 40000 x 1024 58.7, 50.5, of 16384 x 4096 98, 96).  Smaller ones stay for it (norm and products of eight experts of 128 rows of 1024: 34.4, past the caches 36.9).
-constexpr long long PAST_CACHES = 64 << 20;
 
 template <typename T, bool VEC>
 __device__ __forceinline__ void add_rounded(float (&v)[E], const T* residual, int left) {
