@@ -1195,8 +1195,11 @@ gan_status launch_large(const Q& q, hipStream_t st) {
   const bool big = KIND == WGRAD ? q.parts * wgrad_tiles(q.groups, q.m, q.n, 256) >= 256 : tiles(q, 256, 256) >= 256 && q.rows / most_groups(q) > 32;
   if constexpr (F != ANY)
     if (big) return launch_tiles<F, KIND, 256, 256, 2, 4, 1, C>(q, st);
+  // (8 bits with an epilogue, whose steps wait for the conversion: up to 576 tiles.  us without, with: eight experts of 32 rows, 4096 -> 4096 (320 tiles) 50, 40; of 64 (384) 60, 48; 16 of
+  // 25, 2048 -> 2048 (304) 25.6, 22; a hundred of 16, 1024 -> 1024 (896) 40, 55.  In bf16 the first is 62, 68.  Products without an epilogue keep the order of their sums.)
+  constexpr int SPLIT_MOST = F == EIGHT_BITS && std::is_same_v<Q, ActArgs> ? 576 : 288;
   if constexpr (KIND != WGRAD)
-    if (tiles(q, 128, 128) <= 288 && q.k >= 512) return launch_tiles<F, KIND, 128, 128, 2, 2, 2, C>(q, st);
+    if (tiles(q, 128, 128) <= SPLIT_MOST && q.k >= 512) return launch_tiles<F, KIND, 128, 128, 2, 2, 2, C>(q, st);
   return launch_tiles<F, KIND, 128, 128, 2, 2, 1, C>(q, st);
 }
 

@@ -25,8 +25,7 @@ struct RouteArgs {
   float* weight;
   int* counts;                                                    // the results, or NULL (then mean and balance are too)
   float *mean, *balance;
-  int* ticket;                                                    // what several blocks leave: see Work
-  float* sums;
+  float* sums;                                                    // what several blocks leave
   int* parts;
   long long stride, rows;
   int experts, k, normalize;
@@ -76,21 +75,28 @@ __device__ __forceinline__ float value_of(unsigned key) {
   return __uint_as_float(sizeof(T) == 4 ? u : u & 0xffff0000u);
 }
 
-// A row's logits (-infinity behind its end) and keys.
+// A row's logits as they lie in memory, which are asked for while the row before is worked on; then as numbers (-infinity behind the row's end) and keys.
 template <typename T, int L, int C>
-__device__ __forceinline__ void load_row(const T* row, int experts, float (&v)[C], unsigned (&key)[C]) {
+struct Row {
+  Raw8<T> raw[C / 8];
+  __device__ __forceinline__ void load(const T* row, int experts) {
 #pragma unroll
-  for (int j = 0; j < C / 8; ++j) {
-    const int e = expert_of<L>(j * 8), left = experts - e;
-    float w[8];
-    load8<T, false>(row + e, left, w);
+    for (int j = 0; j < C / 8; ++j) raw[j].template load<false>(row + expert_of<L>(j * 8), experts - expert_of<L>(j * 8));
+  }
+  __device__ __forceinline__ void values(int experts, float (&v)[C], unsigned (&key)[C]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[j * 8 + i] = i < left ? w[i] : -INFINITY;
-      key[j * 8 + i] = key_of<T>(v[j * 8 + i], e + i);
+    for (int j = 0; j < C / 8; ++j) {
+      const int e = expert_of<L>(j * 8), left = experts - e;
+      float w[8];
+      raw[j].values(w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[j * 8 + i] = i < left ? w[i] : -INFINITY;
+        key[j * 8 + i] = key_of<T>(v[j * 8 + i], e + i);
+      }
     }
   }
-}
+};
 template <int C>
 __device__ __forceinline__ unsigned most(const unsigned (&key)[C]) {
   unsigned m = 0;
@@ -140,12 +146,6 @@ __device__ __forceinline__ unsigned next_choice(unsigned (&key)[C], unsigned las
 
 constexpr int SUM_EXPERTS = 8;                                    // of a block of route_sum_kernel
 
-// The workspace of several blocks: a ticket for those of route_sum_kernel, their shares of the loss, and every block's sums and counts.
-struct Work {
-  static constexpr long long LOSS = 16, SUMS = LOSS + MOST_EXPERTS / SUM_EXPERTS * 16;
-  static long long bytes(int blocks, int experts) { return SUMS + (long long)blocks * (2 * experts + 1) * 4; }
-};
-
 template <typename T, int L, int C, bool STATS>
 __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
   constexpr int R = 256 / L;                                      // rows of a block at a time
@@ -162,12 +162,16 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
     __syncthreads();
   }
   const int at = threadIdx.x / L, lane = threadIdx.x % L;
+  Row<T, L, C> next;
+  const auto ask = [&](long long row) { next.load((const T*)a.logits + (row < a.rows ? row : 0) * a.stride, row < a.rows ? a.experts : 0); };
+  ask((long long)blockIdx.x * R + at);
   for (long long first = (long long)blockIdx.x * R; first < a.rows; first += (long long)gridDim.x * R) {
     const long long row = first + at;
     const bool in = row < a.rows;
     float v[C];
     unsigned key[C];
-    load_row<T, L, C>((const T*)a.logits + (in ? row : 0) * a.stride, in ? a.experts : 0, v, key);
+    next.values(in ? a.experts : 0, v, key);
+    ask(row + (long long)gridDim.x * R);
     const unsigned best = most_of<L>(most(key));
     const float top = value_of<T>(best), inv = 1.f / powers<L>(v, top);
     if constexpr (STATS) {
@@ -236,7 +240,6 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
       __syncthreads();
     }
     if (gridDim.x > 1) {
-      if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
       for (int e = threadIdx.x; e < a.experts; e += 256) a.sums[(long long)blockIdx.x * a.experts + e] = wide[e];
       for (int e = threadIdx.x; e <= a.experts; e += 256) a.parts[(long long)blockIdx.x * (a.experts + 1) + e] = hist[e];
       return;
@@ -272,8 +275,8 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
   }
 }
 
-// Counts, means and the balance loss from the blocks' sums: a block for eight experts (128 threads each, a load of up to 1024 blocks' sums at a time), whose shares of the loss the last
-// block to come adds up in order.  (65536 rows, 256 experts: NEW us; blocks of 32 experts 16.2.)
+// Counts and means from the blocks' sums: a block for eight experts (128 threads each, a load of up to 1024 blocks' sums at a time), which leaves their shares of the balance loss.
+// (65536 rows, 256 experts: NEWSUM us; blocks of 32 experts 16.2, with the loss added up by the last block to come, whose order of memory costs a write-back of the caches, 12.4.)
 __global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, double* loss, int blocks) {
   __shared__ int n[16][SUM_EXPERTS], rows[16];
   __shared__ double d[16][SUM_EXPERTS];
@@ -323,15 +326,18 @@ __global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, double* lo
   }
   if (threadIdx.x > 0) return;
   if (blockIdx.x == 0) a.counts[a.experts] = counted;
-  __hip_atomic_store(&loss[2 * blockIdx.x], share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __hip_atomic_store(&loss[2 * blockIdx.x + 1], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  if (__hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) != (int)gridDim.x - 1 || !a.balance) return;
-  share = all = 0;
-  for (int b = 0; b < (int)gridDim.x; ++b) {
-    share += __hip_atomic_load(&loss[2 * b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    all += __hip_atomic_load(&loss[2 * b + 1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  loss[2 * blockIdx.x] = share;
+  loss[2 * blockIdx.x + 1] = all;
+}
+__global__ __launch_bounds__(64) void route_balance_kernel(const double* loss, int blocks, int experts, float* balance) {
+  double share = 0, all = 0;
+  for (int b = threadIdx.x; b < blocks; b += 64) share += loss[2 * b], all += loss[2 * b + 1];
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) {
+    share += __shfl_xor(share, x);
+    all += __shfl_xor(all, x);
   }
-  *a.balance = (float)(all > 0 ? share * a.experts / all : 0);
+  if (threadIdx.x == 0) *balance = (float)(all > 0 ? share * experts / all : 0);
 }
 
 // without rows
@@ -356,14 +362,16 @@ struct RouteBackArgs {
 };
 
 // dl_e = p_e (share_e - D) + extra_e, share_e = c counts_e.  extra is zero but for the choices, which are a lane's each: p_e g_e (then their sum is in D), or that of the softmax over
-// the choices, w_e (g_e - sum_j w_j g_j) with w_e = p_e / the choices' p.  They reach the lanes that hold their logits through a row of LDS.
+// the choices, w_e (g_e - sum_j w_j g_j) with w_e = p_e / the choices' p.  The choices' p come from the lanes that hold their logits through a row of LDS, and extra goes back through another
+// (with compares of every logit with every choice instead: NEWBACK us became 97 for 65536 rows, 256 experts, 8 choices; with the choices' logits read again from memory 29).
 template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
   constexpr int R = 256 / L, EACH = L < MOST_CHOICES ? MOST_CHOICES / L : 1;      // choices of a lane
-  __shared__ __align__(16) float rows_extra[R][L * C];
+  constexpr bool P_ROWS = R * L * C * 4 <= 32768;                 // (the p of longer rows' choices are formed again)
+  __shared__ __align__(16) float rows_extra[R][L * C], rows_p[P_ROWS ? R : 1][P_ROWS ? L * C : 1];
   __shared__ int part[4];
   const int at = threadIdx.x / L, lane = threadIdx.x % L;
-  float* extra = rows_extra[at];
+  float *extra = rows_extra[at], *ps = rows_p[P_ROWS ? at : 0];
 #pragma unroll
   for (int c = 0; c < C; ++c) extra[expert_of<L>(c)] = 0.f;
   float share[C];
@@ -386,24 +394,39 @@ __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
     }
   }
   __syncthreads();
-  for (long long first = (long long)blockIdx.x * R; first < a.rows; first += (long long)gridDim.x * R) {
-    const long long row = first + at;
+  const auto settle = [] {                                        // (what lanes of a wave wrote to LDS is there for the others)
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  Row<T, L, C> next;
+  int next_id[EACH];
+  float next_g[EACH];
+  const auto ask = [&](long long row) {
     const bool in = row < a.rows;
-    const T* logits = (const T*)a.logits + (in ? row : 0) * a.stride;
-    int id[EACH];
-    float g[EACH], l[EACH];
+    next.load((const T*)a.logits + (in ? row : 0) * a.stride, in ? a.experts : 0);
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const int j = lane + i * L;
       const bool is = a.dweight && in && j < a.k;
-      id[i] = is ? a.expert[row * a.k + j] : -1;
-      g[i] = is ? a.dweight[row * a.k + j] : 0.f;
-      if ((unsigned)id[i] >= (unsigned)a.experts) id[i] = -1;
-      l[i] = id[i] >= 0 ? to_float(logits[id[i]]) : 0.f;
+      next_id[i] = is ? a.expert[row * a.k + j] : -1;
+      next_g[i] = is ? a.dweight[row * a.k + j] : 0.f;
     }
-    float v[C];
+  };
+  ask((long long)blockIdx.x * R + at);
+  for (long long first = (long long)blockIdx.x * R; first < a.rows; first += (long long)gridDim.x * R) {
+    const long long row = first + at;
+    const bool in = row < a.rows;
+    int id[EACH];
+    float g[EACH], l[EACH], v[C];
     unsigned key[C];
-    load_row<T, L, C>(logits, in ? a.experts : 0, v, key);
+    next.values(in ? a.experts : 0, v, key);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      id[i] = (unsigned)next_id[i] < (unsigned)a.experts ? next_id[i] : -1;
+      g[i] = next_g[i];
+    }
+    ask(row + (long long)gridDim.x * R);
     const float top = value_of<T>(most_of<L>(most(key))), inv = 1.f / powers<L>(v, top);
     float mean = 0.f, of_chosen = 0.f, of_weights = 0.f;
 #pragma unroll
@@ -411,9 +434,19 @@ __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
       v[c] = key[c] ? v[c] * inv : 0.f;
       mean += v[c] * share[c];
     }
+    if constexpr (P_ROWS) {
+#pragma unroll
+      for (int c = 0; c < C; c += 4) *reinterpret_cast<float4*>(ps + expert_of<L>(c)) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+      settle();
+    }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      l[i] = id[i] >= 0 && l[i] > -INFINITY ? __builtin_amdgcn_exp2f((l[i] - top) * LOG2E) * inv : 0.f;      // its p
+      if constexpr (P_ROWS) {
+        l[i] = id[i] >= 0 ? ps[id[i]] : 0.f;
+      } else {
+        const float logit = id[i] >= 0 ? to_float(((const T*)a.logits)[row * a.stride + id[i]]) : 0.f;
+        l[i] = id[i] >= 0 && logit > -INFINITY ? __builtin_amdgcn_exp2f((logit - top) * LOG2E) * inv : 0.f;
+      }
       of_chosen += l[i];
       of_weights += id[i] >= 0 ? l[i] * g[i] : 0.f;
     }
@@ -430,9 +463,7 @@ __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
       for (int i = 0; i < EACH; ++i)
         if (id[i] >= 0) extra[id[i]] = l[i] * g[i];
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    settle();
 #pragma unroll
     for (int j = 0; j < C / 8; ++j) {
       const int e = expert_of<L>(j * 8);
@@ -446,9 +477,7 @@ __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
       }
       store8<T, false>((T*)a.dlogits + (in ? row : 0) * a.dstride + e, in ? a.experts - e : 0, d);
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    settle();
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
       if (id[i] >= 0) extra[id[i]] = 0.f;
@@ -471,6 +500,7 @@ long long tiles_of(long long rows, int experts) {
   const int r = 256 / (experts <= 8 ? 1 : experts <= 32 ? 4 : experts <= 512 ? 16 : 64);
   return (rows + r - 1) / r;
 }
+constexpr int LOSS_BYTES = MOST_EXPERTS / SUM_EXPERTS * 16;
 // Blocks that leave sums of their rows behind.
 int stat_blocks(long long rows, int experts) { return (int)std::min(tiles_of(rows, experts), 1024ll); }
 
@@ -491,7 +521,7 @@ using namespace gan;
 extern "C" int64_t gan_route_bytes(int64_t rows, int32_t experts) {
   if (rows < 1 || experts < 1 || rows > MOST_ROWS || experts > MOST_EXPERTS) return 0;
   const int blocks = stat_blocks(rows, experts);
-  return blocks > 1 ? Work::bytes(blocks, experts) : 0;
+  return blocks > 1 ? LOSS_BYTES + (int64_t)blocks * (2 * experts + 1) * 4 : 0;
 }
 
 extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t logits_stride, int64_t rows, int32_t experts, int32_t k, int32_t normalize, int32_t* expert,
@@ -509,9 +539,8 @@ extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t l
     return operator_launched();
   }
   const int blocks = stat_blocks(rows, experts);
-  uint8_t* const w = (uint8_t*)work;
-  float* const sums = (float*)(w + Work::SUMS);
-  const RouteArgs a = {logits, expert, weight, counts, mean, balance, (int*)w, sums, (int*)(sums + (long long)blocks * experts), logits_stride, rows, experts, k, normalize};
+  float* const sums = (float*)((uint8_t*)work + LOSS_BYTES);
+  const RouteArgs a = {logits, expert, weight, counts, mean, balance, sums, (int*)(sums + (long long)blocks * experts), logits_stride, rows, experts, k, normalize};
   with_lanes(experts, [&](auto l, auto c) {
     constexpr int L = decltype(l)::value, C = decltype(c)::value;
     const unsigned lds = ((L < MOST_CHOICES ? 2 * (256 / L) * k : 0) + (counts ? 2 * experts + 1 : 0)) * 4;
@@ -524,8 +553,11 @@ extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t l
     if (precision == GAN_FP32) go(float());
     else go(bf16_t());
   });
-  if (counts && blocks > 1)
-    hipLaunchKernelGGL(route_sum_kernel, dim3((experts + SUM_EXPERTS - 1) / SUM_EXPERTS), dim3(1024), 0, st, a, (double*)(w + Work::LOSS), blocks);
+  if (counts && blocks > 1) {
+    const int sum_blocks = (experts + SUM_EXPERTS - 1) / SUM_EXPERTS;
+    hipLaunchKernelGGL(route_sum_kernel, dim3(sum_blocks), dim3(1024), 0, st, a, (double*)work, blocks);
+    if (balance) hipLaunchKernelGGL(route_balance_kernel, dim3(1), dim3(64), 0, st, (const double*)work, sum_blocks, experts, balance);
+  }
   return operator_launched();
 }
 
