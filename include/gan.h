@@ -396,7 +396,7 @@ gan_status gan_group_act_backward(int32_t precision, const void* dy, int64_t dy_
                                   int64_t rows, int32_t cols, void* dz, int64_t dz_stride, float* dbias, void* work, int64_t work_bytes, void* hip_stream);
 
 /* Rows that choose their experts.  logits [rows][experts] in the storage type.  An expert whose logit is -infinity or NaN is not there for the row; p are the probabilities of
-   those that are, exp(l - max) / sum of the same (all NaN in a row with a NaN or +infinity).  expert int32 [rows][k]: the k largest, the largest first, the lowest
+   those that are, exp(l - max) / sum of the same (all NaN in a row with a NaN or +infinity, and the means and the balance with them).  expert int32 [rows][k]: the k largest, the largest first, the lowest
    index among equals (-0 and 0 are), -1 where fewer are there; weight fp32 [rows][k] (or NULL): their p, normalize = 1: divided by the sum over the row's choices; 0 behind them.
    counts int32 [experts + 1] (or NULL; then mean and balance are NULL too): how many rows chose each expert, and how many rows have an expert at all; mean fp32 [experts] (or NULL): the
    mean of p over these rows (0 without any); balance fp32 [1] (or NULL): experts * sum over e of counts[e] / sum(counts) * mean[e], 1 where all experts get the same.
