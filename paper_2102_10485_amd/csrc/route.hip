@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
 }
 
 // Counts and means from the blocks' sums: a block for eight experts (128 threads each, a load of up to 1024 blocks' sums at a time), which leaves their shares of the balance loss.
-// (65536 rows, 256 experts: NEWSUM us; blocks of 32 experts 16.2, with the loss added up by the last block to come, whose order of memory costs a write-back of the caches, 12.4.)
+// (65536 rows, 256 experts: 7.2 us; blocks of 32 experts 16.2, with the loss added up by the last block to come, whose order of memory costs a write-back of the caches, 12.4.)
 __global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, double* loss, int blocks) {
   __shared__ int n[16][SUM_EXPERTS], rows[16];
   __shared__ double d[16][SUM_EXPERTS];
@@ -361,7 +361,7 @@ struct RouteBackArgs {
 
 // dl_e = p_e (share_e - D) + extra_e, share_e = c counts_e.  extra is zero but for the choices, which are a lane's each: p_e g_e (then their sum is in D), or that of the softmax over
 // the choices, w_e (g_e - sum_j w_j g_j) with w_e = p_e / the choices' p.  The choices' p come from the lanes that hold their logits through a row of LDS, and extra goes back through another
-// (with compares of every logit with every choice instead: NEWBACK us became 97 for 65536 rows, 256 experts, 8 choices; with the choices' logits read again from memory 29).
+// (65536 rows, 256 experts, 8 choices in bf16: 27 us; with compares of every logit with every choice 97, with the choices' logits read again from memory 29).
 template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
   constexpr int R = 256 / L, EACH = L < MOST_CHOICES ? MOST_CHOICES / L : 1;      // choices of a lane
