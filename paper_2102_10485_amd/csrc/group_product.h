@@ -237,15 +237,15 @@ __device__ __forceinline__ void load_bias(const ActArgs& q, int group, int n, fl
   for (int i = 0; i < N; ++i) b[i] = 0.f;
   if (q.bias && group < q.groups) load_some<float, N>(q.bias + (long long)group * q.n + n, q.n - n, b);
 }
-// Outputs n .. of row m from their sums v; b: their biases, add and z: what the row has there of these operands (where it has them).
-template <typename C, int KIND, bool PAST, int N>
-__device__ __forceinline__ void finish(const ActArgs& q, bool on, int m, int n, float (&v)[N], const float (&b)[N], const float (&add)[N], const float (&z)[N]) {
+// Outputs from their sums v; b: their biases, if the sums are without (not BIASED); add and z: what the row has there of these operands (where it has them).  sums: called with z before the activation.
+template <typename C, int KIND, bool BIASED, int N, typename F>
+__device__ __forceinline__ void finish(const ActArgs& q, bool on, float (&v)[N], const float (&b)[N], const float (&add)[N], const float (&z)[N], F&& sums) {
   constexpr Accuracy A = sizeof(C) == 2 ? NEAR : EXACT;
-  const int left = q.n - n;
   if constexpr (KIND == FORWARD) {
+    if constexpr (!BIASED)
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += b[i];
-    if (q.z_out) store_some<C, N, PAST>((C*)q.z_out + m * q.z_stride + n, left, v);
+      for (int i = 0; i < N; ++i) v[i] += b[i];
+    if (q.z_out) sums();
     activate<A>(q.act, v);
     if (q.add && on)
 #pragma unroll
@@ -256,7 +256,6 @@ __device__ __forceinline__ void finish(const ActArgs& q, bool on, int m, int n, 
       for (int i = 0; i < N; ++i) v[i] += add[i];
     if (on) times_slope<A>(q.act, v, z);
   }
-  store_some<C, N, PAST>((C*)q.c + m * q.c_stride + n, left, v);
 }
 
 // 16 bytes of any alignment as they are, and their values
@@ -278,40 +277,44 @@ __device__ __forceinline__ void values_of(const u32x4& w, float (&v)[N]) {
 
 // store_rows with the epilogue: the sums go through LDS in fp32, sixteen rows at a time, and come back as 16 bytes of outputs a lane.  The other operands of AHEAD sixteens are asked for
 // before they are needed, and results go past the caches, which the weights need: bf16, us on an MI355X, eight experts 4096 -> 4096 over 16384 rows with bias, GELU, residual and stored
-// sums: 539 (through the caches 558; asked for when needed 585), with its reader, a second product, 1021 (1055); a hundred 1024 -> 1024 over 6400: 55 (59) and 114 (127).  Without an epilogue
-// the first takes 468: the bias and GELU's 21 instructions an element are 25 of the rest, the residual and the stored sums 45.
-template <typename C, int KIND, int TM, int TN>
-__device__ __forceinline__ void store_act_rows(const ActArgs& q, const floatx4 (&acc)[TM][TN], int group, unsigned char* lds, int m0, int m_end, int n0, int n_end) {
-  constexpr int EACH = 16 / (int)sizeof(C), LANES = TN * 16 / EACH, ROW = TN * 64 + 16, PASSES = 16 * LANES / 64, AHEAD = KIND == FORWARD ? 4 : 2;
+// sums: 539 (through the caches 558; asked for when needed 585), with its reader, a second product, 1021 (1055); a hundred 1024 -> 1024 over 6400: 55 (59) and 114 (127).
+// Bound by the vector instructions between the matrix ones of two tiles (GELU has 21): addresses move on by additions, and a tile that lies wholly inside has no checks (INNER).
+template <bool INNER, bool BIASED, typename C, int KIND, int TM, int TN>
+__device__ __forceinline__ void store_act_tile(const ActArgs& q, const floatx4 (&acc)[TM][TN], int group, unsigned char* lds, int m0, int m_end, int n0, int n_end) {
+  constexpr int EACH = 16 / (int)sizeof(C), LANES = TN * 16 / EACH, ROW = TN * 64 + 16, PASSES = 16 * LANES / 64, APART = 64 / LANES, AHEAD = KIND == FORWARD ? 4 : 2;
   static_assert(64 % LANES == 0, "whole rows");
-  const int l = threadIdx.x & 63, n = n0 + l % LANES * EACH;
-  const bool on = group < q.groups, whole = n + EACH <= n_end, has_add = q.add && on, has_z = KIND != FORWARD && q.act != GAN_ACT_NONE && on;
+  const int l = threadIdx.x & 63, n = n0 + l % LANES * EACH, m_first = m0 + l / LANES;
+  const bool on = group < q.groups, whole = INNER || n + EACH <= n_end, has_add = q.add && on, has_z = KIND != FORWARD && q.act != GAN_ACT_NONE && on;
   float b[EACH];
 #pragma unroll
   for (int i = 0; i < EACH; ++i) b[i] = 0.f;
-  if (KIND == FORWARD && n < n_end) load_bias(q, group, n, b);
+  if (KIND == FORWARD && !BIASED && n < n_end) load_bias(q, group, n, b);
+  const C *next_add = (const C*)q.add + m_first * q.add_stride + n, *next_z = (const C*)q.z_in + m_first * q.z_stride + n;
+  C *to = (C*)q.c + m_first * q.c_stride + n, *z_to = (C*)q.z_out + m_first * q.z_stride + n;
+  const long long add_step = APART * q.add_stride, z_step = APART * q.z_stride, c_step = APART * q.c_stride;
   u32x4 raw_add[TM][PASSES], raw_z[TM][PASSES];
   const auto ask = [&](int i) {
-    if (m0 + i * 16 >= m_end || !whole) return;
 #pragma unroll
     for (int k = 0; k < PASSES; ++k) {
-      const int m = min(m0 + i * 16 + k * (64 / LANES) + l / LANES, m_end - 1);
-      if (has_add) raw_add[i][k] = load_raw((const C*)q.add + m * q.add_stride + n);
-      if (has_z) raw_z[i][k] = load_raw((const C*)q.z_in + m * q.z_stride + n);
+      const bool in = INNER || (m_first + i * 16 + k * APART < m_end && whole);
+      if (has_add && in) raw_add[i][k] = load_raw(next_add);
+      if (has_z && in) raw_z[i][k] = load_raw(next_z);
+      next_add += add_step;
+      next_z += z_step;
     }
   };
 #pragma unroll
   for (int i = 0; i < TM && i < AHEAD; ++i) ask(i);
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    if (m0 + i * 16 >= m_end) break;
+    if (!INNER && m0 + i * 16 >= m_end) break;
 #pragma unroll
     for (int j = 0; j < TN; ++j) *reinterpret_cast<floatx4*>(lds + (l & 15) * ROW + (j * 16 + (l >> 4) * 4) * 4) = acc[i][j];
     if (i + AHEAD < TM) ask(i + AHEAD);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int k = 0; k < PASSES; ++k) {
-      const int r = k * (64 / LANES) + l / LANES, m = m0 + i * 16 + r;
+      const int r = k * APART + l / LANES, m = m0 + i * 16 + r;
       float v[EACH], add[EACH], z[EACH];
 #pragma unroll
       for (int c = 0; c < EACH; c += 4) {
@@ -319,18 +322,28 @@ __device__ __forceinline__ void store_act_rows(const ActArgs& q, const floatx4 (
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[c + e] = f[e];
       }
-      if (m >= m_end || n >= n_end) continue;
-      if (whole) {
-        values_of<C>(raw_add[i][k], add);
-        values_of<C>(raw_z[i][k], z);
-      } else {
-        if (has_add) load_some<C, EACH>((const C*)q.add + m * q.add_stride + n, n_end - n, add);
-        if (has_z) load_some<C, EACH>((const C*)q.z_in + m * q.z_stride + n, n_end - n, z);
+      if (INNER || (m < m_end && n < n_end)) {
+        const int left = whole ? EACH : n_end - n;
+        if (whole) {
+          values_of<C>(raw_add[i][k], add);
+          values_of<C>(raw_z[i][k], z);
+        } else {
+          if (has_add) load_some<C, EACH>((const C*)q.add + m * q.add_stride + n, left, add);
+          if (has_z) load_some<C, EACH>((const C*)q.z_in + m * q.z_stride + n, left, z);
+        }
+        finish<C, KIND, BIASED>(q, on, v, b, add, z, [&] { store_some<C, EACH, true>(z_to, left, v); });
+        store_some<C, EACH, true>(to, left, v);
       }
-      finish<C, KIND, true>(q, on, m, n, v, b, add, z);
+      to += c_step;
+      z_to += z_step;
     }
     __builtin_amdgcn_wave_barrier();
   }
+}
+template <bool BIASED, typename C, int KIND, int TM, int TN>
+__device__ __forceinline__ void store_act_rows(const ActArgs& q, const floatx4 (&acc)[TM][TN], int group, unsigned char* lds, int m0, int m_end, int n0, int n_end) {
+  if (m0 + TM * 16 <= m_end && n0 + TN * 16 <= n_end) store_act_tile<true, BIASED, C, KIND>(q, acc, group, lds, m0, m_end, n0, n_end);
+  else store_act_tile<false, BIASED, C, KIND>(q, acc, group, lds, m0, m_end, n0, n_end);
 }
 
 template <int KIND, int RT, typename Q>
@@ -451,7 +464,7 @@ __global__ __launch_bounds__(256, RT == 128 ? 2 : 4) void linear_fp32_kernel(Q q
   }
   __syncthreads();
   unsigned char* mine = lds + wave * 16 * (TW * 64 + 16);
-  if constexpr (std::is_same_v<Q, ActArgs>) store_act_rows<float, KIND>(q, acc, group, mine, m0 + wm, m_end, n0 + wn, q.n);
+  if constexpr (std::is_same_v<Q, ActArgs>) store_act_rows<false, float, KIND>(q, acc, group, mine, m0 + wm, m_end, n0 + wn, q.n);
   else store_rows<float, KIND == WGRAD, TW, TW>(acc, c, q.c_stride, mine, m0 + wm, m_end, n0 + wn, q.n);
 }
 
@@ -697,9 +710,17 @@ __device__ __forceinline__ void tile_product(const Q& q, unsigned char* lds, int
 
   floatx4 acc[TM][TN];
 #pragma unroll
-  for (int i = 0; i < TM; ++i)
+  for (int j = 0; j < TN; ++j) {
+    floatx4 start = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (KIND == FORWARD && std::is_same_v<Q, ActArgs>) {                                   // (the sums begin with the biases)
+      const int n = n0 + wn + j * 16 + ((threadIdx.x & 63) >> 4) * 4;
+      float b[4] = {};
+      if (n < q.n && (SPLIT == 1 || set == 0)) load_bias(q, group, n, b);
+      start = floatx4{b[0], b[1], b[2], b[3]};
+    }
 #pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < TM; ++i) acc[i][j] = start;
+  }
 
   if (steps > 0) {
     const int expert = KIND == WGRAD ? 0 : group;
@@ -785,7 +806,7 @@ __device__ __forceinline__ void tile_product(const Q& q, unsigned char* lds, int
   }
   if constexpr (std::is_same_v<Q, ActArgs>) {
     static_assert(NW * 16 * (TN * 64 + 16) <= S * STAGE, "the outputs' LDS");
-    store_act_rows<C, KIND>(q, acc, group, lds + wave * 16 * (TN * 64 + 16), m0 + wm, m_end, n0 + wn, q.n);
+    store_act_rows<true, C, KIND>(q, acc, group, lds + wave * 16 * (TN * 64 + 16), m0 + wm, m_end, n0 + wn, q.n);
   } else {
     C* c = (C*)q.c + (KIND == WGRAD ? part * q.part + (long long)group * q.c_group : 0);
     static_assert(NW * 16 * (TN * 16 * (int)sizeof(C) + 16) <= S * STAGE, "the outputs' LDS");
@@ -949,7 +970,8 @@ __device__ __forceinline__ void write_four(const Q& q, int group, int m, int n, 
     if (KIND == FORWARD) load_bias(q, group, n, b);
     if (q.add && on) load_some<C, 4>((const C*)q.add + m * q.add_stride + n, q.n - n, add);
     if (KIND != FORWARD && q.act != GAN_ACT_NONE && on) load_some<C, 4>((const C*)q.z_in + m * q.z_stride + n, q.n - n, z);
-    finish<C, KIND, false>(q, on, m, n, f, b, add, z);
+    finish<C, KIND, false>(q, on, f, b, add, z, [&] { store_some<C, 4, false>((C*)q.z_out + m * q.z_stride + n, q.n - n, f); });
+    store_some<C, 4, false>((C*)q.c + m * q.c_stride + n, q.n - n, f);
   } else {
     store_four<C>((C*)q.c + (long long)m * q.c_stride + n, q.n - n, v);
   }
