@@ -183,31 +183,36 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
         if (lane == 0) atomicAdd(&hist[a.experts], 1);
       }
     }
-    float of_all = 0.f, my_p = 0.f;
+    // (where a row has as many lanes as it may have choices, lane j has the j-th: its key and expert)
+    float of_all = 0.f;
     int my_id = -1;
-    unsigned m = best;
+    unsigned m = best, my_key = 0;
     for (int j = 0; j < a.k; ++j) {
       int id = -1;
       if (m >= THERE) {                                           // (behind the last expert that is there all are none)
         if (j == 0 && sizeof(T) == 2) id = (int)(0xffffu - (m & 0xffffu));
         else m = next_choice<T, L, C>(key, m, id);
       }
-      const float p = m >= THERE ? __builtin_amdgcn_exp2f((value_of<T>(m) - top) * LOG2E) * inv : 0.f;
-      of_all += p;
       if constexpr (L >= MOST_CHOICES) {
         my_id = lane == j ? id : my_id;
-        my_p = lane == j ? p : my_p;
-      } else if (lane == 0) {
-        ids[at * a.k + j] = id;
-        weights[at * a.k + j] = p;
-        if (STATS && id >= 0) atomicAdd(&hist[id], 1);
+        my_key = lane == j ? m : my_key;
+      } else {
+        const float p = m >= THERE ? __builtin_amdgcn_exp2f((value_of<T>(m) - top) * LOG2E) * inv : 0.f;
+        of_all += p;
+        if (lane == 0) {
+          ids[at * a.k + j] = id;
+          weights[at * a.k + j] = p;
+          if (STATS && id >= 0) atomicAdd(&hist[id], 1);
+        }
       }
     }
     if constexpr (L >= MOST_CHOICES) {
+      const float p = my_id >= 0 ? __builtin_amdgcn_exp2f((value_of<T>(my_key) - top) * LOG2E) * inv : 0.f;
+      if (a.normalize) of_all = sum_of<L>(p);
       if (in && lane < a.k) {
         if (STATS && my_id >= 0) atomicAdd(&hist[my_id], 1);
         a.expert[row * a.k + lane] = my_id;
-        if (a.weight) a.weight[row * a.k + lane] = a.normalize && my_id >= 0 ? my_p / of_all : my_p;
+        if (a.weight) a.weight[row * a.k + lane] = a.normalize && my_id >= 0 ? p / of_all : p;
       }
     } else {
       if (a.normalize && lane == 0 && best >= THERE)
