@@ -194,3 +194,23 @@ def test_no_rows():
     B.combine_rows(B.BF16, 0, 64, 0, 0, offs.data_ptr(), 3, 2, 0, 64, 0, 64, 0, 64)
     B.combine_rows_backward(B.BF16, 0, 64, 0, 64, 0, 0, offs.data_ptr(), 3, 2, 0, 64, 0, 64, 0)
     torch.cuda.synchronize()
+
+
+def test_errors_of_earlier_calls_are_not_the_operators():
+    """A HIP call that failed before leaves its error with the thread: every operator that launches is right all the same."""
+    torch = U.torch_mod()
+    hip = B.load_library()                                            # (the runtime that it is linked with)
+    x, i = torch.ones((4, 64), device="cuda"), torch.tensor([0, 1, 2, 3, 4], dtype=torch.int32, device="cuda")
+    y, work, px, pi = torch.zeros((4, 64), device="cuda"), torch.zeros(4096, dtype=torch.uint8, device="cuda"), x.data_ptr(), i.data_ptr()
+    offs = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    ints = torch.zeros(128, dtype=torch.int32, device="cuda")
+    po, py, pw, spare = offs.data_ptr(), y.data_ptr(), work.data_ptr(), ints.data_ptr()
+    for call in (lambda: B.dropout(B.FP32, px, 64, 0, 0, 4, 64, 0.5, 1, 0, 0, 0, py, 64), lambda: B.route(B.FP32, px, 64, 4, 64, 1, 1, spare, 0, 0, 0, 0, 0, 0),
+                 lambda: B.route_backward(B.FP32, px, 64, 4, 64, 1, 1, 0, 0, 0, 0.0, py, 64), lambda: B.sort_by_label(pi, 4, 5, spare, 0, 0, 0, 0),
+                 lambda: B.gather_rows(B.FP32, px, 64, pi, po, 1, 1, 4, 64, py, 64), lambda: B.combine_rows(B.FP32, px, 64, pi, 0, po, 1, 1, 0, 0, 4, 64, py, 64),
+                 lambda: B.combine_rows_backward(B.FP32, px, 64, px, 64, pi, 0, po, 1, 1, 4, 64, py, 64, 0),
+                 lambda: B.group_linear_act(B.FP32, px, 64, px, po, 1, 4, 64, 4, 0, 1, 0, 0, 0, 0, py, 4), lambda: B.group_linear_dgrad_act(B.FP32, px, 4, px, po, 1, 4, 64, 4, 0, 0, 0, 0, 0, py, 64),
+                 lambda: B.group_act_backward(B.FP32, px, 64, 0, 0, 0, po, 1, 4, 64, py, 64, py, pw, 4096)):
+        assert hip.hipSetDevice(12345) != 0                           # refused by the host
+        call()
+    torch.cuda.synchronize()

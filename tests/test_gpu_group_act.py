@@ -13,7 +13,7 @@ from tests import experts_ref as E
 from tests import gpu_util as U
 from tests import operators_ref as R
 from tests.test_gpu_group_linear import SHAPES, SHAPES8, problem8
-from tests.test_gpu_group_linear_large import CASES
+from tests.test_gpu_group_linear_large import CASES, offsets
 from tests.test_gpu_rms_norm import host, matrix
 
 pytestmark = pytest.mark.gpu
@@ -167,6 +167,50 @@ def test_tiles(name, bf16):
             check_dgrad(dgrad(bf16, p["dy"], p["w"], offs, act, p["z"], p["other"]), bf16, p, offs, act, True)
 
 
+def test_tiles_of_128_in_fp32():
+    """1128 tiles forward and in dgrad, whole numbers: exact."""
+    for offs, n_in, n_out in (([0, 2900, 3000], 40, 6000), ([0, 2900, 3000], 6000, 40)):
+        p = problem(offs, n_in, n_out, False, 5, whole=True)
+        z, _, r = reference(p["x"], p["w"], offs, p["bias"], p["residual"])
+        if n_in == 40:
+            got = forward(False, p["x"], p["w"], offs, p["bias"], E.RELU, p["residual"])
+            assert np.array_equal(got[0], z) and np.array_equal(got[1], E.act(z, E.RELU) + r)
+        else:
+            d = R.linear(p["dy"], p["w"].transpose(0, 2, 1), offs)[0]
+            d[:3000] += p["other"][:3000]
+            assert np.array_equal(dgrad(False, p["dy"], p["w"], offs, E.RELU, p["z"], p["other"]), d * (p["z"] > 0))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_the_same_bits_again_and_in_two_calls_at_once(bf16):
+    """Two calls with workspaces of their own on two streams, and one after the other."""
+    torch = U.torch_mod()
+    offs, n_in, n_out = CASES["eight"]
+    groups, rows, kind, prec = len(offs) - 1, offs[-1], torch.bfloat16 if bf16 else torch.float32, B.BF16 if bf16 else B.FP32
+    p = problem(offs, n_in, n_out, bf16)
+    x, w, r, dy, bias, o = (torch.from_numpy(np.asarray(v)).cuda() for v in (p["x"], p["w"], p["residual"], p["dy"], p["bias"], np.asarray(offs, np.int32)))
+    x, w, r, dy = (v.to(kind) for v in (x, w, r, dy))
+    size = B.group_act_backward_bytes(groups, rows, n_out)
+
+    def passes(stream):
+        z, y, dz, dx, dbias, work = torch.empty_like(r), torch.empty_like(r), torch.empty_like(r), torch.empty_like(x), torch.empty_like(bias), torch.empty(size, dtype=torch.uint8, device="cuda")
+        s = stream.cuda_stream
+        B.group_linear_act(prec, x.data_ptr(), n_in, w.data_ptr(), o.data_ptr(), groups, rows, n_in, n_out, bias.data_ptr(), E.GELU, r.data_ptr(), n_out, z.data_ptr(), n_out, y.data_ptr(), n_out, s)
+        B.group_act_backward(prec, dy.data_ptr(), n_out, E.GELU, z.data_ptr(), n_out, o.data_ptr(), groups, rows, n_out, dz.data_ptr(), n_out, dbias.data_ptr(), work.data_ptr(), size, s)
+        B.group_linear_dgrad_act(prec, dz.data_ptr(), n_out, w.data_ptr(), o.data_ptr(), groups, rows, n_in, n_out, 0, 0, E.SILU, x.data_ptr(), n_in, dx.data_ptr(), n_in, s)
+        return z, y, dz, dbias, dx, work
+
+    first = passes(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    both = [passes(s) for s in streams]
+    torch.cuda.synchronize()
+    for again in both:
+        assert all(torch.equal(a, b) for a, b in zip(first[:5], again[:5]))
+
+
 @pytest.mark.parametrize("bf16", [False, True])
 def test_without_an_epilogue_it_is_the_plain_product(bf16):
     """No bias, activation or residual: the bits of gan_group_linear and its gradient."""
@@ -180,7 +224,8 @@ def test_without_an_epilogue_it_is_the_plain_product(bf16):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("offs,n_in,n_out", SHAPES8 + [CASES[n] for n in ("many", "odd", "long", "wide outputs", "few ends, outputs")])
+@pytest.mark.parametrize("offs,n_in,n_out", SHAPES8 + [CASES[n] for n in ("many", "odd", "long", "wide outputs", "few ends, outputs")] +
+                         [(offsets([30, 33, 0, 64, 65, 20, 1, 40]), 600, 4200), (offsets([300, 0, 129, 90]), 520, 6000)])                     # (two sets of waves with 297 and 329 tiles)
 def test_eight_bits(offs, n_in, n_out, bf16):
     torch = U.torch_mod()
     x8, xs, w8, ws = problem8(offs, n_in, n_out, 3)

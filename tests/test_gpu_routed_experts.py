@@ -63,7 +63,7 @@ def test_gradients_of_the_whole_step():
     got = s @ p["w_out"][0].T + p["b_out"][0]
     balance = E.EXPERTS * (counts[:-1] / counts[:-1].sum() * prob.mean(0)).sum()
     (((got - clean.double().cpu()) ** 2).mean() + E.BALANCE * balance).backward()
-    balance = float(balance.detach())
+    balance, got = float(balance.detach()), got.detach()
     assert abs(float(f["balance"]) - balance) <= 0.01 * balance
     assert float((y.double().cpu() - got).norm() / got.norm()) <= np.sqrt(12) * 2.0 ** -8
     for k in p:
