@@ -62,6 +62,10 @@ __device__ __forceinline__ float sum_of(float v) {
 template <int L>
 __device__ __forceinline__ int expert_of(int c) { return (c / 8 * L + (int)(threadIdx.x % L)) * 8 + c % 8; }
 
+// Where an expert stands in a row of LDS: the halves of a lane's chunks lie apart, so that neighbouring lanes' 16 bytes are neighbours.
+template <int L>
+__device__ __forceinline__ int slot_of(int expert) { return expert / (8 * L) * (8 * L) + expert % 8 / 4 * (4 * L) + expert / 8 % L * 4 + expert % 4; }
+
 // Numbers as whole numbers of the same order.  -0 counts as 0, NaN as -infinity, which keys below THERE are.  A bf16 number leaves room for its expert below it, so that keys are all
 // different and equal numbers come in the experts' order.
 constexpr unsigned THERE = 0x00800000u;
@@ -77,7 +81,7 @@ __device__ __forceinline__ float value_of(unsigned key) {
   return __uint_as_float(sizeof(T) == 4 ? u : u & 0xffff0000u);
 }
 
-// A row's logits as they lie in memory, which are asked for while the row before is worked on; then as numbers (-infinity behind the row's end) and keys.
+// A row's logits as they lie in memory, which are asked for while the row before is worked on; then as numbers (-infinity behind the row's end).
 template <typename T, int L, int C>
 struct Row {
   Raw8<T> raw[C / 8];
@@ -85,17 +89,14 @@ struct Row {
 #pragma unroll
     for (int j = 0; j < C / 8; ++j) raw[j].template load<false>(row + expert_of<L>(j * 8), experts - expert_of<L>(j * 8));
   }
-  __device__ __forceinline__ void values(int experts, float (&v)[C], unsigned (&key)[C]) const {        // (of rows that are not there: zeros)
+  __device__ __forceinline__ void values(int experts, float (&v)[C]) const {                       // (of rows that are not there: zeros)
 #pragma unroll
     for (int j = 0; j < C / 8; ++j) {
-      const int e = expert_of<L>(j * 8), left = experts - e;
+      const int left = experts - expert_of<L>(j * 8);
       float w[8];
       raw[j].values(w);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[j * 8 + i] = i < left ? w[i] : -INFINITY;
-        key[j * 8 + i] = key_of<T>(v[j * 8 + i], e + i);
-      }
+      for (int i = 0; i < 8; ++i) v[j * 8 + i] = i < left ? w[i] : -INFINITY;
     }
   }
 };
@@ -172,7 +173,9 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
     const bool in = row < a.rows;
     float v[C];
     unsigned key[C];
-    next.values(a.experts, v, key);
+    next.values(a.experts, v);
+#pragma unroll
+    for (int c = 0; c < C; ++c) key[c] = key_of<T>(v[c], expert_of<L>(c));
     ask(row + (long long)gridDim.x * R);
     const unsigned best = in ? most_of<L>(most(key)) : 0u;
     const float top = value_of<T>(best), inv = 1.f / powers<L>(v, top);
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
   const int at = threadIdx.x / L, lane = threadIdx.x % L;
   float *extra = rows_extra[at], *ps = rows_p[P_ROWS ? at : 0];
 #pragma unroll
-  for (int c = 0; c < C; ++c) extra[expert_of<L>(c)] = 0.f;
+  for (int c = 0; c < C; ++c) extra[slot_of<L>(expert_of<L>(c))] = 0.f;
   float share[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) share[c] = 0.f;
@@ -422,15 +425,23 @@ __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
     const bool in = row < a.rows;
     int id[EACH];
     float g[EACH], l[EACH], v[C];
-    unsigned key[C];
-    next.values(a.experts, v, key);
+    next.values(a.experts, v);
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       id[i] = (unsigned)next_id[i] < (unsigned)a.experts ? next_id[i] : -1;
       g[i] = next_g[i];
     }
     ask(row + (long long)gridDim.x * R);
-    const float top = value_of<T>(most_of<L>(most(key))), inv = 1.f / powers<L>(v, top);
+    // (what is NaN or -infinity is not there; the largest of the others)
+    unsigned there[(C + 31) / 32] = {};
+    float top = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      there[c / 32] |= (v[c] > -INFINITY ? 1u : 0u) << c % 32;
+      top = fmaxf(top, v[c]);
+    }
+    top = __uint_as_float(join<L>(__float_as_uint(top), [](unsigned a, unsigned b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+    const float inv = 1.f / powers<L>(v, top);
     float mean = 0.f, of_chosen = 0.f, of_weights = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -439,13 +450,13 @@ __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
     }
     if constexpr (P_ROWS) {
 #pragma unroll
-      for (int c = 0; c < C; c += 4) *reinterpret_cast<float4*>(ps + expert_of<L>(c)) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+      for (int c = 0; c < C; c += 4) *reinterpret_cast<float4*>(ps + slot_of<L>(expert_of<L>(c))) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
       settle();
     }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       if constexpr (P_ROWS) {
-        l[i] = id[i] >= 0 ? ps[id[i]] : 0.f;
+        l[i] = id[i] >= 0 ? ps[slot_of<L>(id[i])] : 0.f;
       } else {
         const float logit = id[i] >= 0 ? to_float(((const T*)a.logits)[row * a.stride + id[i]]) : 0.f;
         l[i] = id[i] >= 0 && logit > -INFINITY ? __builtin_amdgcn_exp2f((logit - top) * LOG2E) * inv : 0.f;
@@ -459,31 +470,31 @@ __global__ __launch_bounds__(256) void route_back_kernel(RouteBackArgs a) {
       const float over = 1.f / sum_of<L>(of_chosen);
 #pragma unroll
       for (int i = 0; i < EACH; ++i)
-        if (id[i] >= 0) extra[id[i]] = l[i] * over * (g[i] - of_weights * over);
+        if (id[i] >= 0) extra[slot_of<L>(id[i])] = l[i] * over * (g[i] - of_weights * over);
     } else {
       mean += of_weights;
 #pragma unroll
       for (int i = 0; i < EACH; ++i)
-        if (id[i] >= 0) extra[id[i]] = l[i] * g[i];
+        if (id[i] >= 0) extra[slot_of<L>(id[i])] = l[i] * g[i];
     }
     settle();
 #pragma unroll
     for (int j = 0; j < C / 8; ++j) {
       const int e = expert_of<L>(j * 8);
       float d[8];
-      const float4 x = *reinterpret_cast<const float4*>(extra + e), y = *reinterpret_cast<const float4*>(extra + e + 4);
+      const float4 x = *reinterpret_cast<const float4*>(extra + slot_of<L>(e)), y = *reinterpret_cast<const float4*>(extra + slot_of<L>(e + 4));
       const float more[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int c = j * 8 + i;
-        d[i] = key[c] >= THERE ? v[c] * (share[c] - mean) + more[i] : 0.f;
+        d[i] = there[c / 32] >> c % 32 & 1 ? v[c] * (share[c] - mean) + more[i] : 0.f;
       }
       store8<T, false>((T*)a.dlogits + (in ? row : 0) * a.dstride + e, in ? a.experts - e : 0, d);
     }
     settle();
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
-      if (id[i] >= 0) extra[id[i]] = 0.f;
+      if (id[i] >= 0) extra[slot_of<L>(id[i])] = 0.f;
   }
 }
 
