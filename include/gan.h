@@ -378,7 +378,7 @@ gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scale, const ui
      gan_group_linear_dgrad_act  dx[i] = (dy[i] w[g] + other[i]) act'(z[i])    [rows][n_in]: the gradient of the sums z whose activation was x, from the gradient dy of this
                                  layer's sums and that which reaches x by other ways (NULL: none).  GAN_ACT_NONE: z is not read, and dx is that of x.
      gan_group_act_backward      dz = dy act'(z)  [rows][cols], dbias[g] = sum of dz (before its rounding) over g's rows  fp32 [groups][cols], zero for an expert without
-                                 rows; dz or dbias may be NULL.  GAN_ACT_NONE: z is not read.  work: DEVICE, gan_group_act_backward_bytes(...), 16-byte aligned (dbias NULL: none).
+                                 rows; dz or dbias may be NULL.  GAN_ACT_NONE: z is not read.  work: DEVICE, gan_group_act_backward_bytes(...) (0: none is needed), 16-byte aligned (dbias NULL: none).
    Rows of no expert: all their results are zero.  y may be the memory of residual, dx that of other or z, dz that of dy or z, if the strides are the same; z and y are two
    matrices.  The activations at infinity are their limits; act' of GAN_ACT_RELU is 0 at zero. */
 typedef enum { GAN_ACT_NONE = 0, GAN_ACT_RELU = 1, GAN_ACT_GELU = 2 /* z times the normal distribution's Phi(z) */, GAN_ACT_SILU = 3 /* z / (1 + exp(-z)) */ } gan_act;

@@ -27,11 +27,13 @@ struct ActBackArgs {
 // (bf16, 16384 x 4096 of eight experts with both launches: 83 us = 4.9 TB/s; 1 KiB of a row by a wave 95; results through the caches 87; operands converted as they arrive, two waves a SIMD 157;
 // ten experts' 1117 rows of 512 in fp32 7.9).
 constexpr int LANES = 16, WIDE = LANES * 8, AT = 256 / LANES;     // lanes of a row, columns of a tile, its rows at a time
+// Up to so many rows a block takes all of an expert's, and the second launch is saved (8 rows of 64 experts, 128 columns: NEWALL us with both, NEWALL2 so).
+constexpr int ALL_ROWS = 512;
 int wide_tiles(int cols) { return (cols + WIDE - 1) / WIDE; }
 int tall_of(long long rows, int cols) { return rows / 128 * wide_tiles(cols) >= 512 ? 128 : 32; }
 
-// A lane has eight columns of every sixteenth row, U of them in flight.
-template <typename T, bool VEC, bool PAST, int U>
+// A lane has eight columns of every sixteenth row, U of them in flight.  ALL: a block takes all rows of an expert (or those of none), and `partial` is dbias itself.
+template <typename T, bool VEC, bool PAST, int U, bool ALL>
 __global__ __launch_bounds__(256, 4) void act_back_kernel(ActBackArgs a) {
   __shared__ __align__(16) float part[AT][WIDE + 4];
   const int lane = threadIdx.x % LANES, rows_at = threadIdx.x / LANES, wide = (a.cols + WIDE - 1) / WIDE;
@@ -39,8 +41,13 @@ __global__ __launch_bounds__(256, 4) void act_back_kernel(ActBackArgs a) {
     const long long tile = at / wide;
     const int col0 = (int)(at - tile * wide) * WIDE, col = col0 + lane * 8, left = a.cols - col;
     int group, row, end;
-    if (!find_tile(a.offs, a.groups, a.rows, a.tall, (unsigned)tile, group, row, end)) return;    // (no later tile either)
-    end = min(end, row + a.tall);
+    if (ALL) {
+      group = (int)tile;
+      group_rows(a.offs, a.groups, a.rows, group, row, end);
+    } else {
+      if (!find_tile(a.offs, a.groups, a.rows, a.tall, (unsigned)tile, group, row, end)) return;  // (no later tile either)
+      end = min(end, row + a.tall);
+    }
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
@@ -67,7 +74,7 @@ __global__ __launch_bounds__(256, 4) void act_back_kernel(ActBackArgs a) {
         for (int i = 0; i < 8; ++i) sum[i] += d[i];
       }
     }
-    if (!a.partial) continue;
+    if (!a.partial || (ALL && group == a.groups)) continue;
     __syncthreads();
     *reinterpret_cast<float4*>(&part[rows_at][lane * 8]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
     *reinterpret_cast<float4*>(&part[rows_at][lane * 8 + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
@@ -128,7 +135,7 @@ __global__ __launch_bounds__(64) void bias_sum_kernel(const int* offs, int group
 using namespace gan;
 
 extern "C" int64_t gan_group_act_backward_bytes(int32_t groups, int64_t rows, int32_t cols) {
-  if (groups < 1 || rows < 1 || cols < 1 || groups > 65535 || rows > MOST_ROWS || cols > MOST_COLS) return 0;
+  if (groups < 1 || rows <= ALL_ROWS || cols < 1 || groups > 65535 || rows > MOST_ROWS || cols > MOST_COLS) return 0;
   return most_tiles(rows, groups, tall_of(rows, cols)) * cols * (int64_t)sizeof(float);
 }
 
@@ -153,19 +160,20 @@ extern "C" gan_status gan_group_act_backward(int32_t precision, const void* dy, 
   if (rows > 0) {
     const bool vec = cols % 8 == 0 && rows_aligned16(dy, dy_stride, e) && (act == GAN_ACT_NONE || rows_aligned16(z, z_stride, e)) && (!dz || rows_aligned16(dz, dz_stride, e));
     const int tall = tall_of(rows, cols);
-    const ActBackArgs a = {dy, z, offs, dz, dbias && groups > 0 ? (float*)work : nullptr, dy_stride, z_stride, dz_stride, groups, (int)rows, cols, act, tall,
-                           most_tiles(rows, groups, tall)};
+    const bool all = rows <= ALL_ROWS, past = rows * cols * e > PAST_CACHES;
+    float* const partial = dbias && groups > 0 ? all ? dbias : (float*)work : nullptr;
+    const ActBackArgs a = {dy, z, offs, dz, partial, dy_stride, z_stride, dz_stride, groups, (int)rows, cols, act, tall, all ? groups + 1 : most_tiles(rows, groups, tall)};
     const dim3 grid((unsigned)std::min(a.tiles * wide_tiles(cols), 1ll << 20));
-    const bool past = rows * cols * e > PAST_CACHES;
 #define GAN_ACT_BACK(T, V) \
-  if (tall == 32) hipLaunchKernelGGL((act_back_kernel<T, V, false, 2>), grid, dim3(256), 0, st, a); \
-  else if (V && past) hipLaunchKernelGGL((act_back_kernel<T, V, V, 4>), grid, dim3(256), 0, st, a); \
-  else hipLaunchKernelGGL((act_back_kernel<T, V, false, 4>), grid, dim3(256), 0, st, a)
+  if (all) hipLaunchKernelGGL((act_back_kernel<T, V, false, 2, true>), grid, dim3(256), 0, st, a); \
+  else if (tall == 32) hipLaunchKernelGGL((act_back_kernel<T, V, false, 2, false>), grid, dim3(256), 0, st, a); \
+  else if (V && past) hipLaunchKernelGGL((act_back_kernel<T, V, V, 4, false>), grid, dim3(256), 0, st, a); \
+  else hipLaunchKernelGGL((act_back_kernel<T, V, false, 4, false>), grid, dim3(256), 0, st, a)
     if (precision == GAN_FP32) { if (vec) { GAN_ACT_BACK(float, true); } else { GAN_ACT_BACK(float, false); } }
     else { if (vec) { GAN_ACT_BACK(bf16_t, true); } else { GAN_ACT_BACK(bf16_t, false); } }
 #undef GAN_ACT_BACK
   }
-  if (dbias && groups > 0) {
+  if (dbias && groups > 0 && (rows == 0 || rows > ALL_ROWS)) {
     const long long blocks = groups * (((long long)cols + 63) / 64);
     hipLaunchKernelGGL(bias_sum_kernel, dim3((unsigned)std::min(blocks, 1ll << 20)), dim3(64), 0, st, offs, groups, (int)rows, cols, tall_of(rows, cols), (const float*)work, dbias);
   }

@@ -25,7 +25,9 @@ struct RouteArgs {
   float* weight;
   int* counts;                                                    // the results, or NULL (then mean and balance are too)
   float *mean, *balance;
-  float* sums;                                                    // what several blocks leave
+  int* ticket;                                                    // what several blocks leave
+  double* loss;
+  float* sums;
   int* parts;
   long long stride, rows;
   int experts, k, normalize;
@@ -246,6 +248,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
       __syncthreads();
     }
     if (gridDim.x > 1) {
+      if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
       for (int e = threadIdx.x; e < a.experts; e += 256) a.sums[(long long)blockIdx.x * a.experts + e] = wide[e];
       for (int e = threadIdx.x; e <= a.experts; e += 256) a.parts[(long long)blockIdx.x * (a.experts + 1) + e] = hist[e];
       return;
@@ -281,9 +284,9 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
   }
 }
 
-// Counts and means from the blocks' sums: a block for eight experts (128 threads each, a load of up to 1024 blocks' sums at a time), which leaves their shares of the balance loss.
-// (65536 rows, 256 experts: 7.2 us; blocks of 32 experts 16.2, with the loss added up by the last block to come, whose order of memory costs a write-back of the caches, 12.4.)
-__global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, double* loss, int blocks) {
+// Counts, means and the balance loss from the blocks' sums: a block for eight experts (128 threads each, a load of up to 1024 blocks' sums at a time), whose shares of the loss the last
+// block to come adds up in order.  (65536 rows, 256 experts: 12.4 us; blocks of 32 experts 16.2; the loss in a launch of its own 7.2 + 4, and 6397 rows of 100 with it 3 us a pass longer.)
+__global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, int blocks) {
   __shared__ int n[16][SUM_EXPERTS], rows[16];
   __shared__ double d[16][SUM_EXPERTS];
   const int c = threadIdx.x % SUM_EXPERTS, s = threadIdx.x / SUM_EXPERTS, wave = threadIdx.x >> 6, l = threadIdx.x & 63, e = blockIdx.x * SUM_EXPERTS + c;
@@ -332,18 +335,15 @@ __global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, double* lo
   }
   if (threadIdx.x > 0) return;
   if (blockIdx.x == 0) a.counts[a.experts] = counted;
-  loss[2 * blockIdx.x] = share;
-  loss[2 * blockIdx.x + 1] = all;
-}
-__global__ __launch_bounds__(64) void route_balance_kernel(const double* loss, int blocks, int experts, float* balance) {
-  double share = 0, all = 0;
-  for (int b = threadIdx.x; b < blocks; b += 64) share += loss[2 * b], all += loss[2 * b + 1];
-#pragma unroll
-  for (int x = 1; x < 64; x *= 2) {
-    share += __shfl_xor(share, x);
-    all += __shfl_xor(all, x);
+  __hip_atomic_store(&a.loss[2 * blockIdx.x], share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(&a.loss[2 * blockIdx.x + 1], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (__hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) != (int)gridDim.x - 1 || !a.balance) return;
+  share = all = 0;
+  for (int b = 0; b < (int)gridDim.x; ++b) {
+    share += __hip_atomic_load(&a.loss[2 * b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    all += __hip_atomic_load(&a.loss[2 * b + 1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  if (threadIdx.x == 0) *balance = (float)(all > 0 ? share * experts / all : 0);
+  *a.balance = (float)(all > 0 ? share * a.experts / all : 0);
 }
 
 // without rows
@@ -514,7 +514,7 @@ long long tiles_of(long long rows, int experts) {
   const int r = 256 / (experts <= 8 ? 1 : experts <= 32 ? 4 : experts <= 512 ? 16 : 64);
   return (rows + r - 1) / r;
 }
-constexpr int LOSS_BYTES = MOST_EXPERTS / SUM_EXPERTS * 16;
+constexpr int LOSS_AT = 16, SUMS_AT = LOSS_AT + MOST_EXPERTS / SUM_EXPERTS * 16;       // in the workspace, behind the ticket
 // As many blocks as are on the chip together: each has what it leaves behind, or the counts, to see to once (65536 rows of 64 experts, gradient: 13.8 us with 1024 blocks, 17.1 with 512; 16384 of
 // 512: 20.2 with 512, 27.7 with 1024, and forward with counts 26.5, 37).
 int most_blocks(long long rows, int experts) { return (int)std::min(tiles_of(rows, experts), experts > 1024 ? 256ll : experts > 256 && experts <= 512 ? 512ll : 1024ll); }
@@ -536,7 +536,7 @@ using namespace gan;
 extern "C" int64_t gan_route_bytes(int64_t rows, int32_t experts) {
   if (rows < 1 || experts < 1 || rows > MOST_ROWS || experts > MOST_EXPERTS) return 0;
   const int blocks = most_blocks(rows, experts);
-  return blocks > 1 ? LOSS_BYTES + (int64_t)blocks * (2 * experts + 1) * 4 : 0;
+  return blocks > 1 ? SUMS_AT + (int64_t)blocks * (2 * experts + 1) * 4 : 0;
 }
 
 extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t logits_stride, int64_t rows, int32_t experts, int32_t k, int32_t normalize, int32_t* expert,
@@ -554,8 +554,9 @@ extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t l
     return operator_launched();
   }
   const int blocks = most_blocks(rows, experts);
-  float* const sums = (float*)((uint8_t*)work + LOSS_BYTES);
-  const RouteArgs a = {logits, expert, weight, counts, mean, balance, sums, (int*)(sums + (long long)blocks * experts), logits_stride, rows, experts, k, normalize};
+  uint8_t* const w = (uint8_t*)work;
+  float* const sums = (float*)(w + SUMS_AT);
+  const RouteArgs a = {logits, expert, weight, counts, mean, balance, (int*)w, (double*)(w + LOSS_AT), sums, (int*)(sums + (long long)blocks * experts), logits_stride, rows, experts, k, normalize};
   with_lanes(experts, [&](auto l, auto c) {
     constexpr int L = decltype(l)::value, C = decltype(c)::value;
     const unsigned lds = ((L < MOST_CHOICES ? 2 * (256 / L) * k : 0) + (counts ? 2 * experts + 1 : 0)) * 4;
@@ -568,11 +569,7 @@ extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t l
     if (precision == GAN_FP32) go(float());
     else go(bf16_t());
   });
-  if (counts && blocks > 1) {
-    const int sum_blocks = (experts + SUM_EXPERTS - 1) / SUM_EXPERTS;
-    hipLaunchKernelGGL(route_sum_kernel, dim3(sum_blocks), dim3(1024), 0, st, a, (double*)work, blocks);
-    if (balance) hipLaunchKernelGGL(route_balance_kernel, dim3(1), dim3(64), 0, st, (const double*)work, sum_blocks, experts, balance);
-  }
+  if (counts && blocks > 1) hipLaunchKernelGGL(route_sum_kernel, dim3((experts + SUM_EXPERTS - 1) / SUM_EXPERTS), dim3(1024), 0, st, a, blocks);
   return operator_launched();
 }
 

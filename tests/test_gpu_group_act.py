@@ -315,9 +315,10 @@ def act_backward(bf16, dy, act, z, offs, groups, pad=0, offset=0, into=None, wan
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("offs,cols,extra", [([0, 1], 1, 0), ([0, 3], 7, 2), ([0, 5, 5, 130, 131], 40, 0), ([0, 17, 64, 200], 257, 5), ([0, 0, 65], 520, 0), ([0, 300], 1000, 1), ([0, 64, 128, 256], 2056, 70),
-                                             ([0] + [i // 2 for i in range(1, 300)] + [180], 48, 9), ([0, 9000], 33, 0), ([5, 20, 12, 40, 1 << 30, -7, 60], 64, -50), ([0, 2], 40000, 0)])
+                                             ([0] + [i // 2 for i in range(1, 300)] + [180], 48, 9), ([0, 9000], 33, 0), ([0, 512], 130, 0), ([0, 400, 512], 24, 1), ([5, 20, 12, 40, 1 << 30, -7, 60], 64, -50), ([0, 2], 40000, 0)])
 def test_act_backward(offs, cols, extra, bf16):
-    """dbias: a chain of up to 16 rows a wave and the tiles of 64 rows, one after the other: 20 + rows / 64 roundings of the terms, and those of the slope."""
+    """dbias: up to 512 rows a chain of every sixteenth and four joins, at most 36; beyond, 8 rows, four joins, and chains of every eighth of the tiles of 32 rows: 40 + rows / 256 roundings of the terms at
+    most, and those of the slope."""
     rng = np.random.default_rng([len(offs), cols])
     groups, rows = len(offs) - 1, offs[-1] + extra if extra >= 0 else 70
     g = expert_rows(offs, rows, groups)
@@ -330,7 +331,7 @@ def test_act_backward(offs, cols, extra, bf16):
         assert np.all(np.abs(dz - want) <= e + (R.UBF * np.abs(want) if bf16 else 0) + TINY)
         for k in range(groups):
             mine = g == k
-            size = (np.abs(want[mine]) * (20 + rows / 64) * R.U32 + e[mine]).sum(0)
+            size = (np.abs(want[mine]) * (40 + rows / 256) * R.U32 + e[mine]).sum(0)
             assert np.all(np.abs(dbias[k] - want[mine].sum(0)) <= size + TINY), k
     alone = act_backward(bf16, dy, act, None, offs, groups, want_dz=False)
     assert np.array_equal(alone[1], dbias) and np.array_equal(alone[0], np.full_like(dz, 7.0))
