@@ -25,7 +25,7 @@ struct RouteArgs {
   float* weight;
   int* counts;                                                    // the results, or NULL (then mean and balance are too)
   float *mean, *balance;
-  int* ticket;                                                    // what several blocks leave
+  int* ticket;                                                    // what several blocks leave; NULL: the balance has a launch of its own
   double* loss;
   float* sums;
   int* parts;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
       __syncthreads();
     }
     if (gridDim.x > 1) {
-      if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
+      if (a.ticket && blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
       for (int e = threadIdx.x; e < a.experts; e += 256) a.sums[(long long)blockIdx.x * a.experts + e] = wide[e];
       for (int e = threadIdx.x; e <= a.experts; e += 256) a.parts[(long long)blockIdx.x * (a.experts + 1) + e] = hist[e];
       return;
@@ -284,8 +284,9 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
   }
 }
 
-// Counts, means and the balance loss from the blocks' sums: a block for eight experts (128 threads each, a load of up to 1024 blocks' sums at a time), whose shares of the loss the last
-// block to come adds up in order.  (65536 rows, 256 experts: 12.4 us; blocks of 32 experts 16.2; the loss in a launch of its own 7.2 + 4, and 6397 rows of 100 with it 3 us a pass longer.)
+// Counts, means and the balance loss from the blocks' sums: a block for eight experts (128 threads each, a load of up to 1024 blocks' sums at a time).  Their shares of the loss are added up in
+// order by the last block to come, whose order of memory costs a write-back of the caches, or (no ticket) by a launch of its own: 65536 rows, 256 experts 12.4 us, 7.2 + 4 in two launches, a pass
+// 60, 57; 6397 rows of 100: 7.0, 4.9 + 1.4, but a pass, whose time is the host's, 25.5, 28.5.  (Blocks of 32 experts: 16.2.)
 __global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, int blocks) {
   __shared__ int n[16][SUM_EXPERTS], rows[16];
   __shared__ double d[16][SUM_EXPERTS];
@@ -335,6 +336,11 @@ __global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, int blocks
   }
   if (threadIdx.x > 0) return;
   if (blockIdx.x == 0) a.counts[a.experts] = counted;
+  if (!a.ticket) {
+    a.loss[2 * blockIdx.x] = share;
+    a.loss[2 * blockIdx.x + 1] = all;
+    return;
+  }
   __hip_atomic_store(&a.loss[2 * blockIdx.x], share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __hip_atomic_store(&a.loss[2 * blockIdx.x + 1], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   if (__hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) != (int)gridDim.x - 1 || !a.balance) return;
@@ -344,6 +350,17 @@ __global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a, int blocks
     all += __hip_atomic_load(&a.loss[2 * b + 1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   *a.balance = (float)(all > 0 ? share * a.experts / all : 0);
+}
+
+__global__ __launch_bounds__(64) void route_balance_kernel(const double* loss, int blocks, int experts, float* balance) {
+  double share = 0, all = 0;
+  for (int b = threadIdx.x; b < blocks; b += 64) share += loss[2 * b], all += loss[2 * b + 1];
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) {
+    share += __shfl_xor(share, x);
+    all += __shfl_xor(all, x);
+  }
+  if (threadIdx.x == 0) *balance = (float)(all > 0 ? share * experts / all : 0);
 }
 
 // without rows
@@ -554,9 +571,10 @@ extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t l
     return operator_launched();
   }
   const int blocks = most_blocks(rows, experts);
+  const bool apart = (long long)blocks * experts >= 1 << 17;
   uint8_t* const w = (uint8_t*)work;
   float* const sums = (float*)(w + SUMS_AT);
-  const RouteArgs a = {logits, expert, weight, counts, mean, balance, (int*)w, (double*)(w + LOSS_AT), sums, (int*)(sums + (long long)blocks * experts), logits_stride, rows, experts, k, normalize};
+  const RouteArgs a = {logits, expert, weight, counts, mean, balance, apart ? nullptr : (int*)w, (double*)(w + LOSS_AT), sums, (int*)(sums + (long long)blocks * experts), logits_stride, rows, experts, k, normalize};
   with_lanes(experts, [&](auto l, auto c) {
     constexpr int L = decltype(l)::value, C = decltype(c)::value;
     const unsigned lds = ((L < MOST_CHOICES ? 2 * (256 / L) * k : 0) + (counts ? 2 * experts + 1 : 0)) * 4;
@@ -569,7 +587,11 @@ extern "C" gan_status gan_route(int32_t precision, const void* logits, int64_t l
     if (precision == GAN_FP32) go(float());
     else go(bf16_t());
   });
-  if (counts && blocks > 1) hipLaunchKernelGGL(route_sum_kernel, dim3((experts + SUM_EXPERTS - 1) / SUM_EXPERTS), dim3(1024), 0, st, a, blocks);
+  if (counts && blocks > 1) {
+    const int sum_blocks = (experts + SUM_EXPERTS - 1) / SUM_EXPERTS;
+    hipLaunchKernelGGL(route_sum_kernel, dim3(sum_blocks), dim3(1024), 0, st, a, blocks);
+    if (balance && apart) hipLaunchKernelGGL(route_balance_kernel, dim3(1), dim3(64), 0, st, (const double*)(w + LOSS_AT), sum_blocks, experts, balance);
+  }
   return operator_launched();
 }
 
