@@ -225,7 +225,7 @@ def test_without_an_epilogue_it_is_the_plain_product(bf16):
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("offs,n_in,n_out", SHAPES8 + [CASES[n] for n in ("many", "odd", "long", "wide outputs", "few ends, outputs")] +
-                         [(offsets([30, 33, 0, 64, 65, 20, 1, 40]), 600, 4200), (offsets([300, 0, 129, 90]), 520, 6000)])                     # (two sets of waves with 297 and 329 tiles)
+                         [(offsets([30, 33, 0, 64, 65, 20, 1, 40]), 600, 4200), (offsets([300, 0, 129, 90]), 520, 6000)])                     # (297 tiles for two sets of waves, 329 for one)
 def test_eight_bits(offs, n_in, n_out, bf16):
     torch = U.torch_mod()
     x8, xs, w8, ws = problem8(offs, n_in, n_out, 3)
@@ -317,7 +317,7 @@ def act_backward(bf16, dy, act, z, offs, groups, pad=0, offset=0, into=None, wan
 @pytest.mark.parametrize("offs,cols,extra", [([0, 1], 1, 0), ([0, 3], 7, 2), ([0, 5, 5, 130, 131], 40, 0), ([0, 17, 64, 200], 257, 5), ([0, 0, 65], 520, 0), ([0, 300], 1000, 1), ([0, 64, 128, 256], 2056, 70),
                                              ([0] + [i // 2 for i in range(1, 300)] + [180], 48, 9), ([0, 9000], 33, 0), ([0, 512], 130, 0), ([0, 400, 512], 24, 1), ([5, 20, 12, 40, 1 << 30, -7, 60], 64, -50), ([0, 2], 40000, 0)])
 def test_act_backward(offs, cols, extra, bf16):
-    """dbias: up to 512 rows a chain of every sixteenth and four joins, at most 36; beyond, 8 rows, four joins, and chains of every eighth of the tiles of 32 rows: 40 + rows / 256 roundings of the terms at
+    """dbias: up to 512 rows a chain of every sixteenth and four joins, at most 36; beyond, 8 rows, four joins, and chains of every 64th of the tiles of 32 rows, 3 + 7 joins: 40 + rows / 256 roundings of the terms at
     most, and those of the slope."""
     rng = np.random.default_rng([len(offs), cols])
     groups, rows = len(offs) - 1, offs[-1] + extra if extra >= 0 else 70

@@ -154,6 +154,8 @@ def test_many_rows(e, k):
     assert np.all(np.abs(got["weight"] - want["weight"]) <= 2 * spread(l).max() * want["weight"])
     size = (want["p"] * (spread(l) + 64 * R.U32)).sum(0) / want["counts"][-1]
     assert np.all(np.abs(got["mean"] - want["mean"]) <= size)
+    share = want["counts"][:e] / want["counts"][:e].sum()
+    assert abs(got["balance"] - want["balance"]) <= e * (share * size).sum() + 2 * R.U32 * want["balance"]
     again = run(l, k, True, True)
     assert all(np.array_equal(got[n], again[n]) for n in ("expert", "weight", "counts", "mean")) and got["balance"] == again["balance"]
 
