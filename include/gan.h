@@ -318,9 +318,9 @@ gan_status gan_op_dw4_to_dw3(gan_ctx* ctx, const float* dw4, float* dw3, int32_t
    16 bytes run faster), up to 2^30 rows and 2^28 elements a row; offsets into tensors are 64-bit.  `precision` is the storage
    type: GAN_FP32, or GAN_BF16_FP32MASTER for bf16 matrices; sums and statistics are fp32.
    Every call enqueues its kernels on hip_stream (a hipStream_t of the current device, 0 = the null stream) and returns
-   without waiting; nothing is allocated or kept, so calls may be captured into a graph (of gan_adamw_step see below).  Every sum runs in an order
+   without waiting; nothing is allocated or kept, so calls may be captured into a graph (of gan_adamw_step and gan_dropout's step see below).  Every sum runs in an order
    fixed by sizes and offsets: results are the same bit for bit from run to run.  Zero rows or zero groups are valid, and a matrix
-   without elements may be NULL.
+   without elements may be NULL.  A workspace is a call's until its kernels are done: calls that may run at the same time, replayed graphs among them, need one each.
    Refusals (GAN_E_ARG, GAN_E_SHAPE) come before anything is launched; gan_operator_last_error has the reason (text of the calling
    thread's last failed call, never NULL).
 

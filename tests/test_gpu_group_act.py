@@ -273,6 +273,22 @@ def test_the_activations_at_every_size_of_z(n_in, bf16):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n_in,n_out", [(64, 128), (33, 50), (600, 1100)])
+def test_offsets_that_are_none(n_in, n_out, bf16):
+    """Decreasing offsets and offsets outside the rows count as the nearest that are valid; nothing is read or written elsewhere.  Whole numbers."""
+    offs = [5, 20, 12, 40, 1 << 30, -7, 60]
+    rng = np.random.default_rng(5)
+    m = lambda *s: rng.integers(-2, 3, s).astype(np.float32)  # noqa: E731
+    x, w, bias, res, dy, z, other = m(70, n_in), m(6, n_out, n_in), m(6, n_out), m(70, n_out), m(70, n_out), m(70, n_in), m(70, n_in)
+    s, _, r = reference(x, w, offs, bias, res)
+    got = forward(bf16, x, w, offs, bias, E.RELU, res)
+    assert np.array_equal(got[0], U.round_to(s.astype(np.float32), bf16)) and np.array_equal(got[1], U.round_to((E.act(s, E.RELU) + r).astype(np.float32), bf16))
+    g = expert_rows(offs, 70, 6)
+    d = (R.linear(dy, w.transpose(0, 2, 1), offs)[0] + np.where((g >= 0)[:, None], other, 0)) * (z > 0)
+    assert np.array_equal(dgrad(bf16, dy, w, offs, E.RELU, z, other), U.round_to(d.astype(np.float32), bf16))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("n_in,n_out", [(128, 64), (37, 29)])
 def test_values_that_are_not_finite_stay_with_their_row(n_in, n_out, bf16):
     """In a row of the operands, in one expert's bias, and in rows of no expert, whose residual, z and other hold NaN: their results are zero."""
