@@ -1033,6 +1033,7 @@ __global__ __launch_bounds__(64 * NW) void linear_few_kernel(Q q) {
       __builtin_amdgcn_sched_barrier(0);                          // (all of them in flight before the first is waited for)
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        if (k0 + u * DEEP >= q.k) break;                          // (what is behind the sum's end is zeros)
         if constexpr (ES == 4) {
           const int left = q.k - (k0 + u * DEEP + (l >> 4) * EACH);
           if (q.k % EACH) {                                       // (the values behind a row's last are the next row's)
@@ -1124,6 +1125,7 @@ __global__ __launch_bounds__(64 * NW) void linear_few_dgrad_kernel(Q q) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        if (k0 + u * DEEP >= q.k) break;                          // (what is behind the sum's end is zeros)
         if constexpr (ANY_ROWS) {
 #pragma unroll
           for (int e = 0; e < EACH; ++e) fw[u][e] = shift_last(fw[u][e], q.n - col, q.n < 8);
@@ -1250,7 +1252,13 @@ gan_status launch_few_dgrad_as(const Q& q, hipStream_t st) {
 }
 template <typename T, bool ANY_ROWS, typename Q>
 gan_status launch_few_dgrad(const Q& q, int sixteens, hipStream_t st) {
-  if constexpr (sizeof(T) == 4) return launch_few_dgrad_as<T, 1, 2, 8, false>(q, st);
+  // In fp32 32 rows a block where they leave blocks enough, or the sum is short (us with an epilogue, 16 rows, 32): ten experts of 112, 784 <- 512 (585 blocks of 32) 25.8, 20.0; eight of 250,
+  // 1024 <- 1024 (1120) 55.3, 54.1; one of 1000, 512 <- 512 (256) 9.8, 9.1; but four of 75, 2048 <- 1024 (416) 22.6, 24.3; 16 of 25, 1024 <- 2048 (448) 41.9, 45.7; ten of 112, 110 <- 6272
+  // (90) 41, 61.  The sums' order is the same.
+  if constexpr (sizeof(T) == 4) {
+    const bool two = q.rows / most_groups(q) > 16 && (q.k <= 512 || most_tiles(q.rows, q.groups, 32) * ceil_div(q.n, 64) >= 512);
+    return two ? launch_few_dgrad_as<T, 2, 2, 8, false>(q, st) : launch_few_dgrad_as<T, 1, 2, 8, false>(q, st);
+  }
   else return sixteens == 2 ? launch_few_dgrad_as<T, 2, 2, 8, ANY_ROWS>(q, st) : launch_few_dgrad_as<T, 1, 2, 8, ANY_ROWS>(q, st);
 }
 
