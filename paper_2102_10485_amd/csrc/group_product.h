@@ -1158,7 +1158,7 @@ __global__ __launch_bounds__(64 * NW) void linear_few_dgrad_kernel(Q q) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (k0 + u * DEEP >= q.k) break;                          // (what is behind the sum's end is zeros)
+        if (ES == 4 && k0 + u * DEEP >= q.k) break;                         // (what is behind the sum's end is zeros)
         if constexpr (ANY_ROWS) {
 #pragma unroll
           for (int e = 0; e < EACH; ++e) fw[u][e] = shift_last(fw[u][e], q.n - col, q.n < 8);
