@@ -1,4 +1,4 @@
-// Which codes of its rows an 8-bit operand of a grouped product asks for (group_linear.hip): a step's when the step before it is written to LDS, so that the loads
+// Which codes of its rows an 8-bit operand of a grouped product asks for (group_product.h): a step's when the step before it is written to LDS, so that the loads
 // have a step's time.  Plain arithmetic, which the host can walk too.
 #pragma once
 
@@ -18,6 +18,16 @@ struct CodeWalk {
   GAN_DEVICE_INLINE void started(int k_end) { k = k_end - first > CODE_STEP ? first + CODE_STEP : first; }
   // the step that `left` sum indices begin with has been written, and k asked for
   GAN_DEVICE_INLINE void asked(int left) { k = left > 2 * CODE_STEP ? k + CODE_STEP : first; }
+};
+
+// The same for loads that have two steps' time: two steps are asked for before the first is written, and each write asks for the step two behind it.  Behind the last
+// step it goes on from the first.
+struct CodeWalkTwo {
+  int k, first, end;                                              // k: of the step that is asked for next
+
+  GAN_DEVICE_INLINE void start(int k0, int k_end) { k = first = k0, end = k_end; }
+  // k has been asked for
+  GAN_DEVICE_INLINE void asked() { k = k + CODE_STEP < end ? k + CODE_STEP : first; }
 };
 
 }  // namespace gan

@@ -627,8 +627,25 @@ struct Loaded : Tile<KMAJOR, R, NW> {
   }
 };
 
-// An 8-bit operand, k-major: chunks of sixteen codes of a row, thread t's being chunk t % 4 of rows t / 4, t / 4 + THREADS / 4, ...  A chunk is written to LDS two
-// steps after it was asked for.
+// 16 codes of row r with their scale's byte to LDS as two pieces of bf16 from the c-th on.
+template <typename S>
+__device__ __forceinline__ void write_codes(const uint4& q, int byte, int r, int c, unsigned char* lds) {
+  const float f = power_of_two(byte);
+  const unsigned w[4] = {q.x, q.y, q.z, q.w};
+  u32x4 lo, hi;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    lo[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], f, false));
+    lo[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], f, true));
+    hi[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 + i], f, false));
+    hi[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 + i], f, true));
+  }
+  *reinterpret_cast<u32x4*>(lds + r * 128 + ((c ^ S::swap_of(r)) * 16)) = lo;
+  *reinterpret_cast<u32x4*>(lds + r * 128 + (((c + 1) ^ S::swap_of(r)) * 16)) = hi;
+}
+
+// An 8-bit operand, k-major: chunks of sixteen codes of a row, thread t's being chunk t % 4 of rows t / 4, t / 4 + THREADS / 4, ...  A chunk is written to LDS a
+// step after it was asked for.
 template <int R, int NW>
 struct Converted : Tile<true, R, NW> {
   typedef Tile<true, R, NW> S;
@@ -666,21 +683,59 @@ struct Converted : Tile<true, R, NW> {
   }
   __device__ __forceinline__ void next_step() {}
   __device__ __forceinline__ void piece(int p, int, int left, unsigned char* lds, unsigned) {
-    const int r = thread() / 4 + p * (16 * NW), c = thread() % 4 * 2;
-    const float f = power_of_two(byte[p]);
-    const unsigned w[4] = {q[p].x, q[p].y, q[p].z, q[p].w};
-    u32x4 lo, hi;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      lo[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], f, false));
-      lo[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], f, true));
-      hi[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 + i], f, false));
-      hi[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 + i], f, true));
-    }
-    *reinterpret_cast<u32x4*>(lds + r * 128 + ((c ^ S::swap_of(r)) * 16)) = lo;
-    *reinterpret_cast<u32x4*>(lds + r * 128 + (((c + 1) ^ S::swap_of(r)) * 16)) = hi;
+    write_codes<S>(q[p], byte[p], thread() / 4 + p * (16 * NW), thread() % 4 * 2, lds);
     ask(p);
     if (p == CHUNKS - 1) walk.asked(left);
+  }
+};
+
+// The same with two steps of codes in registers: a chunk is written to LDS two steps after it was asked for, which 128 x 128 tiles have the registers for (194 of
+// 256) and whose few waves wait for the codes otherwise: with an epilogue, one step ahead and two, us: eight experts of 32 rows, 4096 -> 4096, 41.9, 39.4; four of 40 32.2, 29.5; one of 256 41.3, 39.7;
+// 32 of 47, 1024 -> 1024, 16.6, 16.0.  The sums are the same.  piece<B>: of the steps in register set B, every second one.
+template <int R, int NW>
+struct ConvertedTwo : Tile<true, R, NW> {
+  typedef Tile<true, R, NW> S;
+  __device__ static __forceinline__ int thread() { return threadIdx.x & (64 * NW - 1); }
+  typedef uint8_t T;
+  static constexpr bool COPIES = false;
+  static constexpr int CHUNKS = R * 4 / (64 * NW);
+  static constexpr int PIECES = CHUNKS;
+  static_assert(R * 4 % (64 * NW) == 0, "whole chunks");
+  uint4 q[2][CHUNKS];
+  int byte[2][CHUNKS];
+  __amdgpu_buffer_rsrc_t codes, scales;
+  unsigned off[CHUNKS], scale_off[CHUNKS];
+  CodeWalkTwo walk;
+
+  __device__ __forceinline__ void prepare(const T* base, const uint8_t* scale, long long stride, int row0, int rows, int k0, int k_end, int) {
+    const long long blocks = stride / BLOCK8;
+    codes = buffer_of(base + row0 * stride, (unsigned long long)(rows * stride));
+    scales = buffer_of(scale + row0 * blocks, (unsigned long long)(rows * blocks));
+#pragma unroll
+    for (int p = 0; p < CHUNKS; ++p) {
+      const int r = thread() / 4 + p * (16 * NW);
+      off[p] = r < rows ? (unsigned)(r * stride) + thread() % 4 * 16 : NO_ROW;
+      scale_off[p] = r < rows ? (unsigned)(r * blocks) : NO_ROW;
+    }
+    walk.start(k0, k_end);
+#pragma unroll
+    for (int p = 0; p < CHUNKS; ++p) ask<0>(p);
+    walk.asked();
+#pragma unroll
+    for (int p = 0; p < CHUNKS; ++p) ask<1>(p);
+    walk.asked();
+  }
+  template <int B>
+  __device__ __forceinline__ void ask(int p) {
+    q[B][p] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)off[p], walk.k, 0));
+    byte[B][p] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_off[p], walk.k / BLOCK8, 0);
+  }
+  __device__ __forceinline__ void next_step() {}
+  template <int B>
+  __device__ __forceinline__ void piece(int p, unsigned char* lds) {
+    write_codes<S>(q[B][p], byte[B][p], thread() / 4 + p * (16 * NW), thread() % 4 * 2, lds);
+    ask<B>(p);
+    if (p == CHUNKS - 1) walk.asked();
   }
 };
 
@@ -688,14 +743,16 @@ enum Form { ALIGNED, ANY, EIGHT_BITS };
 template <Form F, bool KMAJOR, int R, int NW> struct Operand { typedef Copied<KMAJOR, R, NW> type; };
 template <bool KMAJOR, int R, int NW> struct Operand<ANY, KMAJOR, R, NW> { typedef Loaded<KMAJOR, R, NW> type; };
 template <int R, int NW> struct Operand<EIGHT_BITS, true, R, NW> { typedef Converted<R, NW> type; };
+template <bool TWO, typename O, int R, int NW> struct Ahead { typedef O type; };
+template <typename O, int R, int NW> struct Ahead<true, O, R, NW> { typedef ConvertedTwo<R, NW> type; };
 
-// One tile of expert `group` (q.groups: of none): rows m0 .. m_end - 1, columns n0 .., sum indices k_begin .. k_end - 1.
-template <Form F, int KIND, int BM, int BN, int WM, int WN, int S, int SPLIT, typename C, typename Q>
+// One tile of expert `group` (q.groups: of none): rows m0 .. m_end - 1, columns n0 .., sum indices k_begin .. k_end - 1.  TWO: 8-bit operands are two steps ahead.
+template <Form F, int KIND, int BM, int BN, int WM, int WN, int S, int SPLIT, typename C, bool TWO = false, typename Q>
 __device__ __forceinline__ void tile_product(const Q& q, unsigned char* lds, int group, int part, int m0, int m_end, int n0, int k_begin, int k_end) {
   constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   constexpr bool EIGHT = F == EIGHT_BITS;
-  typedef typename Operand<F, KIND != WGRAD, BM, NW>::type CA;
-  typedef typename Operand<F, KIND == FORWARD, BN, NW>::type CB;
+  typedef typename Ahead<TWO, typename Operand<F, KIND != WGRAD, BM, NW>::type, BM, NW>::type CA;
+  typedef typename Ahead<TWO, typename Operand<F, KIND == FORWARD, BN, NW>::type, BN, NW>::type CB;
   typedef typename CA::T T;
   constexpr int STAGE = CA::BYTES + CB::BYTES;                    // S of them
   // SPLIT = 2: two sets of waves take half of the sum each, with stages of their own
@@ -733,9 +790,14 @@ __device__ __forceinline__ void tile_product(const Q& q, unsigned char* lds, int
     if (SPLIT > 1) lds += set * S * STAGE;
     const unsigned lds0 = lds_address(lds);
     constexpr int PIECES = CA::PIECES + CB::PIECES;
-    auto copy_piece = [&](int p, int stage) {
-      if (p < CA::PIECES) ca.piece(p, wave, left, lds + stage * STAGE, lds0 + stage * STAGE);
-      else cb.piece(p - CA::PIECES, wave, left, lds + stage * STAGE + CA::BYTES, lds0 + stage * STAGE + CA::BYTES);
+    auto copy_piece = [&](int p, auto stage) {                    // (TWO: the stage, a constant, is the register set too)
+      if constexpr (TWO) {
+        if (p < CA::PIECES) ca.template piece<stage.value>(p, lds + stage * STAGE);
+        else cb.template piece<stage.value>(p - CA::PIECES, lds + stage * STAGE + CA::BYTES);
+      } else {
+        if (p < CA::PIECES) ca.piece(p, wave, left, lds + stage * STAGE, lds0 + stage * STAGE);
+        else cb.piece(p - CA::PIECES, wave, left, lds + stage * STAGE + CA::BYTES, lds0 + stage * STAGE + CA::BYTES);
+      }
     };
 
     // Half a step is multiplied while the operands of the next half are read from LDS, so that the matrix pipe sees no wait: the second half's during the
@@ -750,7 +812,7 @@ __device__ __forceinline__ void tile_product(const Q& q, unsigned char* lds, int
     };
     constexpr int SLOTS = TM > 2 ? TM - 1 : TM;                   // rows of products that reads and copies are issued between
     // products of `f`; meanwhile the operands `next` of half h of `stage`, and (copy) the copies of another step into `into`
-    auto half_step = [&](const Operands& f, Operands& next, int stage, int h, auto copy, int into) {
+    auto half_step = [&](const Operands& f, Operands& next, int stage, int h, auto copy, auto into) {
       static_for<0, TM>([&](auto iv) {
         constexpr int i = iv.value;
         static_for<i * (TM + TN) / SLOTS, (i + 1) * (TM + TN) / SLOTS>([&](auto p) { if constexpr (p.value < TM + TN) read_piece(next, p.value, stage, h); });
@@ -764,27 +826,44 @@ __device__ __forceinline__ void tile_product(const Q& q, unsigned char* lds, int
 
     // (Copies behind the last step ask for nothing and fill the stage with zeros; its operands are read and not multiplied.)
     static_assert(CA::COPIES || S == 2, "operands that go through registers are a step ahead");
+    if constexpr (TWO) {
+      static_assert(S == 2, "a register set for each stage");
+      static_for<0, 2>([&](auto s) { static_for<0, PIECES>([&](auto p) { copy_piece(p.value, s); }); });
+    } else {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      ca.next_step();
-      cb.next_step();
+      for (int s = 0; s < S; ++s) {
+        ca.next_step();
+        cb.next_step();
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) copy_piece(p, s);
-      left -= STEP;
+        for (int p = 0; p < PIECES; ++p) copy_piece(p, s);
+        left -= STEP;
+      }
     }
     if constexpr (CA::COPIES) wait_vm<(S - 1) * PIECES>();
     __syncthreads();
     static_for<0, TM + TN>([&](auto p) { read_piece(f0, p.value, 0, 0); });
-    for (int s = 0, stage = 0; s < steps; ++s) {
-      const int next = stage + 1 < S ? stage + 1 : 0;
-      half_step(f0, f1, stage, 1, std::false_type(), 0);
-      if constexpr (CA::COPIES) wait_vm<(S - 2) * PIECES>();
-      __syncthreads();
-      ca.next_step();
-      cb.next_step();
-      half_step(f1, f0, next, 0, std::true_type(), stage);
-      left -= STEP;
-      stage = next;
+    if constexpr (TWO) {
+      const auto step = [&](auto stage) {
+        half_step(f0, f1, stage, 1, std::false_type(), stage);
+        __syncthreads();
+        half_step(f1, f0, 1 - stage, 0, std::true_type(), stage);
+      };
+      for (int s = 0; s < steps; s += 2) {
+        step(std::integral_constant<int, 0>());
+        if (s + 1 < steps) step(std::integral_constant<int, 1>());
+      }
+    } else {
+      for (int s = 0, stage = 0; s < steps; ++s) {
+        const int next = stage + 1 < S ? stage + 1 : 0;
+        half_step(f0, f1, stage, 1, std::false_type(), 0);
+        if constexpr (CA::COPIES) wait_vm<(S - 2) * PIECES>();
+        __syncthreads();
+        ca.next_step();
+        cb.next_step();
+        half_step(f1, f0, next, 0, std::true_type(), stage);
+        left -= STEP;
+        stage = next;
+      }
     }
     if constexpr (CA::COPIES) wait_vm<0>();
     __syncthreads();                                              // nothing is written to LDS any more, or read
@@ -877,17 +956,18 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void linear_kernel(Q q) {
   find_tile_of(sort, q.offs, q.groups, q.rows, BM, r, group, m0, m_end);
   const int k = group < q.groups ? q.k : 0;
   if (sort == WHOLE) m_end = min(m_end, m0 + BM);
+  constexpr bool TWO = F == EIGHT_BITS && BM == 128 && std::is_same_v<Q, ActArgs>;
   if (sort <= HIGH)
-    tile_product<F, KIND, BM, BN, WM, WN, P::S, SPLIT, C>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, k);
+    tile_product<F, KIND, BM, BN, WM, WN, P::S, SPLIT, C, TWO>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, k);
   else if (narrow) {
     if constexpr (P::NARROW) {
       if (sort == HALF) tile_product<F, KIND, BM / 2, BN / 2, WM, WN / 2, P::S_NARROW_HALF, 2, C>(q, lds, group, 0, m0, m_end, (int)c * (BN / 2), 0, k);
       else tile_product<F, KIND, BM / 4, BN / 2, WM, WN / 2, P::S_NARROW_QUARTER, 2, C>(q, lds, group, 0, m0, m_end, (int)c * (BN / 2), 0, k);
     }
   } else if (!P::QUARTERS || sort == HALF) {
-    tile_product<F, KIND, BM / 2, BN, WM, WN, P::S_HALF, SPLIT, C>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, k);
+    tile_product<F, KIND, BM / 2, BN, WM, WN, P::S_HALF, SPLIT, C, TWO>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, k);
   } else if constexpr (P::QUARTERS) {
-    tile_product<F, KIND, BM / 4, BN, WM, WN, P::S_QUARTER, SPLIT, C>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, k);
+    tile_product<F, KIND, BM / 4, BN, WM, WN, P::S_QUARTER, SPLIT, C, TWO>(q, lds, group, 0, m0, m_end, (int)c * BN, 0, k);
   }
 }
 
@@ -1255,7 +1335,8 @@ gan_status launch_large(const Q& q, hipStream_t st) {
     if (big) return launch_tiles<F, KIND, 256, 256, 2, 4, 1, C>(q, st);
   // With an epilogue: up to a tile a CU, as two sets of waves leave room for one block (us without, with: eight experts of 992 rows, 704 -> 512 (280 tiles), 17, 26, in 8 bits 19, 28; of 250,
   // 1024 -> 2048 (368) 22, 32; one of 4000, 4096 -> 1024 (256) 49, 42, 51, 44), and in 8 bits, whose steps wait for the conversion, up to 576 where experts have up to 64 rows, whose tiles are
-  // half as high: eight of 32, 4096 -> 4096 (320) 51, 40, of 62 (352) 58, 46; 16 of 25, 2048 -> 2048 (304) 25.6, 22; but a hundred of 16, 1024 -> 1024 (896) 40, 55, and eight of 125 (480) 66, 74.
+  // half as high: eight of 32, 4096 -> 4096 (320) 42, 39, of 62 (352) 47, 44, of 16 (288) 42, 37; 16 of 25, 2048 -> 2048 (304) 23, 22; but a hundred of 16, 1024 -> 1024 (896) 41, 55, and eight of
+  // 125 (480) 60, 74.
   // In bf16 the first is 62, 68.  (Products without an epilogue keep the order of their sums.)
   const long long count = tiles(q, 128, 128);
   const bool two = !std::is_same_v<Q, ActArgs> ? count <= 288 : count <= 256 || (F == EIGHT_BITS && count <= 576 && q.rows / most_groups(q) <= 64);
