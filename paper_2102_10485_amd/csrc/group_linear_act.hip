@@ -1,5 +1,5 @@
 // Products grouped by label with bias, activation and residual in their epilogue, and the gradient that goes through the activation before them: the calls, and which kernel
-// each takes (group_product.h; the rules are those of the products without).
+// each takes (group_product.h, whose rules are those of the products without but where they say so).
 #include "group_product.h"
 
 using namespace gan;
@@ -11,6 +11,17 @@ gan_status check_epilogue(int32_t act, const void* add, long long add_stride, co
   if (add && add_stride < cols) return operator_fail(GAN_E_ARG, add_why);
   if (z && z_stride < cols) return operator_fail(GAN_E_ARG, "z_stride is below the row's length");
   return GAN_OK;
+}
+
+// Sixteens of rows for the kernel for few rows in 8 bits.  Next to few_rows(): experts of up to 64 rows go to tiles, two sets of waves to each, where those are at most one a CU while this kernel's
+// blocks, each of which converts all of its codes, are several turns of a long sum (us by this kernel, in tiles): four experts of 32, 4096 -> 4096: 46, 32; eight of 32, 4096 -> 2048: 51, 32; eight of
+// 16, 4096 -> 4096: 54, 37; 16 of 25, 2048 -> 1280: 20.3, 19.1; but eight of 50, 2048 -> 1024: 15, 18; one of 64, 4096 -> 4096: 19, 28; 16 of 12, 2048 -> 2432 (304 tiles): 29, 37; one of 160,
+// 4096 -> 2816: 32, 39; two of 60, 8192 -> 2048: 50, 68.
+int few_rows8(const LinearArgs& q) {
+  const int few = few_rows(q, FORWARD, 1);
+  const long long groups = most_groups(q), each = q.rows / groups;
+  const bool tiled = each <= 64 && q.k <= 4096 && groups * ceil_div(q.n, 128) <= 256 && (q.rows + 16 * groups) * ceil_div(q.n, 32) * q.k > 50ll << 20;
+  return few == 2 && tiled ? 0 : few;
 }
 
 }  // namespace
@@ -66,7 +77,7 @@ extern "C" gan_status gan_group_linear8_act(const uint8_t* x8, const uint8_t* x_
   const LinearArgs p = {x8, w8, x_scale, w_scale, y, offs, k, k, y_stride, k * n_out, 0, groups, (int)rows, 0, n_out, (int)k, 1, 0, 0};
   const ActArgs q = {p, bias, residual, nullptr, nullptr, residual_stride, 0, act};
   const hipStream_t st = (hipStream_t)hip_stream;
-  if (const int few = few_rows(q, FORWARD, 1))
+  if (const int few = few_rows8(q))
     return y_precision == GAN_FP32 ? launch_few<uint8_t, false, float>(q, few, st) : launch_few<uint8_t, false, bf16_t>(q, few, st);
   return y_precision == GAN_FP32 ? launch_large<EIGHT_BITS, FORWARD, float>(q, st) : launch_large<EIGHT_BITS, FORWARD, bf16_t>(q, st);
 }

@@ -225,7 +225,8 @@ def test_without_an_epilogue_it_is_the_plain_product(bf16):
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("offs,n_in,n_out", SHAPES8 + [CASES[n] for n in ("many", "odd", "long", "wide outputs", "few ends, outputs")] +
-                         [(offsets([30, 33, 0, 64, 65, 20, 1, 40]), 600, 4200), (offsets([300, 0, 129, 90]), 520, 6000)])                     # (297 tiles for two sets of waves, 329 for one)
+                         [(offsets([30, 33, 0, 64, 65, 20, 1, 40]), 600, 4200), (offsets([300, 0, 129, 90]), 520, 6000),                       # (297 tiles for two sets of waves, 329 for one)
+                          (offsets([40, 0, 70, 20, 32, 33, 1, 50]), 4000, 1100)])      # (few tiles of a long sum)
 def test_eight_bits(offs, n_in, n_out, bf16):
     torch = U.torch_mod()
     x8, xs, w8, ws = problem8(offs, n_in, n_out, 3)
