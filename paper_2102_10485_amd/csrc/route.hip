@@ -221,7 +221,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
       }
     } else {
       if (a.normalize && lane == 0 && best >= THERE)
-        for (int j = 0; j < a.k; ++j) weights[at * a.k + j] /= of_all;
+        for (int j = 0; j < a.k && ids[at * a.k + j] >= 0; ++j) weights[at * a.k + j] /= of_all;  // (0 behind them, also where of_all is NaN)
       __syncthreads();
       const int n = (int)(a.rows - first < R ? a.rows - first : R) * a.k;
       for (int i = threadIdx.x; i < n; i += 256) {
