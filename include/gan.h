@@ -423,7 +423,8 @@ gan_status gan_sort_by_label(const int32_t* labels, int64_t n, int32_t groups, i
      gan_combine_rows           y[i] = residual[i] + sum over s of weight[i][s] out[place[i][s]], without those of no expert; residual NULL: none; weight NULL: all 1,
                                 which is gan_gather_rows' gradient.  y may be the memory of residual, if the strides are the same.
      gan_combine_rows_backward  dout[place[i][s]] = weight[i][s] dy[i] (zero for rows of no expert), dweight[i][s] = the sum of dy[i] * out[place[i][s]] over the
-                                columns, 0 for choices of no expert; either may be NULL.  dout may be the memory of out, if the strides are the same.  (residual's gradient is dy.) */
+                                columns, 0 for choices of no expert; either may be NULL, and out with dweight, for which alone it is read.  dout may be the memory of out, if the
+                                strides are the same.  (residual's gradient is dy.) */
 gan_status gan_gather_rows(int32_t precision, const void* x, int64_t x_stride, const int32_t* place, const int32_t* offs, int32_t groups, int32_t k, int64_t rows,
                            int32_t cols, void* out, int64_t out_stride, void* hip_stream);
 gan_status gan_combine_rows(int32_t precision, const void* out, int64_t out_stride, const int32_t* place, const float* weight, const int32_t* offs, int32_t groups, int32_t k,

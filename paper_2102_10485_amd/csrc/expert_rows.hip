@@ -243,8 +243,9 @@ struct CombineBackArgs {
   int cols, k, groups, n;
 };
 
-// WAVES waves a row (blocks of four waves), four choices at a time.
-template <typename T, int WAVES, bool VEC, bool PAST>
+// WAVES waves a row (blocks of four waves), four choices at a time.  DOTS: with dweight, for which alone `out` is read (16384 x 4096 to two in bf16 122 us, without 59; 1117 x 1000 to three in
+// fp32 7.3, 6.2; with the question in the kernel 2000 x 2048 to two took 9.0 us for 8.4).
+template <typename T, int WAVES, bool VEC, bool PAST, bool DOTS>
 __global__ __launch_bounds__(256) void combine_back_kernel(CombineBackArgs a) {
   __shared__ float part[4][AT_ONCE];
   constexpr int ROWS = 4 / WAVES;
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(256) void combine_back_kernel(CombineBackArgs a) {
           raw.template load<VEC>((const T*)a.dy + row * a.dy_stride + col, left);
 #pragma unroll
           for (int j = 0; j < AT_ONCE; ++j)
-            if ((unsigned)p[j] < (unsigned)routed) out[j].template load<VEC>((const T*)a.out + p[j] * a.out_stride + col, left);
+            if (DOTS && (unsigned)p[j] < (unsigned)routed) out[j].template load<VEC>((const T*)a.out + p[j] * a.out_stride + col, left);
           float d[8];
           raw.values(d);
 #pragma unroll
@@ -278,16 +279,17 @@ __global__ __launch_bounds__(256) void combine_back_kernel(CombineBackArgs a) {
             if ((unsigned)p[j] >= (unsigned)a.n) continue;
             float o[8] = {};
             if (p[j] < routed) {
-              out[j].values(o);
+              if constexpr (DOTS) out[j].values(o);
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
-                dot[j] += d[i] * o[i];
+                if constexpr (DOTS) dot[j] += d[i] * o[i];
                 o[i] = w[j] * d[i];
               }
             }
             if (a.dout) store8<T, VEC, PAST>((T*)a.dout + p[j] * a.dout_stride + col, left, o);
           }
         }
+      if constexpr (!DOTS) continue;
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j)
 #pragma unroll
@@ -299,7 +301,7 @@ __global__ __launch_bounds__(256) void combine_back_kernel(CombineBackArgs a) {
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) dot[j] = part[0][j] + part[1][j] + part[2][j] + part[3][j];
       }
-      if (a.dweight && in && lane < AT_ONCE && s0 + lane < a.k)
+      if (in && lane < AT_ONCE && s0 + lane < a.k)
         a.dweight[row * a.k + s0 + lane] = lane == 0 ? dot[0] : lane == 1 ? dot[1] : lane == 2 ? dot[2] : dot[3];
     }
   }
@@ -407,22 +409,27 @@ extern "C" gan_status gan_combine_rows_backward(int32_t precision, const void* d
                                                 const float* weight, const int32_t* offs, int32_t groups, int32_t k, int64_t rows, int32_t cols, void* dout, int64_t dout_stride,
                                                 float* dweight, void* hip_stream) {
   if (const gan_status s = check_exchange(precision, rows, cols, groups, k)) return s;
-  if (!offs || (rows > 0 && (!dy || !out || !place))) return operator_fail(GAN_E_ARG, "dy, out, place or offs is NULL");
+  if (!offs || (rows > 0 && (!dy || !place))) return operator_fail(GAN_E_ARG, "dy, place or offs is NULL");
+  if (rows > 0 && dweight && !out) return operator_fail(GAN_E_ARG, "out, which dweight is made of, is NULL");
   for (const gan_status s : {check_matrix(dy, dy_stride, cols, "dy_stride is below cols"), check_matrix(out, out_stride, cols, "out_stride is below cols"),
                              check_matrix(dout, dout_stride, cols, "dout_stride is below cols")})
     if (s) return s;
-  if (rows == 0) return GAN_OK;
+  if (rows == 0 || (!dout && !dweight)) return GAN_OK;
   operator_launches();
   const int e = precision == GAN_FP32 ? 4 : 2;
-  const bool vec = cols % 8 == 0 && rows_aligned16(dy, dy_stride, e) && rows_aligned16(out, out_stride, e) && (!dout || rows_aligned16(dout, dout_stride, e));
+  const bool vec = cols % 8 == 0 && rows_aligned16(dy, dy_stride, e) && (!dweight || rows_aligned16(out, out_stride, e)) && (!dout || rows_aligned16(dout, dout_stride, e));
   const CombineBackArgs a = {dy, out, dout, place, offs, weight, dweight, dy_stride, out_stride, dout_stride, rows, cols, k, groups, (int)(rows * k)};
   const hipStream_t st = (hipStream_t)hip_stream;
   const bool wide = cols > 1024;
   const dim3 grid((unsigned)std::min(wide ? (long long)rows : ((long long)rows + 3) / 4, 1ll << 20));
+  // (In fp32 without dweight they go through the caches: nothing is read between a lane's two stores of a row, and past the caches these reach memory as half lines.  us through and past,
+  // 8192 x 1024 to four: 29, 65; 16384 x 2048 to two: 76, 105; with dweight 58, 55 and 128, 139; bf16 without, 16384 x 4096 to two: 72, 59.)
   const bool past = rows * k * cols * e > PAST_CACHES;
 #define GAN_COMBINE_BACK(T, W, V) \
-  if (V && past) hipLaunchKernelGGL((combine_back_kernel<T, W, V, V>), grid, dim3(256), 0, st, a); \
-  else hipLaunchKernelGGL((combine_back_kernel<T, W, V, false>), grid, dim3(256), 0, st, a)
+  if (dweight && V && past) hipLaunchKernelGGL((combine_back_kernel<T, W, V, V, true>), grid, dim3(256), 0, st, a); \
+  else if (dweight) hipLaunchKernelGGL((combine_back_kernel<T, W, V, false, true>), grid, dim3(256), 0, st, a); \
+  else if (V && past && sizeof(T) == 2) hipLaunchKernelGGL((combine_back_kernel<T, W, V, V && sizeof(T) == 2, false>), grid, dim3(256), 0, st, a); \
+  else hipLaunchKernelGGL((combine_back_kernel<T, W, V, false, false>), grid, dim3(256), 0, st, a)
   if (precision == GAN_FP32) {
     if (wide) { if (vec) { GAN_COMBINE_BACK(float, 4, true); } else { GAN_COMBINE_BACK(float, 4, false); } }
     else { if (vec) { GAN_COMBINE_BACK(float, 1, true); } else { GAN_COMBINE_BACK(float, 1, false); } }
