@@ -40,7 +40,7 @@ MEASURED_TRAFFIC = {
 
 
 # the operators for label experts, of which the step compiles and launches nothing
-OPERATOR_SOURCES = {"activation.h", "adamw.hip", "code_walk.h", "dropout.hip", "expert_rows.hip", "group_act.hip", "group_linear.hip", "group_linear_act.hip", "group_product.h",
+OPERATOR_SOURCES = {"activation.h", "adamw.hip", "code_walk.h", "dropout.hip", "expert_rows.hip", "few_rows.h", "group_act.hip", "group_linear.hip", "group_linear_act.hip", "group_product.h",
                     "group_tiles.h", "operators.h", "operators.hip", "rms_norm.hip", "route.hip", "row_chunks.h"}
 
 

@@ -18,6 +18,7 @@
 
 #include "activation.h"
 #include "code_walk.h"
+#include "few_rows.h"
 #include "group_tiles.h"
 #include "lds_copy.h"
 #include "operators.h"
@@ -1367,13 +1368,10 @@ gan_status launch_few_dgrad_as(const Q& q, hipStream_t st) {
 }
 template <typename T, bool ANY_ROWS, typename Q>
 gan_status launch_few_dgrad(const Q& q, int sixteens, hipStream_t st) {
-  // In fp32 32 rows a block where they leave blocks enough, or the sum is short (us with an epilogue, 16 rows, 32): ten experts of 112, 784 <- 512 (585 blocks of 32) 25.8, 20.0; eight of 250,
-  // 1024 <- 1024 (1120) 55.3, 54.1; one of 1000, 512 <- 512 (256) 9.8, 9.1; but four of 75, 2048 <- 1024 (416) 22.6, 24.3; 16 of 25, 1024 <- 2048 (448) 41.9, 45.7; ten of 112, 110 <- 6272
-  // (90) 41, 61.  The sums' order is the same.
-  if constexpr (sizeof(T) == 4) {
-    const bool two = q.rows / most_groups(q) > 16 && (q.k <= 512 || most_tiles(q.rows, q.groups, 32) * ceil_div(q.n, 64) >= 512);
-    return two ? launch_few_dgrad_as<T, 2, 2, 8, false>(q, st) : launch_few_dgrad_as<T, 1, 2, 8, false>(q, st);
-  }
+  // (fp32: the sums' order is the same by 16 rows and by 32)
+  if constexpr (sizeof(T) == 4)
+    return dgrad_sixteens(q.rows / most_groups(q), most_tiles(q.rows, q.groups, 32) * ceil_div(q.n, 64), q.k) == 2 ? launch_few_dgrad_as<T, 2, 2, 8, false>(q, st)
+                                                                                                              : launch_few_dgrad_as<T, 1, 2, 8, false>(q, st);
   else return sixteens == 2 ? launch_few_dgrad_as<T, 2, 2, 8, ANY_ROWS>(q, st) : launch_few_dgrad_as<T, 1, 2, 8, ANY_ROWS>(q, st);
 }
 
