@@ -1335,12 +1335,10 @@ gan_status launch_large(const Q& q, hipStream_t st) {
   if constexpr (F != ANY)
     if (big) return launch_tiles<F, KIND, 256, 256, 2, 4, 1, C>(q, st);
   // With an epilogue: up to a tile a CU, as two sets of waves leave room for one block (us without, with: eight experts of 992 rows, 704 -> 512 (280 tiles), 17, 26, in 8 bits 19, 28; of 250,
-  // 1024 -> 2048 (368) 22, 32; one of 4000, 4096 -> 1024 (256) 49, 42, 51, 44), and in 8 bits, whose steps wait for the conversion, up to 576 where experts have up to 64 rows, whose tiles are
-  // half as high: eight of 32, 4096 -> 4096 (320) 42, 39, of 62 (352) 47, 44, of 16 (288) 42, 37; 16 of 25, 2048 -> 2048 (304) 23, 22; but a hundred of 16, 1024 -> 1024 (896) 41, 55, and eight of
-  // 125 (480) 60, 74.
-  // In bf16 the first is 62, 68.  (Products without an epilogue keep the order of their sums.)
+  // 1024 -> 2048 (368) 22, 32; one of 4000, 4096 -> 1024 (256) 49, 42, 51, 44), and in 8 bits, whose steps wait for the conversion, where it is a tile a CU though this count is higher (few_rows.h).
+  // In bf16 that is slower (eight of 32, 4096 -> 4096 62, 68).  (Products without an epilogue keep the order of their sums.)
   const long long count = tiles(q, 128, 128);
-  const bool two = !std::is_same_v<Q, ActArgs> ? count <= 288 : count <= 256 || (F == EIGHT_BITS && count <= 576 && q.rows / most_groups(q) <= 64);
+  const bool two = !std::is_same_v<Q, ActArgs> ? count <= 288 : count <= 256 || (F == EIGHT_BITS && two_sets8(q.rows / most_groups(q), most_groups(q), ceil_div(q.n, 128), q.k));
   if constexpr (KIND != WGRAD)
     if (two && q.k >= 512) return launch_tiles<F, KIND, 128, 128, 2, 2, 2, C>(q, st);
   return launch_tiles<F, KIND, 128, 128, 2, 2, 1, C>(q, st);

@@ -1,4 +1,5 @@
-"""How many rows a block of the fp32 gradient for few rows takes (csrc/few_rows.h), on the host: no length of the sum is a case of its own, and calls of few blocks keep 16 rows."""
+"""The rules for products of few rows (csrc/few_rows.h), on the host.  Rows of a block of the fp32 gradient: no length of the sum is a case of its own, and calls of few blocks keep 16 rows.  Two sets of
+waves for an 8-bit tile: only where every tile, whatever the heights, has a CU of its own."""
 import ctypes
 import os
 import subprocess
@@ -9,12 +10,18 @@ from tests.test_code_walk import ROOT
 
 
 @pytest.fixture(scope="module")
-def sixteens(tmp_path_factory):
+def rules(tmp_path_factory):
     so = str(tmp_path_factory.mktemp("few_rows") / "few_rows.so")
     subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", os.path.join(ROOT, "tests", "c", "few_rows_host.cpp"), "-o", so], check=True)
-    fn = ctypes.CDLL(so).dgrad_sixteens
-    fn.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int]
-    return fn
+    lib = ctypes.CDLL(so)
+    lib.dgrad_sixteens.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int]
+    lib.two_sets8.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int]
+    return lib
+
+
+@pytest.fixture(scope="module")
+def sixteens(rules):
+    return rules.dgrad_sixteens
 
 
 @pytest.mark.parametrize("k", [512, 513, 520, 640, 1024, 4096])
@@ -30,3 +37,18 @@ def test_more_blocks_and_shorter_sums_never_turn_back(sixteens):
     for k in (512, 576, 577, 2048):
         of_blocks = [sixteens(100, b, k) for b in range(1, 2000)]
         assert of_blocks == sorted(of_blocks) and of_blocks[-1] == 2
+
+
+def test_two_sets_of_waves_have_a_cu_for_every_tile(rules):
+    """Tiles of the two heights are dealt to eight XCDs of 32 CUs apart: at most 32 on each, however the experts fall to the heights."""
+    taken = 0
+    for groups in range(1, 300):
+        for cols in range(1, 300):
+            if not rules.two_sets8(40, groups, cols, 4096):
+                assert groups * cols > 240
+                continue
+            taken += 1
+            assert all(-(-high * cols // 8) + -(-(groups - high) * cols // 8) <= 32 for high in range(groups + 1)), (groups, cols)
+    assert taken > 500
+    assert not rules.two_sets8(65, 2, 2, 4096) and not rules.two_sets8(32, 8, 32, 1024)          # (more than one height of tile; a short sum)
+    assert rules.two_sets8(32, 8, 32, 4096) and not rules.two_sets8(32, 16, 20, 2048) and not rules.two_sets8(40, 64, 6, 1024)
