@@ -380,7 +380,7 @@ gan_status gan_group_linear8(const uint8_t* x8, const uint8_t* x_scale, const ui
      gan_group_act_backward      dz = dy act'(z)  [rows][cols], dbias[g] = sum of dz (before its rounding) over g's rows  fp32 [groups][cols], zero for an expert without
                                  rows; dz or dbias may be NULL.  GAN_ACT_NONE: z is not read.  work: DEVICE, gan_group_act_backward_bytes(...) (0: none is needed), 16-byte aligned (dbias NULL: none).
    Rows of no expert: all their results are zero.  y may be the memory of residual, dx that of other or z, dz that of dy or z, if the strides are the same; z and y are two
-   matrices.  The activations at infinity are their limits; act' of GAN_ACT_RELU is 0 at zero. */
+   matrices.  The activations at infinity are their limits; act' of GAN_ACT_RELU is 0 at zero; values and slopes of the other two below 2^-119 may be 0. */
 typedef enum { GAN_ACT_NONE = 0, GAN_ACT_RELU = 1, GAN_ACT_GELU = 2 /* z times the normal distribution's Phi(z) */, GAN_ACT_SILU = 3 /* z / (1 + exp(-z)) */ } gan_act;
 gan_status gan_group_linear_act(int32_t precision, const void* x, int64_t x_stride, const void* w, const int32_t* offs, int32_t groups, int64_t rows, int32_t n_in,
                                 int32_t n_out, const float* bias, int32_t act, const void* residual, int64_t residual_stride, void* z, int64_t z_stride, void* y,

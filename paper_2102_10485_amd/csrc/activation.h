@@ -4,7 +4,8 @@
 //   GAN_ACT_GELU  z Phi(z)          Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi)       (Phi: the normal distribution's; no approximation by tanh)
 //   GAN_ACT_SILU  z s(z)            s(z) (1 + z (1 - s(z))),  s(z) = 1 / (1 + exp(-z))
 //
-// At infinity they are their limits; NaN stays NaN.
+// At infinity they are their limits; NaN stays NaN.  Results below 2^-119 may be zero: from z = -88.7 down, where SiLU is -2.6e-37, its exp(-z) is infinite in fp32, and the hardware's reciprocal, which
+// results in bf16 take, has no numbers below 2^-126.
 #pragma once
 
 #include "operators.h"
@@ -16,8 +17,9 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 // The normal distribution's tail beyond a = |z|, Phi(-a), and bell = exp(-a^2 / 2): bell times a polynomial of t = 1 / (1 + 0.305 a), fitted to exp(a^2 / 2) erfc(a / sqrt 2) / 2 on
 // [0, 13] with the least largest relative error.
-//   NEAR   six terms, 4.7e-6: for results that are rounded to bf16 (half a step is 2^-9 of the value); 15 instructions, where erfc and exp take 80
-//   else   eight terms, 1e-7: what an fp32 evaluation of any formula keeps where Phi is of size one
+//   NEAR   six terms, 4.5e-6 (4.7e-6 in fp32): for results that are rounded to bf16 (half a step is 2^-8 of the value); 15 instructions, where erfc and exp take 80
+//   else   eight terms, 1.27e-7 with the coefficients in fp32, which is two roundings of 2^-24: what an fp32 evaluation of any formula keeps where Phi is of size one.  Those of
+//          the reciprocal, the exponential and the products come on top
 //   EXACT  and the exponent a^2 / (2 ln 2) with the rounding errors of its products, which would cost a^2 roundings of the value
 enum Accuracy { NEAR, FULL, EXACT };
 template <Accuracy A>

@@ -28,6 +28,8 @@ struct ActBackArgs {
 // ten experts' 1117 rows of 512 in fp32 7.9).
 constexpr int LANES = 16, WIDE = LANES * 8, AT = 256 / LANES;     // lanes of a row, columns of a tile, its rows at a time
 // Up to so many rows a block takes all of an expert's, and the second launch is saved (a training pass through 64 experts of 128 -> 128 with 8 rows, whose time is the host's: 30.4 us with both, 26.6 so).
+// us of a call in bf16 so, and in tiles with sums: 8 rows of 64 experts, 128 columns 4.3, 7.2; 256 of eight, 1024 5.2, 7.4; 500 of a hundred, 1024 5.4, 12.3; 512 of eight, 4096 7.0, 9.3.  It loses where one or
+// a few experts have all rows, which leave few blocks with long turns: 512 of four, 1024 8.8, 7.5; 300 of one, 512 14.8, 7.3; 512 of one, 4096 23.1, 8.7, in fp32 1024 28.7, 8.0.
 constexpr int ALL_ROWS = 512;
 int wide_tiles(int cols) { return (cols + WIDE - 1) / WIDE; }
 int tall_of(long long rows, int cols) { return rows / 128 * wide_tiles(cols) >= 512 ? 128 : 32; }
